@@ -392,6 +392,136 @@ petra_status petra_net_probe_backprop(petra_net* net, const void* images, const 
 petra_status petra_net_backprop_step(petra_net* net, const void* images, const int32_t* labels,
                                      float* loss, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Operators of stages over tokens: attention, the coupling of a residual
+ * function to its stream with norms, gate and residual scale, and dropout.
+ *
+ * They are stateless: a description, device pointers and a stream a call, no
+ * handle.  The conventions above hold (the caller owns all memory, workspaces
+ * included; work is ordered on `stream` only; errors are found on the host
+ * before anything is enqueued; nothing is allocated, so calls may be captured
+ * in a HIP graph).  A workspace holds nothing between calls; calls that
+ * overlap in time need one each.  Results do not depend on timing: no sum is
+ * taken by atomic additions.
+ *
+ * Dropout.  `rng` points to two 64-bit device numbers {seed, offset}, read by
+ * the kernels.  An element is kept if its 16 bits of Philox-4x32 (7 rounds, key
+ * seed, counter (group, offset)) are at least round(65536 p), and then divided
+ * by the share kept, 1 - round(65536 p) / 65536.  No mask is stored: a backward
+ * (or a recomputed forward) with the same {seed, offset} has the same mask, so a
+ * micro-batch in flight keeps 16 bytes; a new call takes a new offset.  Group i
+ * of a tensor is its elements 8 i .. 8 i + 7.  rng may be NULL where the
+ * dropout probability is 0.
+ * ------------------------------------------------------------------------ */
+
+/* Attention.  For query i of head h in batch row b, over the visible keys j of
+ * key head h / (heads / kv_heads):
+ *   lse_i = log sum_j exp(scale q_i.k_j),  p_ij = exp(scale q_i.k_j - lse_i),
+ *   o_i = sum_j m_ij p_ij v_j
+ * Visible are the keys j < kv_lens[b], and with `causal` j <= i + kv_lens[b] -
+ * q_lens[b] (the last query sees every key).  A query without visible keys, or
+ * at or past q_lens[b], has o = 0, lse = -inf and takes no part in any gradient.
+ * Nothing at or past the lengths is used, whatever it holds.  m is dropout's 0
+ * or 1 / (share kept); its groups are, for each row (b, h, i), the keys 16 a +
+ * 4 c + {0, 1, 2, 3, 8, 9, 10, 11} for c = 0, 1, in the order (b, h, i, a, c).
+ *
+ * Layout: tensors [batch][q_len or kv_len][heads or kv_heads][head_dim] with the
+ * given strides, in elements, of the first three dimensions (all three zero:
+ * contiguous); channels are contiguous.  o and d_o have o_stride; a gradient has
+ * its tensor's strides.  lse is fp32 [batch][heads][q_len].
+ * Limits: heads a multiple of kv_heads; head_dim a multiple of 8, at most 128;
+ * strides not negative and multiples of 16 bytes, those of written tensors such
+ * that no elements share memory, a token stride of k and v below 2^22 elements;
+ * q_len * heads / kv_heads and kv_len at most 2^30, batch * kv_heads at most
+ * 65535; scale > 0. */
+typedef struct {
+  int32_t batch, q_len, kv_len;
+  int32_t heads, kv_heads, head_dim;
+  int32_t dtype;    /* petra_dtype */
+  int32_t causal;
+  float scale;
+  float dropout;    /* probability of dropping, 0 <= p < 1 - 2^-17 */
+  int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];   /* batch, token, head */
+} petra_attn_desc;
+
+/* Workspace of the two calls, in bytes (may be 0). */
+petra_status petra_attn_query(const petra_attn_desc* desc, size_t* forward_bytes,
+                              size_t* backward_bytes);
+/* q_lens, kv_lens: device int32 [batch] (nullable: full lengths; values are
+ * taken as if clamped to 0 .. q_len, kv_len).  Writes o and lse. */
+petra_status petra_attn_forward(const petra_attn_desc* desc, const void* q, const void* k,
+                                const void* v, const int32_t* q_lens, const int32_t* kv_lens,
+                                const uint64_t* rng, void* o, float* lse, void* workspace,
+                                size_t workspace_bytes, void* stream);
+/* o, lse: the forward's, of the same inputs and rng.  Writes dq, dk, dv whole
+ * (zeros where nothing is visible); gradients of a shared key head are summed
+ * over its query heads. */
+petra_status petra_attn_backward(const petra_attn_desc* desc, const void* q, const void* k,
+                                 const void* v, const void* o, const float* lse, const void* d_o,
+                                 const int32_t* q_lens, const int32_t* kv_lens,
+                                 const uint64_t* rng, void* dq, void* dk, void* dv,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* Coupling of a residual function's output f to a stream x, row by row (a row is
+ * a token's width channels, contiguous), with the norm before the next function:
+ *   y = residual_scale x + gate m n(f; post),   u = n(y as stored; pre)
+ * n is a root-mean-square norm (z / sqrt(mean z^2 + eps) gamma) or a layer norm
+ * ((z - mean) / sqrt(var + eps) gamma + beta); m is dropout's.  Parameters are fp32
+ * [width]; beta is nullable in either norm.  gate is fp32 [rows / rows_per_gate][width]: row r takes
+ * gate r / rows_per_gate (0: one gate for all rows).
+ * Limits: width a multiple of 8, at most 8192; rows a multiple of
+ * rows_per_gate. */
+typedef enum { PETRA_NORM_RMS = 0, PETRA_NORM_LAYER = 1 } petra_norm;
+
+typedef struct {
+  int64_t rows;
+  int64_t rows_per_gate;
+  int32_t width;
+  int32_t dtype;           /* petra_dtype */
+  int32_t norm;            /* petra_norm */
+  float eps;               /* > 0 */
+  float residual_scale;    /* not 0 */
+  float dropout;           /* as in petra_attn_desc */
+} petra_coupling_desc;
+
+/* Parameters of one norm, or where their gradients go. */
+typedef struct {
+  float* gamma;
+  float* beta;   /* nullable */
+} petra_norm_params;
+
+petra_status petra_coupling_query(const petra_coupling_desc* desc, size_t* backward_bytes);
+/* f = NULL (with gate, post and y NULL): only u = n(x; pre), the norm before a
+ * stage's first function.  u = NULL (with pre NULL): only y.  y == x is allowed,
+ * and u == f; no other overlap. */
+petra_status petra_coupling_forward(const petra_coupling_desc* desc, const void* x, const void* f,
+                                    const float* gate, const petra_norm_params* post,
+                                    const petra_norm_params* pre, const uint64_t* rng, void* y,
+                                    void* u, void* stream);
+/* From y, f, the gradient dy of y and (nullable, with pre and dpre) du of u:
+ *   t = dy + (dn(y; pre)/dy)^T du,  dx = residual_scale t,
+ *   df = (dn(f; post)/df)^T (gate m t),  and the gradients of gate, post and pre,
+ * and rebuilds x = (y - gate m n(f; post)) / residual_scale (x nullable).  Gradients of
+ * parameters are written, not added; d*.beta is written where beta is given.
+ * f = NULL (with gate, post, x, df, dgate and dpost NULL): only dx and dpre, the
+ * norm before a stage's first function.
+ * x == y, dx == dy, df == f and dx == du are allowed; no other overlap. */
+petra_status petra_coupling_backward(const petra_coupling_desc* desc, const void* y,
+                                     const void* f, const void* dy, const void* du,
+                                     const float* gate, const petra_norm_params* post,
+                                     const petra_norm_params* pre, const uint64_t* rng, void* x,
+                                     void* dx, void* df, float* dgate,
+                                     const petra_norm_params* dpost,
+                                     const petra_norm_params* dpre, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/* y = residual + alpha m x over n elements (residual nullable: 0).  alpha = -1
+ * takes the same dropout off again: the inverse of a coupling y = x + m f.  With
+ * x a gradient it is the backward.  y == x and y == residual are allowed, no other
+ * overlap with them. */
+petra_status petra_dropout(int64_t n, int32_t dtype, float p, float alpha, const void* x,
+                           const void* residual, const uint64_t* rng, void* y, void* stream);
+
 /* Measurement support (not part of the method).  petra_stage_profile(st, 1)
  * clears the counters and starts bracketing every kernel launch of the stage
  * with HIP events on the stream the kernel is launched on; 0 stops it.

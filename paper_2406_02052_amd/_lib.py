@@ -70,6 +70,29 @@ class NetMem(ctypes.Structure):
                 ("total", ctypes.c_int64)]
 
 
+class AttnDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("q_len", ctypes.c_int32), ("kv_len", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("dropout", ctypes.c_float), ("q_stride", ctypes.c_int64 * 3),
+                ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3),
+                ("o_stride", ctypes.c_int64 * 3)]
+
+
+class CouplingDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("rows_per_gate", ctypes.c_int64),
+                ("width", ctypes.c_int32), ("dtype", ctypes.c_int32), ("norm", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float),
+                ("dropout", ctypes.c_float)]
+
+
+class NormParams(ctypes.Structure):
+    _fields_ = [("gamma", ctypes.c_void_p), ("beta", ctypes.c_void_p)]
+
+
+PETRA_NORM_RMS, PETRA_NORM_LAYER = 0, 1
+
 # petra_bwd_mode
 BWD_RECONSTRUCT, BWD_INPUT_BUFFER, BWD_PARAM_BUFFER, BWD_DELAYED = 0, 1, 2, 3
 
@@ -117,6 +140,22 @@ _SIGS = {
     "petra_net_memory": (ctypes.c_int, [_VP, ctypes.c_int32, ctypes.POINTER(NetMem)]),
     "petra_net_probe_tick": (ctypes.c_int, [_VP, ctypes.c_int32, _VP, _VP]),
     "petra_net_probe_backprop": (ctypes.c_int, [_VP, _VP, _VP, _VP, _VP]),
+    "petra_attn_query": (ctypes.c_int, [ctypes.POINTER(AttnDesc), ctypes.POINTER(ctypes.c_size_t),
+                                        ctypes.POINTER(ctypes.c_size_t)]),
+    "petra_attn_forward": (ctypes.c_int, [ctypes.POINTER(AttnDesc)] + [_VP] * 9 +
+                           [ctypes.c_size_t, _VP]),
+    "petra_attn_backward": (ctypes.c_int, [ctypes.POINTER(AttnDesc)] + [_VP] * 13 +
+                            [ctypes.c_size_t, _VP]),
+    "petra_coupling_query": (ctypes.c_int, [ctypes.POINTER(CouplingDesc),
+                                            ctypes.POINTER(ctypes.c_size_t)]),
+    "petra_coupling_forward": (ctypes.c_int, [ctypes.POINTER(CouplingDesc), _VP, _VP, _VP,
+                                              ctypes.POINTER(NormParams),
+                                              ctypes.POINTER(NormParams), _VP, _VP, _VP, _VP]),
+    "petra_coupling_backward": (ctypes.c_int, [ctypes.POINTER(CouplingDesc)] + [_VP] * 5 +
+                                [ctypes.POINTER(NormParams)] * 2 + [_VP] * 5 +
+                                [ctypes.POINTER(NormParams)] * 2 + [_VP, ctypes.c_size_t, _VP]),
+    "petra_dropout": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_float,
+                                     ctypes.c_float, _VP, _VP, _VP, _VP, _VP]),
     "petra_stage_forward_noalloc": (ctypes.c_int, [_VP, _VP, _VP, _VP, _VP, _VP]),
     "petra_stage_profile": (ctypes.c_int, [_VP, ctypes.c_int32]),
     "petra_stage_profile_read": (ctypes.c_int, [_VP, ctypes.c_int32,
@@ -411,3 +450,65 @@ def petra_net_state(handle):
     _check(load().petra_net_state(handle, ctypes.byref(t), ctypes.byref(fed), ctypes.byref(fl)),
            "petra_net_state")
     return t.value, fed.value, fl.value
+
+
+# ---- operators of stages over tokens -----------------------------------------
+
+def petra_attn_query(desc: AttnDesc):
+    """Workspace bytes of (the forward, the backward)."""
+    fwd, bwd = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(load().petra_attn_query(ctypes.byref(desc), ctypes.byref(fwd), ctypes.byref(bwd)),
+           "petra_attn_query")
+    return fwd.value, bwd.value
+
+
+def petra_attn_forward(desc: AttnDesc, q, k, v, q_lens, kv_lens, rng, o, lse, workspace,
+                       workspace_bytes: int, stream=None) -> None:
+    _check(load().petra_attn_forward(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(q_lens),
+                                     _ptr(kv_lens), _ptr(rng), _ptr(o), _ptr(lse),
+                                     _ptr(workspace), workspace_bytes, _stream(stream)),
+           "petra_attn_forward")
+
+
+def petra_attn_backward(desc: AttnDesc, q, k, v, o, lse, d_o, q_lens, kv_lens, rng, dq, dk, dv,
+                        workspace, workspace_bytes: int, stream=None) -> None:
+    _check(load().petra_attn_backward(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(o),
+                                      _ptr(lse), _ptr(d_o), _ptr(q_lens), _ptr(kv_lens),
+                                      _ptr(rng), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace),
+                                      workspace_bytes, _stream(stream)), "petra_attn_backward")
+
+
+def _norm(p):
+    """(gamma, beta or None) as the C structure; None stays."""
+    return None if p is None else ctypes.byref(NormParams(_ptr(p[0]), _ptr(p[1])))
+
+
+def petra_coupling_query(desc: CouplingDesc) -> int:
+    n = ctypes.c_size_t()
+    _check(load().petra_coupling_query(ctypes.byref(desc), ctypes.byref(n)),
+           "petra_coupling_query")
+    return n.value
+
+
+def petra_coupling_forward(desc: CouplingDesc, x, f, gate, post, pre, rng, y, u,
+                           stream=None) -> None:
+    """post and pre: (gamma, beta or None), or None."""
+    _check(load().petra_coupling_forward(ctypes.byref(desc), _ptr(x), _ptr(f), _ptr(gate),
+                                         _norm(post), _norm(pre), _ptr(rng), _ptr(y), _ptr(u),
+                                         _stream(stream)), "petra_coupling_forward")
+
+
+def petra_coupling_backward(desc: CouplingDesc, y, f, dy, du, gate, post, pre, rng, x, dx, df,
+                            dgate, dpost, dpre, workspace, workspace_bytes: int,
+                            stream=None) -> None:
+    _check(load().petra_coupling_backward(
+        ctypes.byref(desc), _ptr(y), _ptr(f), _ptr(dy), _ptr(du), _ptr(gate), _norm(post),
+        _norm(pre), _ptr(rng), _ptr(x), _ptr(dx), _ptr(df), _ptr(dgate), _norm(dpost),
+        _norm(dpre), _ptr(workspace), workspace_bytes, _stream(stream)),
+        "petra_coupling_backward")
+
+
+def petra_dropout(n: int, dtype: int, p: float, alpha: float, x, residual, rng, y,
+                  stream=None) -> None:
+    _check(load().petra_dropout(n, dtype, p, alpha, _ptr(x), _ptr(residual), _ptr(rng), _ptr(y),
+                                _stream(stream)), "petra_dropout")

@@ -194,6 +194,11 @@ hipError_t static_scratch(StaticScratch* out) {
 
 }  // namespace
 
+namespace petra {
+// Error reporting of the entry points in ops_api.hip.
+petra_status set_error(petra_status s, const std::string& msg) { return fail(s, msg); }
+}  // namespace petra
+
 extern "C" {
 
 const char* petra_status_str(petra_status s) {

@@ -1,0 +1,512 @@
+// extern "C" entry points of the token operators (attention, coupling, dropout):
+// argument validation and dispatch.  Nothing here allocates device memory.
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <string>
+
+#include "../../include/petra.h"
+#include "ops.h"
+
+namespace petra {
+petra_status set_error(petra_status s, const std::string& msg);
+}
+
+namespace {
+
+using petra::set_error;
+
+// Errors leave through this: thrown inside an entry point, caught at its end.
+struct Refused {
+  petra_status status;
+  std::string what;
+};
+
+void need(bool ok, petra_status s, const char* what) {
+  if (!ok) throw Refused{s, what};
+}
+
+// Runs an entry point's body, which says whether it enqueued work; nothing it throws
+// crosses the C boundary.
+template <typename F>
+petra_status entry(const char* name, F body) {
+  try {
+    const hipError_t e = body() ? hipGetLastError() : hipSuccess;
+    if (e != hipSuccess) return set_error(PETRA_ERR_HIP, std::string(name) + ": " + hipGetErrorString(e));
+    return PETRA_OK;
+  } catch (const Refused& r) {
+    return set_error(r.status, r.what);
+  } catch (...) {
+    return set_error(PETRA_ERR_STATE, std::string(name) + ": out of host memory");
+  }
+}
+
+size_t size_of(int32_t dtype) { return dtype == PETRA_BF16 ? 2 : 4; }
+
+void need_dtype(int32_t dtype) {
+  need(dtype == PETRA_FP32 || dtype == PETRA_BF16, PETRA_ERR_DTYPE, "dtype must be fp32 or bf16");
+}
+
+// A tensor's pointer: present unless it has no elements, 16-byte aligned.
+void need_ptr(const void* p, const char* name, bool empty = false) {
+  if (empty) return;
+  if (p == nullptr) throw Refused{PETRA_ERR_INVALID_ARG, std::string("null pointer: ") + name};
+  if (reinterpret_cast<uintptr_t>(p) & 15u)
+    throw Refused{PETRA_ERR_ALIGN, std::string("misaligned pointer: ") + name};
+}
+
+void need_int_ptr(const void* p, const char* name, uintptr_t align) {
+  if (p != nullptr && (reinterpret_cast<uintptr_t>(p) & (align - 1)))
+    throw Refused{PETRA_ERR_ALIGN, std::string("misaligned pointer: ") + name};
+}
+
+// A range of memory that a call reads or writes.
+struct Span {
+  const void* p;
+  size_t bytes;
+  const char* name;
+};
+
+bool overlap(const Span& a, const Span& b) {
+  if (a.p == nullptr || b.p == nullptr || a.bytes == 0 || b.bytes == 0) return false;
+  const char *x = static_cast<const char*>(a.p), *y = static_cast<const char*>(b.p);
+  return x < y + b.bytes && y < x + a.bytes;
+}
+
+void need_apart(const Span& a, const Span& b, bool same_allowed = false) {
+  if (same_allowed && a.p == b.p) return;
+  if (overlap(a, b)) throw Refused{PETRA_ERR_ALIAS, std::string("buffers overlap: ") + a.name + " and " + b.name};
+}
+
+// Threshold of the generator's 16 bits, 0 for no dropout.
+uint32_t need_dropout(float p, const uint64_t* rng, bool check_rng) {
+  need(p >= 0.f && p < 1.f, PETRA_ERR_INVALID_ARG, "dropout probability outside [0, 1)");
+  const long cut = std::lround(65536.0 * p);
+  need(cut < 65536, PETRA_ERR_INVALID_ARG, "dropout probability keeps nothing");
+  if (check_rng && cut > 0) need(rng != nullptr, PETRA_ERR_INVALID_ARG, "dropout without rng");
+  need_int_ptr(rng, "rng", 8);
+  return static_cast<uint32_t>(cut);
+}
+
+float inv_keep(uint32_t cut) { return static_cast<float>(65536.0 / (65536.0 - cut)); }
+
+void need_workspace(const void* w, size_t have, size_t want) {
+  if (want == 0) return;
+  need(w != nullptr && have >= want, PETRA_ERR_WORKSPACE, "workspace missing or too small");
+  need_ptr(w, "workspace");
+}
+
+// ---------------------------------------------------------------------------
+// attention
+// ---------------------------------------------------------------------------
+
+// Strides of [batch][len][heads][dim], contiguous where all three are zero.
+void strides(const int64_t in[3], int64_t out[3], int64_t len, int64_t heads, int64_t dim, size_t esz,
+             const char* name) {
+  const bool dense = in[0] == 0 && in[1] == 0 && in[2] == 0;
+  out[0] = dense ? len * heads * dim : in[0];
+  out[1] = dense ? heads * dim : in[1];
+  out[2] = dense ? dim : in[2];
+  for (int i = 0; i < 3; ++i) {
+    if (out[i] < 0 || out[i] > (int64_t{1} << 46))
+      throw Refused{PETRA_ERR_SHAPE, std::string("negative or too large stride: ") + name};
+    if (out[i] * static_cast<int64_t>(esz) % 16 != 0)
+      throw Refused{PETRA_ERR_ALIGN, std::string("stride not a multiple of 16 bytes: ") + name};
+  }
+}
+
+// No two elements of a written tensor share memory: by growing stride, each dimension
+// steps past what the smaller ones cover.
+void need_distinct(const int64_t st[3], const int64_t n[3], int64_t dim, const char* name) {
+  if (n[0] == 0 || n[1] == 0 || n[2] == 0) return;
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + 3, [&](int a, int b) { return st[a] < st[b]; });
+  int64_t extent = dim;
+  for (int i : order) {
+    if (n[i] <= 1) continue;
+    if (st[i] < extent) throw Refused{PETRA_ERR_SHAPE, std::string("elements share memory: ") + name};
+    extent += (n[i] - 1) * st[i];
+  }
+}
+
+struct Attn {
+  petra::AttnArgs a{};
+  petra::AttnPlan plan{};
+  size_t esz;
+
+  bool no_q() const { return a.batch == 0 || a.q_len == 0; }
+  bool no_kv() const { return a.batch == 0 || a.kv_len == 0; }
+
+  Attn(const petra_attn_desc* d, const uint64_t* rng, bool call, bool backward) {
+    need(d != nullptr, PETRA_ERR_INVALID_ARG, "null description");
+    need_dtype(d->dtype);
+    esz = size_of(d->dtype);
+    need(d->batch >= 0 && d->q_len >= 0 && d->kv_len >= 0, PETRA_ERR_SHAPE, "negative size");
+    need(d->heads >= 1 && d->kv_heads >= 1 && d->heads % d->kv_heads == 0, PETRA_ERR_SHAPE,
+         "heads must be a positive multiple of kv_heads");
+    need(d->head_dim >= 8 && d->head_dim <= 128 && d->head_dim % 8 == 0, PETRA_ERR_SHAPE,
+         "head_dim must be a multiple of 8, at most 128");
+    need(d->scale > 0.f && std::isfinite(d->scale), PETRA_ERR_INVALID_ARG, "scale must be positive and finite");
+    a.batch = d->batch;
+    a.q_len = d->q_len;
+    a.kv_len = d->kv_len;
+    a.heads = d->heads;
+    a.kv_heads = d->kv_heads;
+    a.group = d->heads / d->kv_heads;
+    a.dim = d->head_dim;
+    a.causal = d->causal != 0;
+    const int64_t most = int64_t{1} << 30;
+    need(static_cast<int64_t>(a.q_len) * a.group <= most && a.kv_len <= most, PETRA_ERR_SHAPE, "sequence too long");
+    need(static_cast<int64_t>(a.batch) * a.kv_heads <= 65535, PETRA_ERR_SHAPE, "batch * kv_heads above 65535");
+    a.scale = d->scale;
+    a.scale_log2 = d->scale * 1.44269504088896340736f;
+    a.cut = need_dropout(d->dropout, rng, call);
+    a.inv_keep = inv_keep(a.cut);
+    a.rng = a.cut > 0 ? rng : nullptr;
+    strides(d->q_stride, a.q_stride, a.q_len, a.heads, a.dim, esz, "q");
+    strides(d->k_stride, a.k_stride, a.kv_len, a.kv_heads, a.dim, esz, "k");
+    strides(d->v_stride, a.v_stride, a.kv_len, a.kv_heads, a.dim, esz, "v");
+    strides(d->o_stride, a.o_stride, a.q_len, a.heads, a.dim, esz, "o");
+    need(a.k_stride[1] < (1 << 22) && a.v_stride[1] < (1 << 22), PETRA_ERR_SHAPE,
+         "token stride of k or v of 2^22 elements or more");
+    const int64_t nq[3] = {a.batch, a.q_len, a.heads}, nk[3] = {a.batch, a.kv_len, a.kv_heads};
+    need_distinct(a.o_stride, nq, a.dim, "o");
+    if (backward) {
+      need_distinct(a.q_stride, nq, a.dim, "dq");
+      need_distinct(a.k_stride, nk, a.dim, "dk");
+      need_distinct(a.v_stride, nk, a.dim, "dv");
+    }
+    plan = petra::attn_plan(a, d->dtype);
+  }
+
+  // From a tensor's first element to its last; zero bytes for a strided one, whose
+  // elements may lie between another's.
+  Span dense(const void* p, const int64_t st[3], bool kv, const char* name) const {
+    const int64_t len = kv ? a.kv_len : a.q_len, heads = kv ? a.kv_heads : a.heads;
+    const int64_t n = a.batch * len * heads * a.dim;
+    int64_t extent = a.dim;
+    if (n > 0) extent += (a.batch - 1) * st[0] + (len - 1) * st[1] + (heads - 1) * st[2];
+    return {p, n > 0 && extent == n ? n * esz : n > 0 ? 1 : 0, name};
+  }
+};
+
+}  // namespace
+
+extern "C" {
+
+petra_status petra_attn_query(const petra_attn_desc* desc, size_t* forward_bytes, size_t* backward_bytes) {
+  return entry("petra_attn_query", [&]() -> bool {
+    const Attn t(desc, nullptr, false, false);
+    if (forward_bytes != nullptr) *forward_bytes = t.plan.fwd_bytes;
+    if (backward_bytes != nullptr) *backward_bytes = t.plan.bwd_bytes;
+    return false;
+  });
+}
+
+petra_status petra_attn_forward(const petra_attn_desc* desc, const void* q, const void* k, const void* v,
+                                const int32_t* q_lens, const int32_t* kv_lens, const uint64_t* rng, void* o,
+                                float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  return entry("petra_attn_forward", [&]() -> bool {
+    Attn t(desc, rng, true, false);
+    need_ptr(q, "q", t.no_q());
+    need_ptr(k, "k", t.no_kv());
+    need_ptr(v, "v", t.no_kv());
+    need_ptr(o, "o", t.no_q());
+    need_ptr(lse, "lse", t.no_q());
+    need_int_ptr(q_lens, "q_lens", 4);
+    need_int_ptr(kv_lens, "kv_lens", 4);
+    const Span so = t.dense(o, t.a.o_stride, false, "o");
+    const Span sl{lse, static_cast<size_t>(t.a.batch) * t.a.heads * t.a.q_len * 4, "lse"};
+    for (const Span& in : {t.dense(q, t.a.q_stride, false, "q"), t.dense(k, t.a.k_stride, true, "k"),
+                           t.dense(v, t.a.v_stride, true, "v")}) {
+      need_apart(so, in);
+      need_apart(sl, in);
+    }
+    need_apart(so, sl);
+    need_workspace(workspace, workspace_bytes, t.plan.fwd_bytes);
+    if (t.no_q()) return false;
+    t.a.q = q;
+    t.a.k = k;
+    t.a.v = v;
+    t.a.q_lens = q_lens;
+    t.a.kv_lens = kv_lens;
+    t.a.out = o;
+    t.a.lse = lse;
+    petra::attn_forward(t.a, t.plan, desc->dtype, workspace, static_cast<hipStream_t>(stream));
+    return true;
+  });
+}
+
+petra_status petra_attn_backward(const petra_attn_desc* desc, const void* q, const void* k, const void* v,
+                                 const void* o, const float* lse, const void* d_o, const int32_t* q_lens,
+                                 const int32_t* kv_lens, const uint64_t* rng, void* dq, void* dk, void* dv,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+  return entry("petra_attn_backward", [&]() -> bool {
+    Attn t(desc, rng, true, true);
+    const bool nq = t.no_q(), nk = t.no_kv();
+    need_ptr(q, "q", nq);
+    need_ptr(k, "k", nk);
+    need_ptr(v, "v", nk);
+    need_ptr(o, "o", nq);
+    need_ptr(lse, "lse", nq);
+    need_ptr(d_o, "d_o", nq);
+    need_ptr(dq, "dq", nq);
+    need_ptr(dk, "dk", nk);
+    need_ptr(dv, "dv", nk);
+    need_int_ptr(q_lens, "q_lens", 4);
+    need_int_ptr(kv_lens, "kv_lens", 4);
+    const Span in[6] = {t.dense(q, t.a.q_stride, false, "q"), t.dense(k, t.a.k_stride, true, "k"),
+                        t.dense(v, t.a.v_stride, true, "v"), t.dense(o, t.a.o_stride, false, "o"),
+                        t.dense(d_o, t.a.o_stride, false, "d_o"),
+                        {lse, static_cast<size_t>(t.a.batch) * t.a.heads * t.a.q_len * 4, "lse"}};
+    const Span out[3] = {t.dense(dq, t.a.q_stride, false, "dq"), t.dense(dk, t.a.k_stride, true, "dk"),
+                         t.dense(dv, t.a.v_stride, true, "dv")};
+    for (int i = 0; i < 3; ++i) {
+      for (const Span& s : in) need_apart(out[i], s);
+      for (int j = 0; j < i; ++j) need_apart(out[i], out[j]);
+    }
+    need_workspace(workspace, workspace_bytes, t.plan.bwd_bytes);
+    if (t.a.batch == 0) return false;
+    t.a.q = q;
+    t.a.k = k;
+    t.a.v = v;
+    t.a.o = o;
+    t.a.lse = const_cast<float*>(lse);
+    t.a.d_o = d_o;
+    t.a.q_lens = q_lens;
+    t.a.kv_lens = kv_lens;
+    t.a.dq = dq;
+    t.a.dk = dk;
+    t.a.dv = dv;
+    petra::attn_backward(t.a, t.plan, desc->dtype, workspace, static_cast<hipStream_t>(stream));
+    return true;
+  });
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// coupling
+// ---------------------------------------------------------------------------
+
+namespace {
+
+struct Coupling {
+  petra::CoupleArgs a{};
+  size_t bytes, param, gates;   // of an activation, a parameter vector, the gates
+
+  Coupling(const petra_coupling_desc* d, const uint64_t* rng, bool with_f) {
+    need(d != nullptr, PETRA_ERR_INVALID_ARG, "null description");
+    need_dtype(d->dtype);
+    need(d->rows >= 0 && d->rows_per_gate >= 0, PETRA_ERR_SHAPE, "negative size");
+    need(d->width >= 8 && d->width <= 8192 && d->width % 8 == 0, PETRA_ERR_SHAPE,
+         "width must be a multiple of 8, at most 8192");
+    need(d->rows <= (int64_t{1} << 31) - 64, PETRA_ERR_SHAPE, "too many rows");
+    need(d->norm == PETRA_NORM_RMS || d->norm == PETRA_NORM_LAYER, PETRA_ERR_INVALID_ARG, "unknown norm");
+    need(d->eps > 0.f && std::isfinite(d->eps), PETRA_ERR_INVALID_ARG, "eps must be positive and finite");
+    need(d->residual_scale != 0.f && std::isfinite(d->residual_scale), PETRA_ERR_INVALID_ARG,
+         "residual_scale must be finite and not 0");
+    a.rows = d->rows;
+    a.width = d->width;
+    a.rows_per_gate = d->rows_per_gate > 0 ? d->rows_per_gate : std::max<int64_t>(d->rows, 1);
+    need(a.rows % a.rows_per_gate == 0, PETRA_ERR_SHAPE, "rows must be a multiple of rows_per_gate");
+    a.gates = d->rows_per_gate > 0 ? a.rows / a.rows_per_gate : 1;
+    a.layer = d->norm == PETRA_NORM_LAYER;
+    a.eps = d->eps;
+    a.scale = d->residual_scale;
+    a.inv_scale = 1.f / d->residual_scale;
+    a.inv_width = 1.f / static_cast<float>(d->width);
+    a.cut = need_dropout(d->dropout, rng, with_f);
+    a.inv_keep = inv_keep(a.cut);
+    a.rng = with_f && a.cut > 0 ? rng : nullptr;
+    bytes = static_cast<size_t>(a.rows) * a.width * size_of(d->dtype);
+    param = static_cast<size_t>(a.width) * 4;
+    gates = static_cast<size_t>(a.gates) * param;
+    petra::couple_plan(a);
+  }
+
+  size_t part_bytes() const { return static_cast<size_t>(a.blocks) * param; }
+};
+
+void need_norm(const petra_norm_params* p, const char* name) {
+  if (p == nullptr) throw Refused{PETRA_ERR_INVALID_ARG, std::string("null pointer: ") + name};
+  need_ptr(p->gamma, name);
+  need_ptr(p->beta, name, p->beta == nullptr);
+}
+
+}  // namespace
+
+extern "C" {
+
+petra_status petra_coupling_query(const petra_coupling_desc* desc, size_t* backward_bytes) {
+  return entry("petra_coupling_query", [&]() -> bool {
+    const Coupling t(desc, nullptr, false);
+    if (backward_bytes != nullptr) *backward_bytes = 5 * t.part_bytes();
+    return false;
+  });
+}
+
+petra_status petra_coupling_forward(const petra_coupling_desc* desc, const void* x, const void* f,
+                                    const float* gate, const petra_norm_params* post,
+                                    const petra_norm_params* pre, const uint64_t* rng, void* y, void* u,
+                                    void* stream) {
+  return entry("petra_coupling_forward", [&]() -> bool {
+    Coupling t(desc, rng, f != nullptr);
+    const bool empty = t.a.rows == 0;
+    need_ptr(x, "x", empty);
+    if (f != nullptr) {
+      need_ptr(f, "f");
+      need_ptr(y, "y", empty);
+      need_ptr(gate, "gate", empty);
+      need_norm(post, "post");
+      t.a.post_gamma = post->gamma;
+      t.a.post_beta = post->beta;
+    } else {
+      need(empty || (y == nullptr && gate == nullptr && post == nullptr), PETRA_ERR_INVALID_ARG,
+           "y, gate and post belong to f");
+      need(empty || u != nullptr, PETRA_ERR_INVALID_ARG, "nothing to compute: neither f nor u");
+    }
+    if (u != nullptr) {
+      need_ptr(u, "u");
+      need_norm(pre, "pre");
+      t.a.pre_gamma = pre->gamma;
+      t.a.pre_beta = pre->beta;
+    }
+    const Span sx{x, t.bytes, "x"}, sf{f, t.bytes, "f"}, sy{y, t.bytes, "y"}, su{u, t.bytes, "u"},
+        sg{gate, t.gates, "gate"};
+    need_apart(sy, sx, true);
+    need_apart(sy, sf);
+    need_apart(sy, su);
+    need_apart(su, sf, true);
+    need_apart(su, sx);
+    need_apart(sy, sg);
+    need_apart(su, sg);
+    if (empty) return false;
+    t.a.x = x;
+    t.a.f = f;
+    t.a.gate = gate;
+    t.a.y = y;
+    t.a.u = u;
+    petra::couple_forward(t.a, desc->dtype, static_cast<hipStream_t>(stream));
+    return true;
+  });
+}
+
+petra_status petra_coupling_backward(const petra_coupling_desc* desc, const void* y, const void* f, const void* dy,
+                                     const void* du, const float* gate, const petra_norm_params* post,
+                                     const petra_norm_params* pre, const uint64_t* rng, void* x, void* dx, void* df,
+                                     float* dgate, const petra_norm_params* dpost, const petra_norm_params* dpre,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+  return entry("petra_coupling_backward", [&]() -> bool {
+    // without rows the parameters' gradients are still written
+    const bool with_f = post != nullptr, with_u = pre != nullptr;
+    Coupling t(desc, rng, with_f);
+    const bool empty = t.a.rows == 0;
+    need_ptr(y, "y", empty);
+    need_ptr(dy, "dy", empty);
+    need_ptr(dx, "dx", empty);
+    if (with_f) {
+      need_ptr(f, "f", empty);
+      need_ptr(df, "df", empty);
+      need_ptr(x, "x", empty || x == nullptr);
+      const bool no_gates = t.a.gates == 0;
+      need_ptr(gate, "gate", no_gates);
+      need_ptr(dgate, "dgate", no_gates);
+      need_norm(post, "post");
+      need_norm(dpost, "dpost");
+      need((post->beta != nullptr) == (dpost->beta != nullptr), PETRA_ERR_INVALID_ARG, "post and dpost differ in beta");
+    } else {
+      need(f == nullptr && gate == nullptr && x == nullptr && df == nullptr && dgate == nullptr && dpost == nullptr,
+           PETRA_ERR_INVALID_ARG, "f, gate, x, df, dgate and dpost belong to post");
+    }
+    if (with_u) {
+      need_ptr(du, "du", empty);
+      need_norm(pre, "pre");
+      need_norm(dpre, "dpre");
+      need((pre->beta != nullptr) == (dpre->beta != nullptr), PETRA_ERR_INVALID_ARG, "pre and dpre differ in beta");
+    } else {
+      need(du == nullptr && dpre == nullptr, PETRA_ERR_INVALID_ARG, "du and dpre belong to pre");
+    }
+    need(with_f || with_u, PETRA_ERR_INVALID_ARG, "nothing to compute: neither post nor pre");
+    const Span in[4] = {{y, t.bytes, "y"}, {dy, t.bytes, "dy"}, {f, t.bytes, "f"}, {du, t.bytes, "du"}};
+    const Span out[3] = {{x, t.bytes, "x"}, {dx, t.bytes, "dx"}, {df, t.bytes, "df"}};
+    const Span small[5] = {{dgate, t.gates, "dgate"},
+                           {with_f ? dpost->gamma : nullptr, t.param, "dpost.gamma"},
+                           {with_f ? dpost->beta : nullptr, t.param, "dpost.beta"},
+                           {with_u ? dpre->gamma : nullptr, t.param, "dpre.gamma"},
+                           {with_u ? dpre->beta : nullptr, t.param, "dpre.beta"}};
+    for (int i = 0; i < 3; ++i) {
+      for (int j = 0; j < 4; ++j) need_apart(out[i], in[j], i == j || (i == 1 && j == 3));
+      for (int j = 0; j < i; ++j) need_apart(out[i], out[j]);
+      for (const Span& s : small) need_apart(out[i], s);
+    }
+    const Span params[5] = {{gate, t.gates, "gate"},
+                            {with_f ? post->gamma : nullptr, t.param, "post.gamma"},
+                            {with_f ? post->beta : nullptr, t.param, "post.beta"},
+                            {with_u ? pre->gamma : nullptr, t.param, "pre.gamma"},
+                            {with_u ? pre->beta : nullptr, t.param, "pre.beta"}};
+    for (int i = 0; i < 5; ++i) {
+      for (const Span& s : in) need_apart(small[i], s);
+      for (const Span& s : params) need_apart(small[i], s);
+      for (const Span& s : out) need_apart(params[i], s);
+      for (int j = 0; j < i; ++j) need_apart(small[i], small[j]);
+    }
+    need_workspace(workspace, workspace_bytes, 5 * t.part_bytes());
+    petra::CoupleArgs& a = t.a;
+    a.y_in = y;
+    a.dy = dy;
+    a.dx = dx;
+    float* const ws = static_cast<float*>(workspace);
+    const size_t part = t.part_bytes() / 4;
+    if (with_f) {
+      a.f = empty ? y : f;
+      a.has_f = 1;
+      a.gate = gate;
+      a.x_out = x;
+      a.df = df;
+      a.dgate = dgate;
+      a.post_gamma = post->gamma;
+      a.post_beta = post->beta;
+      a.dpost_gamma = dpost->gamma;
+      a.dpost_beta = dpost->beta;
+      a.part_gate = ws;
+      a.part_post_gamma = ws + part;
+      a.part_post_beta = ws + 2 * part;
+    }
+    if (with_u) {
+      a.du = du;
+      a.has_u = 1;
+      a.pre_gamma = pre->gamma;
+      a.pre_beta = pre->beta;
+      a.dpre_gamma = dpre->gamma;
+      a.dpre_beta = dpre->beta;
+      a.part_pre_gamma = ws + 3 * part;
+      a.part_pre_beta = ws + 4 * part;
+    }
+    petra::couple_backward(a, desc->dtype, static_cast<hipStream_t>(stream));
+    return true;
+  });
+}
+
+petra_status petra_dropout(int64_t n, int32_t dtype, float p, float alpha, const void* x, const void* residual,
+                           const uint64_t* rng, void* y, void* stream) {
+  return entry("petra_dropout", [&]() -> bool {
+    need_dtype(dtype);
+    need(n >= 0 && n < (int64_t{1} << 46), PETRA_ERR_SHAPE, "negative or too large size");
+    need(std::isfinite(alpha), PETRA_ERR_INVALID_ARG, "alpha must be finite");
+    const uint32_t cut = need_dropout(p, rng, true);
+    need(rng != nullptr, PETRA_ERR_INVALID_ARG, "dropout without rng");
+    need_ptr(x, "x", n == 0);
+    need_ptr(y, "y", n == 0);
+    need_ptr(residual, "residual", n == 0 || residual == nullptr);
+    const size_t bytes = static_cast<size_t>(n) * size_of(dtype);
+    const Span sx{x, bytes, "x"}, sr{residual, bytes, "residual"}, sy{y, bytes, "y"};
+    need_apart(sy, sx, true);
+    need_apart(sy, sr, true);
+    if (n == 0) return false;
+    petra::dropout(x, residual, y, n, alpha * inv_keep(cut), cut, rng, dtype, static_cast<hipStream_t>(stream));
+    return true;
+  });
+}
+
+}  // extern "C"

@@ -1,0 +1,478 @@
+"""GPU parity of the token operators with oracle/tokens.py (fp64), at the sizes, masks and
+layouts where tiles, splits and lengths end.
+
+Bars, normwise per output.  fp32: products and sums of n terms in fp32, (n 2^-24 at
+most, far less in practice) 1e-5; parameter gradients, sums over all rows, the same.
+bf16 (2^-9 a rounding): o has one rounding of p and its own, 2^-8; gradients one of p or
+ds, their own, and those of o and of its like in D = do . o, which a row with few keys
+does not average out: 2^-7.  The coupling has its own rounding only, and u that of
+y, once more: 2^-8.  lse is an fp32 result of exact products: 1e-5."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import tokens as T
+
+pytestmark = pytest.mark.gpu
+
+FP32_BAR = 1e-5
+BAR = {("fp32", "o"): FP32_BAR, ("fp32", "grad"): FP32_BAR, ("bf16", "o"): 2.0 ** -8, ("bf16", "grad"): 2.0 ** -7}
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+RNG = (0x123456789ABCDEF, (7 << 40) + 3)
+
+
+def dev(a, dtype):
+    return torch.tensor(a).to("cuda", TYPES[dtype])
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def draw(seed, *shapes, dtype="fp32", std=1.0):
+    r = np.random.RandomState(seed)
+    return [host(torch.tensor(r.randn(*s) * std).to(TYPES[dtype])) for s in shapes]
+
+
+def near(got, want, bar, name, terms=0.0):
+    """terms: the size of the terms, for a result that cancels to nothing."""
+    got, want = host(got) if torch.is_tensor(got) else got, np.asarray(want)
+    assert got.shape == want.shape, name
+    assert np.isfinite(got).all(), name
+    err, size = np.linalg.norm(got - want), np.linalg.norm(want) or terms
+    assert err <= bar * size, (name, err / max(size, 1e-300))
+
+
+def like(x):
+    """NaN in a tensor with the strides of x."""
+    return torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device="cuda").fill_(math.nan)
+
+
+def rng_tensor():
+    return torch.tensor(RNG, dtype=torch.int64, device="cuda")
+
+
+# ---------------------------------------------------------------------------
+# attention
+# ---------------------------------------------------------------------------
+
+def attention(dtype, b, nq, nk, h, kvh, d, causal=False, lens=None, p=0.0, poison=False, layout=None, stream=None,
+              backward=True, seed=0):
+    from paper_2406_02052_amd import Attention
+
+    q, k, v, g = draw(seed, (b, nq, h, d), (b, nk, kvh, d), (b, nk, kvh, d), (b, nq, h, d), dtype=dtype)
+    lq, lk = lens or (None, None)
+    mask = T.factor_attention(RNG, p, b, h, nq, nk) if p else None
+    scale = 1.0 / math.sqrt(d)
+    want = T.attention(q, k, v, scale, causal, lq, lk, mask, g)
+    t = [dev(x, dtype) for x in (q, k, v, g)]
+    if poison:   # what lies past the lengths
+        for x, n in ((t[0], lq), (t[3], lq), (t[1], lk), (t[2], lk)):
+            for i in range(b):
+                x[i, max(0, n[i]):] = (math.nan, math.inf, -3.38e38)[i % 3]
+    if layout is not None:
+        t = [layout(x) for x in t]
+    tq, tk, tv, tg = t
+    op = Attention(b, nq, nk, h, kvh, d, dtype, causal=causal, scale=scale, dropout=p)
+    o = like(tg)
+    lse = torch.full((b, h, nq), math.nan, device="cuda")
+    more = dict(rng=rng_tensor() if p else None,
+                **{n: None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda")
+                   for n, x in (("q_lens", lq), ("kv_lens", lk))})
+    torch.cuda.synchronize()
+    op.forward(tq, tk, tv, o, lse, stream=stream, **more)
+    out = [o, lse]
+    if backward:
+        grads = [like(x) for x in (tq, tk, tv)]
+        op.backward(tq, tk, tv, o, lse, tg, *grads, stream=stream, **more)
+        out += grads
+    torch.cuda.synchronize()
+    return out, want
+
+
+def check(out, want, dtype):
+    near(out[0], want[0], BAR[dtype, "o"], "o")
+    lse, ref = host(out[1]), want[1]
+    assert np.array_equal(np.isneginf(lse), np.isneginf(ref))
+    fine = np.isfinite(ref)
+    assert np.abs(lse[fine] - ref[fine]).max(initial=0) <= 1e-5 * max(1.0, np.abs(ref[fine]).max(initial=0))
+    for name, x, y in zip(("dq", "dk", "dv"), out[2:], want[2:]):
+        # a query with one key has ds = p (dp - D) = 0: terms of about do . v scale q
+        near(x, y, BAR[dtype, "grad"], name, terms=math.sqrt(y.size))
+
+
+# (batch, q_len, kv_len, heads, kv_heads, head_dim, causal)
+SHAPES = [(1, 1, 1, 1, 1, 8, False), (2, 1, 1, 2, 1, 32, True), (2, 3, 5, 2, 2, 40, False), (1, 31, 33, 4, 2, 64, True),
+          (3, 64, 64, 2, 2, 32, False), (2, 65, 64, 3, 1, 96, True), (1, 129, 127, 2, 1, 128, True),
+          (1, 127, 200, 2, 2, 80, True), (1, 200, 77, 1, 1, 72, True), (2, 257, 300, 4, 2, 104, False),
+          (1, 515, 515, 2, 1, 128, True), (1, 5, 1000, 8, 1, 64, True), (1, 1, 2049, 8, 2, 128, True)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_attention_sizes(shape, dtype):
+    print("case", shape, dtype, flush=True)
+    check(*attention(dtype, *shape), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dim", range(8, 129, 8))
+def test_attention_head_widths(dim, dtype):
+    print("case", dim, dtype, flush=True)
+    check(*attention(dtype, 1, 45, 70, 2, 1, dim, True, seed=dim), dtype)
+
+
+LENS = [([1, 70, 33], [97, 0, 64]), ([70, 70, 69], [1, 96, 97]), ([0, 5, 70], [97, 97, 2]), ([64, 65, 1], [63, 64, 65])]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("lens", LENS, ids=str)
+def test_attention_lengths_and_empty_rows(lens, causal, dtype):
+    """Rows and whole sequences without a key; NaN, infinities and the type's lowest
+    values past the lengths reach nothing."""
+    print("case", lens, causal, dtype, flush=True)
+    check(*attention(dtype, 3, 70, 97, 4, 2, 64, causal, lens, poison=True), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_attention_lengths_with_splits(dtype):
+    print("case splits", dtype, flush=True)
+    check(*attention(dtype, 3, 2, 1500, 4, 2, 64, True, ([2, 1, 2], [1500, 0, 3]), poison=True), dtype)
+    check(*attention(dtype, 2, 40, 900, 6, 2, 40, True, ([40, 7], [900, 300]), poison=True), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape", [(2, 33, 70, 4, 2, 64, True), (1, 200, 200, 3, 1, 40, False), (2, 1, 600, 4, 1, 128, False)],
+                         ids=str)
+def test_attention_dropout(shape, dtype):
+    print("case", shape, dtype, flush=True)
+    check(*attention(dtype, *shape, p=0.3), dtype)
+    check(*attention(dtype, *shape, lens=([shape[1]] * shape[0], [shape[2] - 3] * shape[0]), p=0.1, poison=True), dtype)
+
+
+def _packed(x):
+    big = torch.full((*x.shape[:2], x.shape[2] * 3 + 1, x.shape[3]), math.nan, dtype=x.dtype, device="cuda")
+    big[:, :, 1:1 + x.shape[2]] = x
+    return big[:, :, 1:1 + x.shape[2]]
+
+
+def _heads_first(x):
+    return x.transpose(1, 2).contiguous().transpose(1, 2)
+
+
+def _tokens_first(x):
+    return x.transpose(0, 1).contiguous().transpose(0, 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("layout", [_packed, _heads_first, _tokens_first], ids=lambda f: f.__name__)
+def test_attention_strides(layout, dtype):
+    print("case", layout.__name__, dtype, flush=True)
+    check(*attention(dtype, 2, 70, 70, 4, 2, 64, True, layout=layout), dtype)
+    check(*attention(dtype, 2, 1, 700, 4, 2, 40, layout=layout), dtype)
+
+
+def test_attention_broadcast_keys_forward():
+    from paper_2406_02052_amd import Attention
+
+    q, k = draw(1, (3, 9, 2, 32), (1, 20, 2, 32), dtype="bf16")
+    kk = dev(k, "bf16").expand(3, -1, -1, -1)
+    o, lse = torch.empty(3, 9, 2, 32, dtype=torch.bfloat16, device="cuda"), torch.empty(3, 2, 9, device="cuda")
+    Attention(3, 9, 20, 2, 2, 32).forward(dev(q, "bf16"), kk, kk, o, lse)
+    kb = np.broadcast_to(k, (3, 20, 2, 32))
+    near(o, T.attention(q, kb, kb, 1 / math.sqrt(32))[0], BAR["bf16", "o"], "o")
+
+
+def test_attention_on_another_stream_and_repeated():
+    s = torch.cuda.Stream()
+    a, want = attention("bf16", 2, 130, 130, 4, 2, 64, True, p=0.1, stream=s)
+    check(a, want, "bf16")
+    b, _ = attention("bf16", 2, 130, 130, 4, 2, 64, True, p=0.1)
+    for x, y in zip(a, b):   # the same bits, whenever they run
+        assert torch.equal(x, y)
+
+
+def test_attention_large_scores():
+    """Scores far outside exp's range: the running maximum takes them."""
+    from paper_2406_02052_amd import Attention
+
+    for dtype in ("bf16", "fp32"):
+        q, k, v = draw(4, (1, 40, 2, 64), (1, 300, 2, 64), (1, 300, 2, 64), dtype=dtype, std=4.0)
+        want = T.attention(q, k, v, 3.0)
+        o, lse = torch.empty(1, 40, 2, 64, dtype=TYPES[dtype], device="cuda"), torch.empty(1, 2, 40, device="cuda")
+        Attention(1, 40, 300, 2, 2, 64, dtype, scale=3.0).forward(*(dev(x, dtype) for x in (q, k, v)), o, lse)
+        assert np.abs(want[1]).max() > 100
+        # probabilities change by their exponent's rounding: |s| 2^-24 of each term
+        near(o, want[0], BAR[dtype, "o"] + 2 * np.abs(want[1]).max() * 2.0 ** -23, "o")
+        near(lse, want[1], 1e-5, "lse")
+
+
+def test_attention_cache_past_32_bits():
+    """A cache of more than 2^31 bytes: one row's keys lie past 32-bit offsets."""
+    from paper_2406_02052_amd import Attention
+
+    n, h, d = 1_200_000, 8, 128
+    k = torch.zeros(1, n, h, d, dtype=torch.bfloat16, device="cuda")
+    assert k.numel() * 2 > 2 ** 31
+    q = torch.ones(1, 1, h, d, dtype=torch.bfloat16, device="cuda")
+    k[0, n - 1] = 4.0                        # its score is 4 sqrt(128) above the others'
+    v = k[:, :, :, :].clone()
+    o, lse = torch.empty_like(q), torch.empty(1, h, 1, device="cuda")
+    Attention(1, 1, n, h, h, d).forward(q, k, v, o, lse)
+    top = 4.0 * math.sqrt(d)
+    total = math.exp(top) + (n - 1)
+    near(o, np.full((1, 1, h, d), 4.0 * math.exp(top) / total), BAR["bf16", "o"], "o")
+    near(lse, np.full((1, h, 1), math.log(total)), 1e-5, "lse")
+
+
+def test_attention_gradients_match_differences():
+    """fp32, a direction's derivative of sum(o g) by differences of the kernel's own forward
+    (fp64 sums of fp32 results: 2^-24 |o g| / step, 1e-3 of the derivative at this step)."""
+    from paper_2406_02052_amd import Attention
+
+    b, n, h, kvh, d = 1, 40, 4, 2, 32
+    (o, lse, dq, dk, dv), _ = attention("fp32", b, n, n, h, kvh, d, True, p=0.2)
+    q, k, v, g = draw(0, (b, n, h, d), (b, n, kvh, d), (b, n, kvh, d), (b, n, h, d))
+    op = Attention(b, n, n, h, kvh, d, "fp32", causal=True, dropout=0.2)
+    for i, grad in enumerate((dq, dk, dv)):
+        # along the gradient, so that the derivative is its norm
+        e = host(grad) / np.linalg.norm(host(grad))
+        f = []
+        for sgn in (1, -1):
+            t = [q, k, v]
+            t[i] = t[i] + sgn * 0.05 * e
+            out, l2 = torch.empty(b, n, h, d, device="cuda"), torch.empty(b, h, n, device="cuda")
+            op.forward(*(dev(x, "fp32") for x in t), out, l2, rng=rng_tensor())
+            f.append((host(out) * g).sum())
+        want = np.linalg.norm(host(grad))
+        assert abs((f[0] - f[1]) / 0.1 - want) <= 5e-3 * want
+
+
+def test_attention_in_a_graph():
+    from paper_2406_02052_amd import Attention
+
+    b, n, h, d = 2, 100, 2, 64
+    op = Attention(b, n, n, h, h, d, causal=True, dropout=0.1)
+    q, k, v, g = (dev(x, "bf16") for x in draw(2, *[(b, n, h, d)] * 4, dtype="bf16"))
+    rng = rng_tensor()
+    o, lse = torch.empty_like(q), torch.empty(b, h, n, device="cuda")
+    grads = [torch.empty_like(q) for _ in range(3)]
+
+    def step():
+        op.forward(q, k, v, o, lse, rng=rng)
+        op.backward(q, k, v, o, lse, g, *grads, rng=rng)
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(3):
+        rng[1] = i          # another mask, read by the kernels
+        q.add_(0.25)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (o, lse, *grads)]
+        step()
+        torch.cuda.synchronize()
+        for x, y in zip(got, (o, lse, *grads)):
+            assert torch.equal(x, y)
+
+
+def test_attention_without_queries_or_keys():
+    from paper_2406_02052_amd import Attention
+
+    def z(*s):
+        return torch.full(s, math.nan, dtype=torch.bfloat16, device="cuda")
+
+    op = Attention(2, 0, 5, 2, 2, 32)
+    dk, dv = z(2, 5, 2, 32), z(2, 5, 2, 32)
+    q = z(2, 0, 2, 32)
+    lse = torch.empty(2, 2, 0, device="cuda")
+    op.forward(q, dk.clone(), dv.clone(), q.clone(), lse)
+    op.backward(q, z(2, 5, 2, 32), z(2, 5, 2, 32), q.clone(), lse, q.clone(), q.clone(), dk, dv)
+    assert (dk == 0).all() and (dv == 0).all()
+    op = Attention(2, 3, 0, 2, 2, 32)
+    o, lse, dq = z(2, 3, 2, 32), torch.empty(2, 2, 3, device="cuda"), z(2, 3, 2, 32)
+    e = z(2, 0, 2, 32)
+    op.forward(z(2, 3, 2, 32), e, e, o, lse)
+    op.backward(z(2, 3, 2, 32), e, e, o, lse, z(2, 3, 2, 32), dq, e.clone(), e.clone())
+    assert (o == 0).all() and torch.isneginf(lse).all() and (dq == 0).all()
+
+
+def test_attention_refuses_tensors_that_do_not_fit():
+    from paper_2406_02052_amd import Attention
+
+    op = Attention(1, 4, 4, 2, 2, 32)
+    q = torch.zeros(1, 4, 2, 32, dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros(1, 2, 4, device="cuda")
+    bad = [q.float(), q[:, :3], q.cpu(), q.transpose(2, 3).contiguous().transpose(2, 3),
+           torch.zeros(32, dtype=torch.bfloat16, device="cuda").expand(1, 4, 2, 32)]
+    for x in bad:
+        with pytest.raises(ValueError):
+            op.forward(x, q, q, q.clone(), lse)
+    with pytest.raises(ValueError):
+        op.forward(q, q, q, q.clone(), lse.double())
+    with pytest.raises(ValueError):
+        op.forward(q, q, q, q.clone(), lse, kv_lens=torch.zeros(1, device="cuda"))
+
+
+# ---------------------------------------------------------------------------
+# coupling
+# ---------------------------------------------------------------------------
+
+def coupling(dtype, rows, width, norm="rms", per_gate=0, scale=1.0, p=0.0, pre=True, beta=None, seed=0, in_place=False,
+             with_f=True):
+    from paper_2406_02052_amd import Coupling
+
+    beta = norm == "layer" if beta is None else beta
+    x, f, dy, du = draw(seed, *[(rows, width)] * 4, dtype=dtype)
+    f = host(torch.tensor(2 * f + 0.5).to(TYPES[dtype]))
+    gates = rows // per_gate if per_gate else 1
+    gate, g1, b1, g2, b2 = draw(seed + 1, (gates, width), *[(width,)] * 4)
+    post, pr = (1 + 0.1 * g1, b1 if beta else None), (1 + 0.1 * g2, b2 if beta else None)
+    post, pr = [tuple(None if t is None else host(torch.tensor(t).float()) for t in q) for q in (post, pr)]
+    mask = T.factor(RNG, p, (rows, width)) if p else None
+    op = Coupling(rows, width, dtype, norm=norm, residual_scale=scale, dropout=p, rows_per_gate=per_gate)
+    rng = rng_tensor() if p else None
+    tp, tpre = [tuple(None if t is None else dev(t, "fp32") for t in q) for q in (post, pr)]
+    tgate, tx, tf = dev(gate, "fp32"), dev(x, dtype), dev(f, dtype)
+    bar = BAR[dtype, "o"]
+    if with_f:
+        want = T.coupling(x, f, gate, post, norm, 1e-5, scale, mask)
+        y, u = tx if in_place else torch.full_like(tx, math.nan), torch.full_like(tx, math.nan)
+        op.forward(tx, tf, tgate, tp, y, pre=tpre if pre else None, u=u if pre else None, rng=rng)
+        torch.cuda.synchronize()
+        near(y, want, bar, "y")
+        if pre:
+            near(u, T.norm_forward(host(y), pr, norm, 1e-5), bar, "u")
+    else:
+        y, u = dev(x, dtype), torch.full_like(tx, math.nan)
+        op.forward(y, pre=tpre, u=u)
+        torch.cuda.synchronize()
+        near(u, T.norm_forward(x, pr, norm, 1e-5), bar, "u")
+    ref = T.coupling_backward(host(y), f if with_f else None, dy, gate, post, norm, 1e-5, scale, mask, du if pre else None, pr)
+    tdy, tdu = dev(dy, dtype), dev(du, dtype) if pre else None
+    new = lambda t: tuple(None if s is None else torch.full_like(s, math.nan) for s in t)  # noqa: E731
+    dpost, dpre, dgate = new(tp), new(tpre) if pre else None, torch.full_like(tgate, math.nan)
+    if in_place:
+        xo, dx, df = y, tdy, tf
+    else:
+        xo, dx, df = (torch.full_like(tx, math.nan) for _ in range(3))
+    if with_f:
+        op.backward(y, tf, tdy, tgate, tp, xo, dx, df, dgate, dpost, du=tdu, pre=tpre if pre else None, dpre=dpre, rng=rng)
+    else:
+        op.backward(y, None, tdy, None, None, None, dx, None, None, None, du=tdu, pre=tpre, dpre=dpre)
+    torch.cuda.synchronize()
+    near(dx, ref["dx"], bar, "dx")
+    if with_f:
+        near(xo, ref["x"], bar, "x")
+        near(df, ref["df"], bar, "df")
+        near(dgate, ref["dgate"], FP32_BAR, "dgate")
+        for i in range(2):
+            if dpost[i] is not None:
+                near(dpost[i], ref["dpost"][i], FP32_BAR, "dpost")
+    if pre:
+        for i in range(2):
+            if dpre[i] is not None:
+                near(dpre[i], ref["dpre"][i], FP32_BAR, "dpre")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("rows,width", [(1, 8), (3, 64), (33, 72), (9, 256), (5, 264), (7, 512), (70, 520), (4, 1024),
+                                        (3, 1032), (600, 48), (2, 2048), (5, 2056), (3, 4104), (2, 8192), (1500, 16)])
+def test_coupling_sizes(rows, width, norm, dtype):
+    print("case", rows, width, norm, dtype, flush=True)
+    coupling(dtype, rows, width, norm)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,width,per_gate", [(12, 64, 1), (12, 264, 3), (2050, 40, 1), (3000, 64, 1500), (700, 256, 7),
+                                                 (1026, 1000, 513), (6, 2056, 6), (1300, 2048, 13), (40, 4096, 1)])
+def test_coupling_gates(rows, width, per_gate, dtype):
+    print("case", rows, width, per_gate, dtype, flush=True)
+    coupling(dtype, rows, width, "layer", per_gate, 0.75)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("over", [dict(p=0.3), dict(p=0.1, per_gate=3, norm="layer"), dict(pre=False), dict(beta=True),
+                                  dict(norm="layer", beta=False), dict(in_place=True, p=0.2), dict(scale=-0.5),
+                                  dict(with_f=False), dict(with_f=False, norm="layer", scale=0.75)], ids=str)
+def test_coupling_forms(over, dtype):
+    for rows, width in ((33, 264), (6, 3000)):
+        print("case", over, rows, width, dtype, flush=True)
+        coupling(dtype, rows, width, **over)
+
+
+def test_coupling_without_rows():
+    from paper_2406_02052_amd import Coupling
+
+    op = Coupling(0, 64, norm="layer")
+    z = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
+    one = lambda: torch.full((64,), math.nan, device="cuda")  # noqa: E731
+    gate, dgate = torch.ones(1, 64, device="cuda"), torch.full((1, 64), math.nan, device="cuda")
+    p, dpost, dpre = (one(), one()), (one(), one()), (one(), one())
+    op.forward(z, z, gate, p, z, pre=p, u=z)
+    op.backward(z, z, z, gate, p, z, z, z, dgate, dpost, du=z, pre=p, dpre=dpre)
+    torch.cuda.synchronize()
+    assert all((t == 0).all() for t in (dgate, *dpost, *dpre))
+
+
+def test_coupling_keeps_what_was_dropped_out_of_it():
+    """Infinities and NaN of f in dropped places do not reach y through the mask (only through
+    their row's norm, so a mask of a whole row is checked by dropout alone below)."""
+    from paper_2406_02052_amd import dropout
+
+    m = T.factor(RNG, 0.5, (64,))
+    x = torch.tensor(np.where(m > 0, 1.0, np.nan), dtype=torch.float32, device="cuda")
+    y = torch.empty_like(x)
+    dropout(x, y, 0.5, rng_tensor())
+    assert np.array_equal(host(y), np.where(m > 0, 2.0, 0.0))
+
+
+# ---------------------------------------------------------------------------
+# dropout
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n", [1, 7, 8, 9, 2047, 2049, 100003])
+@pytest.mark.parametrize("p", [0.0, 0.1, 0.9])
+def test_dropout(n, p, dtype):
+    from paper_2406_02052_amd import dropout
+
+    print("case", n, p, dtype, flush=True)
+    x, r = draw(n, (n,), (n,), dtype=dtype)
+    tx, tr = dev(x, dtype), dev(r, dtype)
+    y = torch.full_like(tx, math.nan)
+    dropout(tx, y, p, rng_tensor())
+    want = T.dropout(x, p, RNG)
+    assert np.array_equal(host(y) == 0, want == 0)
+    near(y, want, BAR[dtype, "o"], "y")
+    dropout(tx, y, p, rng_tensor(), residual=tr, alpha=0.5)
+    near(y, T.dropout(x, p, RNG, r, 0.5), BAR[dtype, "o"], "y with residual")
+    dropout(tx, tr, p, rng_tensor(), residual=tr)       # in place, and its inverse
+    dropout(tx, tr, p, rng_tensor(), residual=tr, alpha=-1.0)
+    torch.cuda.synchronize()
+    big = np.abs(T.dropout(x, p, RNG)) + np.abs(r)
+    assert (np.abs(host(tr) - r) <= 2 * big * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -22)).all()
+
+
+def test_dropout_offsets_and_seeds_differ():
+    from paper_2406_02052_amd import dropout
+
+    x = torch.ones(4096, device="cuda")
+    masks = []
+    for rng in ((1, 1), (1, 2), (2, 1), (1, 1 << 40), (1 << 40, 1)):
+        y = torch.empty_like(x)
+        dropout(x, y, 0.5, torch.tensor(rng, dtype=torch.int64, device="cuda"))
+        assert np.array_equal(host(y) > 0, T.factor(rng, 0.5, (4096,)) > 0)
+        masks.append(host(y) > 0)
+    for i in range(len(masks)):
+        for j in range(i):
+            assert 0.4 < (masks[i] == masks[j]).mean() < 0.6
