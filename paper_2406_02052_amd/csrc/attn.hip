@@ -65,20 +65,27 @@ __device__ __forceinline__ void operand(const f32x16_t& c, int half, Frag<float>
   for (int i = 0; i < 8; ++i) f.v[i] = c[8 * half + i];
 }
 
-// A tile of rows of DP elements in LDS, in chunks of 16 bytes.  Chunks are moved
-// within a row by an exclusive or with a key of the row: eight consecutive rows at
-// one chunk (a straight read) and four consecutive rows at two chunks (a transposing
-// read) then lie in different banks.
+// A tile of rows of DP elements in LDS, in chunks of 16 bytes.  LDS serves 256 bytes a
+// cycle if they lie in different banks: 16 lanes of a straight read (16 rows at one
+// chunk), 32 of a transposing one (4 rows at 4 chunks).  Chunks are therefore moved
+// within a row by an exclusive or with a key of the row.
 template <typename T, int DP>
 struct Tile {
   static constexpr int CHUNKS = DP * static_cast<int>(sizeof(T)) / 16;
   static constexpr int ROW_BYTES = CHUNKS * 16;
   static constexpr int STEPS = DP / 16;
+  static __device__ __forceinline__ int key(int row) {
+    if constexpr (CHUNKS % 16 == 0 && sizeof(T) == 2)
+      return ((row & 3) << 2) | ((row >> 2) & 3);
+    else if constexpr (CHUNKS % 16 == 0)   // fp32 reads across rows take a row and its fourth next
+      return (((row >> 2) & 1) << 3) | ((row & 3) << 1) | ((row >> 3) & 1);
+    else if constexpr (CHUNKS % 8 == 0)    // two rows to 256 bytes
+      return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+    else                                   // four, or four thirds
+      return (row >> 2) & 3;
+  }
   static __device__ __forceinline__ int at(int row, int chunk) {
-    if constexpr (CHUNKS % 8 == 0)
-      return row * ROW_BYTES + ((chunk ^ (((row & 3) << 1) | ((row >> 2) & 1))) << 4);
-    else
-      return row * ROW_BYTES + ((chunk ^ ((row & 2) | ((row >> 2) & 1))) << 4);
+    return row * ROW_BYTES + ((chunk ^ key(row)) << 4);
   }
   // Operand whose free index is the row (this lane's `row`) and inner index the
   // channels 16 step .. 16 step + 15.
@@ -118,47 +125,95 @@ struct Tile {
   }
 };
 
-// A tile of ROWS rows on its way from memory to LDS, THREADS threads.
+// Brings tiles of ROWS rows from memory to LDS without passing through registers:
+// each wave's load puts 64 chunks of 16 bytes in a row into LDS, so the lanes ask for
+// the chunks in the order that Tile gives them.  Offsets from the tile's first row
+// are the same for every whole tile; lanes without an element ask past the end of
+// the resource, which brings zeros.
 template <typename T, int DP, int ROWS, int THREADS>
-struct Mover {
+struct Stager {
   using Tl = Tile<T, DP>;
-  static constexpr int N = (ROWS * Tl::CHUNKS + THREADS - 1) / THREADS;
+  static constexpr int N = ROWS * Tl::CHUNKS / THREADS;
   static_assert(ROWS * Tl::CHUNKS % THREADS == 0, "whole chunks a thread");
-  u32x4_t v[N];
+  uint32_t off[N];
 
-  // Keys first .. first + ROWS - 1 of one head (base: its key 0); keys at or past `end` and channels
-  // past dim as zeros.  The resource starts at the tile, so offsets stay small however long the cache.
-  __device__ __forceinline__ void keys(const T* base, int64_t stride, int first, int end, int dim) {
+  static __device__ __forceinline__ int place(int i) { return i * THREADS + static_cast<int>(threadIdx.x); }
+  static __device__ __forceinline__ int row(int i) { return place(i) / Tl::CHUNKS; }
+  static __device__ __forceinline__ int chunk_offset(int i, int dim) {
+    const int p = place(i), r = p / Tl::CHUNKS, c = (Tl::at(r, p % Tl::CHUNKS) >> 4) - r * Tl::CHUNKS;
+    return c * 16 < dim * static_cast<int>(sizeof(T)) ? c * 16 : -1;
+  }
+  // Rows one stride apart.
+  __device__ __forceinline__ void keys(int64_t stride, int dim) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = chunk_offset(i, dim);
+      off[i] = c < 0 ? BUF_OOB : static_cast<uint32_t>(row(i) * stride * sizeof(T)) + c;
+    }
+  }
+  // Rows of a key head's queries from row `first`, of `left` rows: token row / group, head row % group.
+  __device__ __forceinline__ void queries(int64_t st, int64_t sh, int first, int left, int group, int dim) {
+    const int token0 = first / group;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = chunk_offset(i, dim), r = first + row(i), token = r / group;
+      const int64_t o = ((token - token0) * st + (r - token * group) * sh) * static_cast<int64_t>(sizeof(T));
+      off[i] = c < 0 || row(i) >= left ? BUF_OOB : static_cast<uint32_t>(o) + c;
+    }
+  }
+  // The loads are written out: the compiler would let every later transposing LDS read wait for them,
+  // those of the other buffer too.  They write no register, and arrived() waits for them.
+  __device__ __forceinline__ void load(const T* first, uint32_t bytes, char* lds) const {
+    const uint64_t base = reinterpret_cast<uint64_t>(first);
+    const u32x4_t r = {static_cast<uint32_t>(base), static_cast<uint32_t>(base >> 32) & 0xffffu, bytes, 0x00020000u};
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t to = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds)) + wave * 1024;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   ::"s"(to + i * THREADS * 16), "v"(off[i]), "s"(r) : "memory");
+  }
+  // Keys first .. of a head whose key 0 is at base; those at or past `end` as zeros.
+  __device__ __forceinline__ void load_keys(const T* base, int64_t stride, int first, int end, int dim, char* lds) const {
     const int left = end - first < ROWS ? end - first : ROWS;
-    const __amdgpu_buffer_rsrc_t r =
-        make_rsrc(base + static_cast<int64_t>(first) * stride, left > 0 ? (left - 1) * stride * sizeof(T) + dim * sizeof(T) : 0);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int c = threadIdx.x + i * THREADS, row = c / Tl::CHUNKS, chunk = c % Tl::CHUNKS;
-      const bool in = row < left && chunk * 16 < dim * static_cast<int>(sizeof(T));
-      v[i] = buf_load16(r, in ? static_cast<uint32_t>(row * stride * sizeof(T)) + chunk * 16 : BUF_OOB);
-    }
-  }
-  // Rows first .. of a key head's queries: token row / group, head row % group.
-  __device__ __forceinline__ void queries(const T* base, int64_t st, int64_t sh, int first, int end, int group, int dim) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int c = threadIdx.x + i * THREADS, row = first + c / Tl::CHUNKS, chunk = c % Tl::CHUNKS;
-      v[i] = u32x4_t{0u, 0u, 0u, 0u};
-      if (row < end && chunk * 16 < dim * static_cast<int>(sizeof(T))) {
-        const int token = row / group, head = row - token * group;
-        v[i] = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const char*>(base + token * st + head * sh) + chunk * 16);
-      }
-    }
-  }
-  __device__ __forceinline__ void put(char* lds) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int c = threadIdx.x + i * THREADS;
-      *reinterpret_cast<u32x4_t*>(lds + Tl::at(c / Tl::CHUNKS, c % Tl::CHUNKS)) = v[i];
-    }
+    load(base + first * stride, static_cast<uint32_t>(((left - 1) * stride + dim) * sizeof(T)), lds);
   }
 };
+
+// Every load of the workgroup has arrived in LDS, and every wave has left the buffer that is next.
+// The builtin tells the compiler that its own loads from before a loop have arrived too, which
+// it would otherwise wait for inside the loop, with the tile that was just asked for.
+__device__ __forceinline__ void arrived() {
+  __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+// 64 consecutive floats (or zeros past `bytes`) into LDS, by the wave that calls.
+__device__ __forceinline__ void stage_floats(const float* from, int bytes, float* lds) {
+  const uint64_t base = reinterpret_cast<uint64_t>(from);
+  const u32x4_t r = {static_cast<uint32_t>(base), static_cast<uint32_t>(base >> 32) & 0xffffu, static_cast<uint32_t>(bytes), 0x00020000u};
+  const uint32_t to = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) float*)lds));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               ::"s"(to), "v"((threadIdx.x & 63) * 4), "s"(r) : "memory");
+}
+
+// What this workgroup works on: (batch row, key head), split, tile.  Heads run fastest:
+// workgroups go to the 8 XCDs in turn, so that with a multiple of 8 heads each XCD's L2
+// has the keys of its own; tiles run slowest, from the one with most visible pairs where
+// the mask is causal, so that what is left for the end is short.
+struct Item {
+  int bh, split, tile;
+};
+__device__ __forceinline__ Item work_item(const AttnArgs& a, bool last_first) {
+  const int heads = a.batch * a.kv_heads, rest = blockIdx.x / heads;
+  Item i;
+  i.bh = blockIdx.x - rest * heads;
+  i.tile = rest / a.splits;
+  i.split = rest - i.tile * a.splits;
+  if (last_first) i.tile = a.tiles - 1 - i.tile;
+  return i;
+}
 
 // This lane's row of an operand, straight from memory: channels 16 step + 8 h .. + 7 of each step.
 template <typename T, int DP>
@@ -237,184 +292,223 @@ __device__ __forceinline__ void store_row(T* p, const f32x16_t (&acc)[DP / 32], 
 // forward
 // ---------------------------------------------------------------------------
 
-// WR waves side by side over rows (32 each), WK over keys (KB blocks of 32 each in a tile).
-template <typename T, int DP, int WR, int WK, int KB, bool DROP>
-__global__ __launch_bounds__(64 * WR * WK) void attn_forward_kernel(AttnArgs a) {
+// WR waves side by side over rows (32 NT each), WK over keys (KB blocks of 32 each in a tile).
+template <typename T, int DP, int WR, int WK, int NT, int KB, bool DROP>
+__global__ __launch_bounds__(64 * WR * WK, (NT * DP * sizeof(T) > 256 ? 1 : 2)) void attn_forward_kernel(AttnArgs a) {
   using Tl = Tile<T, DP>;
-  constexpr int THREADS = 64 * WR * WK, ROWS = 32 * WR, KT = 32 * KB * WK;
+  constexpr int THREADS = 64 * WR * WK, ROWS = 32 * NT * WR, KT = 32 * KB * WK;
   constexpr int TILE_BYTES = KT * Tl::ROW_BYTES;
-  constexpr int JOIN_BYTES = WK > 1 ? WK * WR * 32 * (DP + 2) * 4 : 0;
-  __shared__ __attribute__((aligned(16))) char lds[2 * TILE_BYTES > JOIN_BYTES ? 2 * TILE_BYTES : JOIN_BYTES];
-  char* const kt = lds;
-  char* const vt = lds + TILE_BYTES;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+  constexpr int JOIN_BYTES = WK > 1 ? WK * ROWS * (DP + 2) * 4 : 0;
+  __shared__ __attribute__((aligned(16))) char lds[4 * TILE_BYTES > JOIN_BYTES ? 4 * TILE_BYTES : JOIN_BYTES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int wr = wave % WR, wk = wave / WR;
-  const Where w = where(a, blockIdx.y);
+  const Item item = work_item(a, true);
+  const int bh = item.bh, split = item.split, tile = item.tile;
+  const Where w = where(a, bh);
   const int rows = a.q_len * a.group;
-  const int row0 = blockIdx.x * ROWS;
-  const int row = row0 + wr * 32 + (lane & 31);
-  const int token = row / a.group, head = w.kvh * a.group + row % a.group;
-  const bool in_q = row < rows;
-  const int limit = in_q ? seen(a, w, token) : 0;
+  const int row0 = tile * ROWS, wave0 = row0 + wr * 32 * NT;
+  int token[NT], head[NT], limit[NT];
+  Frag<T> q[NT][Tl::STEPS];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int row = wave0 + 32 * n + (lane & 31);
+    token[n] = row / a.group;
+    head[n] = w.kvh * a.group + row - token[n] * a.group;
+    const bool in_q = row < rows;
+    limit[n] = in_q ? seen(a, w, token[n]) : 0;
+    load_row<T, DP>(at<T>(a.q, a.q_stride, w.b, in_q ? token[n] : 0, head[n]), in_q && token[n] < w.q_len, h, a.dim, q[n]);
+  }
 
-  Frag<T> q[Tl::STEPS];
-  load_row<T, DP>(at<T>(a.q, a.q_stride, w.b, in_q ? token : 0, head), in_q && token < w.q_len, h, a.dim, q);
-
-  // keys that any row of the workgroup and of the wave sees, and that every row of the wave sees
+  // keys that any row of the workgroup sees, and that every row of the wave sees
   const int last_row = (row0 + ROWS < rows ? row0 + ROWS : rows) - 1;
   int last_token = last_row / a.group;
   if (last_token > w.q_len - 1) last_token = w.q_len - 1;
   const int end = row0 / a.group < w.q_len ? seen(a, w, last_token) : 0;
   int all = w.kv_len;
   if (a.causal) {
-    all = (row0 + wr * 32) / a.group + w.kv_len - w.q_len + 1;
+    all = wave0 / a.group + w.kv_len - w.q_len + 1;
     all = all < w.kv_len ? all : w.kv_len;
   }
   const int tiles = (end + KT - 1) / KT;
   const int per = (tiles + a.splits - 1) / a.splits;
-  const int t0 = blockIdx.z * per, t1 = t0 + per < tiles ? t0 + per : tiles;
+  const int t0 = split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
-  f32x16_t acc[DP / 32];
+  f32x16_t acc[NT][DP / 32];
+  float top[NT], sum[NT];
 #pragma unroll
-  for (int m = 0; m < DP / 32; ++m) zero(acc[m]);
-  float top = -INFINITY, sum = 0.f;
+  for (int n = 0; n < NT; ++n) {
+    top[n] = -INFINITY;
+    sum[n] = 0.f;
+#pragma unroll
+    for (int m = 0; m < DP / 32; ++m) zero(acc[n][m]);
+  }
   const float c = a.scale_log2;
   Rng rng{};
   if (DROP) rng = load_rng(a.rng);
-  const int64_t drop_row = (static_cast<int64_t>(w.b) * a.heads + head) * a.q_len + token;
 
   const T* const kb = at<T>(a.k, a.k_stride, w.b, 0, w.kvh);
   const T* const vb = at<T>(a.v, a.v_stride, w.b, 0, w.kvh);
-  Mover<T, DP, KT, THREADS> mk, mv;
-  if (t0 < t1) {
-    mk.keys(kb, a.k_stride[1], t0 * KT, end, a.dim);
-    mv.keys(vb, a.v_stride[1], t0 * KT, end, a.dim);
-  }
+  Stager<T, DP, KT, THREADS> sk, sv;
+  sk.keys(a.k_stride[1], a.dim);
+  sv.keys(a.v_stride[1], a.dim);
+  auto stage = [&](int t) {
+    char* const to = lds + (t & 1) * 2 * TILE_BYTES;
+    sk.load_keys(kb, a.k_stride[1], t * KT, end, a.dim, to);
+    sv.load_keys(vb, a.v_stride[1], t * KT, end, a.dim, to + TILE_BYTES);
+  };
+  if (t0 < t1) stage(t0);
   for (int t = t0; t < t1; ++t) {
-    __syncthreads();
-    mk.put(kt);
-    mv.put(vt);
-    __syncthreads();
-    if (t + 1 < t1) {
-      mk.keys(kb, a.k_stride[1], (t + 1) * KT, end, a.dim);
-      mv.keys(vb, a.v_stride[1], (t + 1) * KT, end, a.dim);
-    }
+    arrived();
+    if (t + 1 < t1) stage(t + 1);
+    char* const kt = lds + (t & 1) * 2 * TILE_BYTES;
+    char* const vt = kt + TILE_BYTES;
     const int at0 = wk * 32 * KB;          // this wave's keys in the tile
     const int key0 = t * KT + at0;
-    f32x16_t s[KB];
+    f32x16_t s[NT][KB];
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
-      zero(s[b]);
 #pragma unroll
-      for (int i = 0; i < Tl::STEPS; ++i)
-        s[b] = mfma32(Tl::straight(kt, at0 + 32 * b + (lane & 31), i, h), q[i], s[b]);
+      for (int n = 0; n < NT; ++n) zero(s[n][b]);
+#pragma unroll
+      for (int i = 0; i < Tl::STEPS; ++i) {
+        const Frag<T> k = Tl::straight(kt, at0 + 32 * b + (lane & 31), i, h);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s[n][b] = mfma32(k, q[n][i], s[n][b]);
+      }
     }
     if (key0 + 32 * KB > all) {
 #pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = key0 + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3);
+            s[n][b][i] = key < limit[n] ? s[n][b][i] : -INFINITY;
+          }
+    }
+    // the running maximum moves only when some row's grew by more than 2^8: exp stays far inside fp32
+    float m[NT];
+    bool grew = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      m[n] = s[n][0][0];
+#pragma unroll
       for (int b = 0; b < KB; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = key0 + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3);
-          s[b][i] = key < limit ? s[b][i] : -INFINITY;
-        }
+        for (int i = 0; i < 16; ++i) m[n] = fmaxf(m[n], s[n][b][i]);
+      m[n] = fmaxf(m[n], other_half(m[n]));
+      grew |= fmaf(m[n], c, -8.f) > top[n] * c;
     }
-    float m = s[0][0];
+    if (__any(grew)) {
 #pragma unroll
-    for (int b = 0; b < KB; ++b)
+      for (int n = 0; n < NT; ++n) {
+        const float to = fmaxf(top[n], m[n]);
+        const float f = to == -INFINITY ? 1.f : exp2_((top[n] - to) * c);
+        top[n] = to;
+        sum[n] *= f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) m = fmaxf(m, s[b][i]);
-    m = fmaxf(m, other_half(m));
-    // the running maximum moves only when some row's grew by more than 2^8: exp stays far inside fp32
-    if (__any(fmaf(m, c, -8.f) > top * c)) {
-      const float n = fmaxf(top, m);
-      const float f = n == -INFINITY ? 1.f : exp2_((top - n) * c);
-      top = n;
-      sum *= f;
+        for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-      for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[d][i] *= f;
+          for (int i = 0; i < 16; ++i) acc[n][d][i] *= f;
+      }
     }
-    const float base = top == -INFINITY ? 0.f : top * c;
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[b][i] = exp2_(fmaf(s[b][i], c, -base));
-        sum += s[b][i];
+      for (int n = 0; n < NT; ++n) {
+        const float base = top[n] == -INFINITY ? 0.f : top[n] * c;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[n][b][i] = exp2_(fmaf(s[n][b][i], c, -base));
+          sum[n] += s[n][b][i];
+        }
       }
 #pragma unroll
       for (int k16 = 0; k16 < 2; ++k16) {
-        if (DROP) {
-          uint32_t bits[4];
-          drop_bits(a, rng, drop_row, ((key0 + 32 * b) >> 4) + k16, h, bits);
+        Frag<T> p[NT];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) s[b][8 * k16 + i] = kept(bits, i, a.cut) ? s[b][8 * k16 + i] : 0.f;
+        for (int n = 0; n < NT; ++n) {
+          if (DROP) {
+            uint32_t bits[4];
+            drop_bits(a, rng, (static_cast<int64_t>(w.b) * a.heads + head[n]) * a.q_len + token[n],
+                      ((key0 + 32 * b) >> 4) + k16, h, bits);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[n][b][8 * k16 + i] = kept(bits, i, a.cut) ? s[n][b][8 * k16 + i] : 0.f;
+          }
+          operand(s[n][b], k16, p[n]);
         }
-        Frag<T> p;
-        operand(s[b], k16, p);
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
-          acc[d] = mfma32(Tl::across(vt, at0 + 32 * b + 16 * k16, 32 * d, lane), p, acc[d]);
+        for (int d = 0; d < DP / 32; ++d) {
+          const Frag<T> v = Tl::across(vt, at0 + 32 * b + 16 * k16, 32 * d, lane);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) acc[n][d] = mfma32(v, p[n], acc[n][d]);
+        }
       }
     }
   }
-  sum += other_half(sum);
+#pragma unroll
+  for (int n = 0; n < NT; ++n) sum[n] += other_half(sum[n]);
 
   if constexpr (WK > 1) {
     // join the waves that shared the rows: statistics, then the scaled accumulators, in a fixed order
-    float* const stat = reinterpret_cast<float*>(lds);              // [WK][WR][32][2]
-    float* const part = stat + WK * WR * 32 * 2;                     // [WK][WR][32][DP]
+    static_assert(WK == 1 || NT == 1, "one block of rows a wave");
+    float* const stat = reinterpret_cast<float*>(lds);              // [WK][ROWS][2]
+    float* const part = stat + WK * ROWS * 2;                       // [WK][ROWS][DP]
     const int at_row = wr * 32 + (lane & 31);
     __syncthreads();
     if (h == 0) {
-      stat[(wk * ROWS + at_row) * 2] = top;
-      stat[(wk * ROWS + at_row) * 2 + 1] = sum;
+      stat[(wk * ROWS + at_row) * 2] = top[0];
+      stat[(wk * ROWS + at_row) * 2 + 1] = sum[0];
     }
     __syncthreads();
-    float n = -INFINITY;
+    float to = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < WK; ++i) n = fmaxf(n, stat[(i * ROWS + at_row) * 2]);
-    const float f = n == -INFINITY ? 0.f : exp2_((top - n) * c);
-    sum = 0.f;
+    for (int i = 0; i < WK; ++i) to = fmaxf(to, stat[(i * ROWS + at_row) * 2]);
+    const float f = to == -INFINITY ? 0.f : exp2_((top[0] - to) * c);
+    sum[0] = 0.f;
 #pragma unroll
     for (int i = 0; i < WK; ++i) {
       const float ti = stat[(i * ROWS + at_row) * 2];
-      sum += ti == -INFINITY ? 0.f : stat[(i * ROWS + at_row) * 2 + 1] * exp2_((ti - n) * c);
+      sum[0] += ti == -INFINITY ? 0.f : stat[(i * ROWS + at_row) * 2 + 1] * exp2_((ti - to) * c);
     }
-    top = n;
-    if (wk > 0) store_row<float, DP>(part + (wk * ROWS + at_row) * DP, acc, f, h, DP);
+    top[0] = to;
+    if (wk > 0) store_row<float, DP>(part + (wk * ROWS + at_row) * DP, acc[0], f, h, DP);
     __syncthreads();
     if (wk > 0) return;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        float4 v = make_float4(acc[d][4 * g] * f, acc[d][4 * g + 1] * f, acc[d][4 * g + 2] * f, acc[d][4 * g + 3] * f);
+        float4 v = make_float4(acc[0][d][4 * g] * f, acc[0][d][4 * g + 1] * f, acc[0][d][4 * g + 2] * f, acc[0][d][4 * g + 3] * f);
 #pragma unroll
         for (int i = 1; i < WK; ++i) {
           const float4 u = *reinterpret_cast<const float4*>(part + (i * ROWS + at_row) * DP + 32 * d + 8 * g + 4 * h);
           v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
         }
-        acc[d][4 * g] = v.x; acc[d][4 * g + 1] = v.y; acc[d][4 * g + 2] = v.z; acc[d][4 * g + 3] = v.w;
+        acc[0][d][4 * g] = v.x; acc[0][d][4 * g + 1] = v.y; acc[0][d][4 * g + 2] = v.z; acc[0][d][4 * g + 3] = v.w;
       }
   }
-  if (!in_q) return;
-  if (a.splits > 1) {
-    // [split][batch x key heads][rows][DP], and the statistics as [..][rows][2]
-    const int64_t at_part = (static_cast<int64_t>(blockIdx.z) * gridDim.y + blockIdx.y) * rows + row;
-    store_row<float, DP>(a.part + at_part * DP, acc, 1.f, h, DP);
-    if (h == 0) {   // a row without keys: as if it had met none
-      a.part_ml[at_part * 2] = limit > 0 ? top : -INFINITY;
-      a.part_ml[at_part * 2 + 1] = limit > 0 ? sum : 0.f;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int row = wave0 + 32 * n + (lane & 31);
+    if (row >= rows) continue;
+    if (a.splits > 1) {
+      // [split][batch x key heads][rows][DP], and the statistics as [..][rows][2]
+      const int64_t at_part = (static_cast<int64_t>(split) * a.batch * a.kv_heads + bh) * rows + row;
+      store_row<float, DP>(a.part + at_part * DP, acc[n], 1.f, h, DP);
+      if (h == 0) {   // a row without keys: as if it had met none
+        a.part_ml[at_part * 2] = limit[n] > 0 ? top[n] : -INFINITY;
+        a.part_ml[at_part * 2 + 1] = limit[n] > 0 ? sum[n] : 0.f;
+      }
+      continue;
     }
-    return;
+    const bool any = limit[n] > 0 && (sum[n] > 0.f || sum[n] != sum[n]);
+    store_row<T, DP>(at<T>(a.out, a.o_stride, w.b, token[n], head[n]), acc[n], any ? a.inv_keep / sum[n] : 0.f, h, a.dim);
+    if (h == 0)
+      a.lse[(static_cast<int64_t>(w.b) * a.heads + head[n]) * a.q_len + token[n]] =
+          any ? fmaf(top[n], a.scale, __builtin_amdgcn_logf(sum[n]) * LN2) : -INFINITY;
   }
-  const bool any = sum > 0.f || sum != sum;
-  store_row<T, DP>(at<T>(a.out, a.o_stride, w.b, token, head), acc, limit > 0 && any ? a.inv_keep / sum : 0.f, h, a.dim);
-  if (h == 0)
-    a.lse[(w.head0 + row % a.group) * a.q_len + token] =
-        limit > 0 && any ? fmaf(top, a.scale, __builtin_amdgcn_logf(sum) * LN2) : -INFINITY;
 }
 
 // Joins the splits of one row: a wave a row, DP / 64 channels a lane.
@@ -456,22 +550,52 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // ---------------------------------------------------------------------------
 
 template <typename T, int DP, int WR, int KB, bool DROP>
-__global__ __launch_bounds__(64 * WR) void attn_dq_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * WR, (DP * sizeof(T) > 256 ? 1 : 2)) void attn_dq_kernel(AttnArgs a) {
   using Tl = Tile<T, DP>;
   constexpr int THREADS = 64 * WR, ROWS = 32 * WR, KT = 32 * KB;
   constexpr int TILE_BYTES = KT * Tl::ROW_BYTES;
-  __shared__ __attribute__((aligned(16))) char lds[2 * TILE_BYTES];
-  char* const kt = lds;
-  char* const vt = lds + TILE_BYTES;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-  const Where w = where(a, blockIdx.y);
+  __shared__ __attribute__((aligned(16))) char lds[4 * TILE_BYTES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const Item item = work_item(a, true);
+  const int bh = item.bh, split = item.split, tile = item.tile;
+  const Where w = where(a, bh);
   const int rows = a.q_len * a.group;
-  const int row0 = blockIdx.x * ROWS;
-  const int row = row0 + wave * 32 + (lane & 31);
-  const int token = row / a.group, head = w.kvh * a.group + row % a.group;
+  const int row0 = tile * ROWS, wave0 = row0 + wave * 32;
+  const int row = wave0 + (lane & 31);
+  const int token = row / a.group, head = w.kvh * a.group + row - token * a.group;
   const bool in_q = row < rows, live = in_q && token < w.q_len;
   const int limit = in_q ? seen(a, w, token) : 0;
   const int from = in_q ? token : 0;
+
+  const int last_row = (row0 + ROWS < rows ? row0 + ROWS : rows) - 1;
+  int last_token = last_row / a.group;
+  if (last_token > w.q_len - 1) last_token = w.q_len - 1;
+  const int end = row0 / a.group < w.q_len ? seen(a, w, last_token) : 0;
+  int all = w.kv_len;
+  if (a.causal) {
+    all = wave0 / a.group + w.kv_len - w.q_len + 1;
+    all = all < w.kv_len ? all : w.kv_len;
+  }
+  const int tiles = (end + KT - 1) / KT;
+  const int per = (tiles + a.splits - 1) / a.splits;
+  const int t0 = split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
+
+  const T* const kb = at<T>(a.k, a.k_stride, w.b, 0, w.kvh);
+  const T* const vb = at<T>(a.v, a.v_stride, w.b, 0, w.kvh);
+  Stager<T, DP, KT, THREADS> sk, sv;
+  sk.keys(a.k_stride[1], a.dim);
+  sv.keys(a.v_stride[1], a.dim);
+  auto stage = [&](int t, int buffer) {
+    char* const to = lds + buffer * 2 * TILE_BYTES;
+    sk.load_keys(kb, a.k_stride[1], t * KT, end, a.dim, to);
+    sv.load_keys(vb, a.v_stride[1], t * KT, end, a.dim, to + TILE_BYTES);
+  };
+  // A row that sees at most the first tile takes D from that tile's own products: with few keys
+  // p is large and o's rounding, which do . o would bring in, does not average out over them.
+  const bool few = sizeof(T) == 2 && all < KT && tiles > 0;
+  const bool few_any = sizeof(T) == 2 && tiles > 0 && (w.kv_len <= KT || (a.causal && row0 / a.group + w.kv_len - w.q_len < KT));
+  if (few_any) stage(0, 1);
+  if (t0 < t1) stage(t0, 0);
 
   Frag<T> q[Tl::STEPS], g[Tl::STEPS];
   load_row<T, DP>(at<T>(a.q, a.q_stride, w.b, from, head), live, h, a.dim, q);
@@ -492,77 +616,77 @@ __global__ __launch_bounds__(64 * WR) void attn_dq_kernel(AttnArgs a) {
       }
     delta += other_half(delta);
   }
-  const int64_t stat = (w.head0 + row % a.group) * a.q_len + token;
+  const int64_t stat = (static_cast<int64_t>(w.b) * a.heads + head) * a.q_len + token;
   // a row without keys: lse +inf makes every p zero
   const float lse = limit > 0 ? a.lse[stat] * LOG2E : INFINITY;
-  if (in_q && h == 0) a.delta[stat] = delta;
+  const float c = a.scale_log2;
+  Rng rng{};
+  if (DROP) rng = load_rng(a.rng);
+  const int64_t drop_row = stat;
 
-  const int last_row = (row0 + ROWS < rows ? row0 + ROWS : rows) - 1;
-  int last_token = last_row / a.group;
-  if (last_token > w.q_len - 1) last_token = w.q_len - 1;
-  const int end = row0 / a.group < w.q_len ? seen(a, w, last_token) : 0;
-  int all = w.kv_len;
-  if (a.causal) {
-    all = (row0 + wave * 32) / a.group + w.kv_len - w.q_len + 1;
-    all = all < w.kv_len ? all : w.kv_len;
+  // s = p and dp (with dropout's factor) of a block of keys
+  auto products = [&](char* kt, int b, int key0, f32x16_t& s, f32x16_t& dp) {
+    zero(s);
+    zero(dp);
+#pragma unroll
+    for (int i = 0; i < Tl::STEPS; ++i) {
+      s = mfma32(Tl::straight(kt, 32 * b + (lane & 31), i, h), q[i], s);
+      dp = mfma32(Tl::straight(kt + TILE_BYTES, 32 * b + (lane & 31), i, h), g[i], dp);
+    }
+#pragma unroll
+    for (int k16 = 0; k16 < 2; ++k16) {
+      uint32_t bits[4];
+      if (DROP) drop_bits(a, rng, drop_row, (key0 >> 4) + k16, h, bits);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int i = 8 * k16 + j;
+        s[i] = exp2_(fmaf(s[i], c, -lse));
+        if (DROP) dp[i] = kept(bits, j, a.cut) ? dp[i] * a.inv_keep : 0.f;
+      }
+    }
+    if (key0 + 32 > all) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = key0 + 8 * (i >> 2) + 4 * h + (i & 3);
+        s[i] = key < limit ? s[i] : 0.f;
+      }
+    }
+  };
+
+  if (few_any) {
+    arrived();
+    if (few) {
+      float own = 0.f;
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+        f32x16_t s, dp;
+        products(lds + 2 * TILE_BYTES, b, 32 * b, s, dp);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) own = s[i] > 0.f ? fmaf(s[i], dp[i], own) : own;
+      }
+      own += other_half(own);
+      delta = limit <= KT ? own : delta;
+    }
+    __syncthreads();
   }
-  const int tiles = (end + KT - 1) / KT;
+  if (in_q && h == 0 && split == 0) {   // for the key gradients, by row
+    a.stat_lse[static_cast<int64_t>(bh) * rows + row] = lse;
+    a.stat_delta[static_cast<int64_t>(bh) * rows + row] = delta;
+  }
 
   f32x16_t acc[DP / 32];
 #pragma unroll
   for (int m = 0; m < DP / 32; ++m) zero(acc[m]);
-  const float c = a.scale_log2;
-  Rng rng{};
-  if (DROP) rng = load_rng(a.rng);
-  const int64_t drop_row = (static_cast<int64_t>(w.b) * a.heads + head) * a.q_len + token;
-
-  const T* const kb = at<T>(a.k, a.k_stride, w.b, 0, w.kvh);
-  const T* const vb = at<T>(a.v, a.v_stride, w.b, 0, w.kvh);
-  Mover<T, DP, KT, THREADS> mk, mv;
-  if (tiles > 0) {
-    mk.keys(kb, a.k_stride[1], 0, end, a.dim);
-    mv.keys(vb, a.v_stride[1], 0, end, a.dim);
-  }
-  for (int t = 0; t < tiles; ++t) {
-    __syncthreads();
-    mk.put(kt);
-    mv.put(vt);
-    __syncthreads();
-    if (t + 1 < tiles) {
-      mk.keys(kb, a.k_stride[1], (t + 1) * KT, end, a.dim);
-      mv.keys(vb, a.v_stride[1], (t + 1) * KT, end, a.dim);
-    }
+  for (int t = t0; t < t1; ++t) {
+    arrived();
+    if (t + 1 < t1) stage(t + 1, (t + 1 - t0) & 1);
+    char* const kt = lds + ((t - t0) & 1) * 2 * TILE_BYTES;
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
-      const int key0 = t * KT + 32 * b;
       f32x16_t s, dp;
-      zero(s);
-      zero(dp);
+      products(kt, b, t * KT + 32 * b, s, dp);
 #pragma unroll
-      for (int i = 0; i < Tl::STEPS; ++i) {
-        s = mfma32(Tl::straight(kt, 32 * b + (lane & 31), i, h), q[i], s);
-        dp = mfma32(Tl::straight(vt, 32 * b + (lane & 31), i, h), g[i], dp);
-      }
-#pragma unroll
-      for (int k16 = 0; k16 < 2; ++k16) {
-        uint32_t bits[4];
-        if (DROP) drop_bits(a, rng, drop_row, (key0 >> 4) + k16, h, bits);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int i = 8 * k16 + j;
-          const float p = exp2_(fmaf(s[i], c, -lse));
-          float d = dp[i];
-          if (DROP) d = kept(bits, j, a.cut) ? d * a.inv_keep : 0.f;
-          s[i] = p * (d - delta);
-        }
-      }
-      if (key0 + 32 > all) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = key0 + 8 * (i >> 2) + 4 * h + (i & 3);
-          s[i] = key < limit ? s[i] : 0.f;
-        }
-      }
+      for (int i = 0; i < 16; ++i) s[i] = s[i] * (dp[i] - delta);
 #pragma unroll
       for (int k16 = 0; k16 < 2; ++k16) {
         Frag<T> p;
@@ -574,28 +698,68 @@ __global__ __launch_bounds__(64 * WR) void attn_dq_kernel(AttnArgs a) {
     }
   }
   if (!in_q) return;
-  store_row<T, DP>(at<T>(a.dq, a.q_stride, w.b, token, head), acc, limit > 0 ? a.scale : 0.f, h, a.dim);
+  const float f = limit > 0 ? a.scale : 0.f;
+  if (a.splits > 1)
+    store_row<float, DP>(a.part + ((static_cast<int64_t>(split) * a.batch * a.kv_heads + bh) * rows + row) * DP, acc, f, h, DP);
+  else
+    store_row<T, DP>(at<T>(a.dq, a.q_stride, w.b, token, head), acc, f, h, a.dim);
 }
 
 // ---------------------------------------------------------------------------
 // backward: key and value gradients
 // ---------------------------------------------------------------------------
 
+// One wave a SIMD above 64 channels of bf16: its key and value rows, and their gradients, take 192
+// registers.  With the value rows in LDS and two waves a SIMD it has too few left to ask for its
+// operands early: 890 us against 356 for 2 x 4096 causal tokens, 16 heads of 128 over 4.
 template <typename T, int DP, int WC, int RB, bool DROP>
-__global__ __launch_bounds__(64 * WC) void attn_dkv_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * WC, (DP * sizeof(T) > 128 ? 1 : 2)) void attn_dkv_kernel(AttnArgs a) {
   using Tl = Tile<T, DP>;
   constexpr int THREADS = 64 * WC, KEYS = 32 * WC, RT = 32 * RB;
-  constexpr int TILE_BYTES = RT * Tl::ROW_BYTES;
-  __shared__ __attribute__((aligned(16))) char lds[2 * TILE_BYTES + RT * 8 + (DROP ? WC * 32 * 4 : 0)];
-  char* const qt = lds;
-  char* const gt = lds + TILE_BYTES;
-  float* const lse_t = reinterpret_cast<float*>(lds + 2 * TILE_BYTES);
-  float* const delta_t = lse_t + RT;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-  const Where w = where(a, blockIdx.y);
-  const int key0 = blockIdx.x * KEYS + wave * 32, key = key0 + (lane & 31);
+  constexpr int TILE_BYTES = RT * Tl::ROW_BYTES, STAT_BYTES = 512;
+  constexpr int BUFFER = 2 * TILE_BYTES + STAT_BYTES;
+  __shared__ __attribute__((aligned(16))) char lds[2 * BUFFER + (DROP ? WC * 32 * 4 : 0)];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const Item item = work_item(a, false);
+  const int bh = item.bh, split = item.split, tile = item.tile;
+  const Where w = where(a, bh);
+  const int key0 = tile * KEYS + wave * 32, key = key0 + (lane & 31);
   const bool live = key < w.kv_len;
   const int key_at = live ? key : 0;
+
+  const int rows = w.q_len * a.group;
+  // the first token that sees the workgroup's first key
+  int first = 0;
+  if (a.causal) first = tile * KEYS - (w.kv_len - w.q_len);
+  first = first < 0 ? 0 : first;
+  const bool any = tile * KEYS < w.kv_len && first < w.q_len;
+  const int from = any ? first * a.group / RT : 0, tiles = any ? (rows + RT - 1) / RT - from : 0;
+  const int per = (tiles + a.splits - 1) / a.splits;
+  const int t0 = from + split * per, t1 = split * per + per < tiles ? t0 + per : from + tiles;
+  const float c = a.scale_log2;
+  Rng rng{};
+  if (DROP) rng = load_rng(a.rng);
+
+  const T* const qb = at<T>(a.q, a.q_stride, w.b, 0, w.kvh * a.group);
+  const T* const gb = at<T>(a.d_o, a.o_stride, w.b, 0, w.kvh * a.group);
+  Stager<T, DP, RT, THREADS> sq, sg;
+  const bool same = RT % a.group == 0;   // every whole tile has the same offsets
+  const int64_t stat0 = static_cast<int64_t>(bh) * a.q_len * a.group;
+  auto stage = [&](int t, bool offsets) {
+    const int r0 = t * RT, left = rows - r0, token0 = r0 / a.group;
+    if (offsets || !same || left < RT) {
+      sq.queries(a.q_stride[1], a.q_stride[2], r0, left, a.group, a.dim);
+      sg.queries(a.o_stride[1], a.o_stride[2], r0, left, a.group, a.dim);
+    }
+    char* const to = lds + (t & 1) * BUFFER;
+    sq.load(qb + token0 * a.q_stride[1], 0x7fffffffu, to);
+    sg.load(gb + token0 * a.o_stride[1], 0x7fffffffu, to + TILE_BYTES);
+    float* const st = reinterpret_cast<float*>(to + 2 * TILE_BYTES);
+    const int bytes = (left < RT ? left : RT) * 4;
+    if (wave == 0) stage_floats(a.stat_lse + stat0 + r0, bytes, st);
+    if (wave == 1) stage_floats(a.stat_delta + stat0 + r0, bytes, st + 64);
+  };
+  if (t0 < t1) stage(t0, true);
 
   Frag<T> k[Tl::STEPS], v[Tl::STEPS];
   load_row<T, DP>(at<T>(a.k, a.k_stride, w.b, key_at, w.kvh), live, h, a.dim, k);
@@ -606,64 +770,24 @@ __global__ __launch_bounds__(64 * WC) void attn_dkv_kernel(AttnArgs a) {
     zero(dk[m]);
     zero(dv[m]);
   }
-  const int rows = w.q_len * a.group;
-  // the first token that sees the workgroup's first key
-  int first = 0;
-  if (a.causal) first = blockIdx.x * KEYS - (w.kv_len - w.q_len);
-  first = (first < 0 ? 0 : first) * a.group;
-  const int t0 = static_cast<int>(blockIdx.x) * KEYS < w.kv_len ? first / RT : 0;
-  const int t1 = static_cast<int>(blockIdx.x) * KEYS < w.kv_len ? (rows + RT - 1) / RT : 0;
-  const float c = a.scale_log2;
-  Rng rng{};
-  if (DROP) rng = load_rng(a.rng);
-
-  const T* const qb = at<T>(a.q, a.q_stride, w.b, 0, w.kvh * a.group);
-  const T* const gb = at<T>(a.d_o, a.o_stride, w.b, 0, w.kvh * a.group);
-  Mover<T, DP, RT, THREADS> mq, mg;
-  float lse = INFINITY, delta = 0.f;
-  auto fetch = [&](int t) {
-    mq.queries(qb, a.q_stride[1], a.q_stride[2], t * RT, rows, a.group, a.dim);
-    mg.queries(gb, a.o_stride[1], a.o_stride[2], t * RT, rows, a.group, a.dim);
-    const int r = t * RT + static_cast<int>(threadIdx.x);
-    lse = INFINITY;
-    delta = 0.f;
-    if (threadIdx.x < RT && r < rows) {
-      const int token = r / a.group;
-      const int64_t stat = (w.head0 + r % a.group) * a.q_len + token;
-      if (seen(a, w, token) > 0) lse = a.lse[stat] * LOG2E;
-      delta = a.delta[stat];
-    }
-  };
-  if (t0 < t1) fetch(t0);
   for (int t = t0; t < t1; ++t) {
-    __syncthreads();
-    mq.put(qt);
-    mg.put(gt);
-    if (threadIdx.x < RT) {
-      lse_t[threadIdx.x] = lse;
-      delta_t[threadIdx.x] = delta;
-    }
-    __syncthreads();
-    if (t + 1 < t1) fetch(t + 1);
+    arrived();
+    if (t + 1 < t1) stage(t + 1, false);
+    char* const qt = lds + (t & 1) * BUFFER;
+    char* const gt = qt + TILE_BYTES;
+    const float* const lse_t = reinterpret_cast<const float*>(gt + TILE_BYTES);
+    const float* const delta_t = lse_t + 64;
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
       const int row0 = t * RT + 32 * b;
-      f32x16_t s, dp;
-      zero(s);
-      zero(dp);
-#pragma unroll
-      for (int i = 0; i < Tl::STEPS; ++i) {
-        s = mfma32(Tl::straight(qt, 32 * b + (lane & 31), i, h), k[i], s);
-        dp = mfma32(Tl::straight(gt, 32 * b + (lane & 31), i, h), v[i], dp);
-      }
       uint32_t keep = 0xffffffffu;   // bit n: row row0 + n keeps this lane's key
       if (DROP) {
         // the generator's groups run along the keys: each lane draws for its row, and the wave turns the
         // 32 x 32 bits round (a compare gives the bits of one key of each half for 32 rows)
         const int r = row0 + (lane & 31);
-        const int token = r / a.group, head = w.kvh * a.group + r % a.group;
+        const int token = r / a.group, head = w.kvh * a.group + r - token * a.group;
         const int64_t drop_row = (static_cast<int64_t>(w.b) * a.heads + head) * a.q_len + token;
-        uint32_t* const turn = reinterpret_cast<uint32_t*>(delta_t + RT) + wave * 32;
+        uint32_t* const turn = reinterpret_cast<uint32_t*>(lds + 2 * BUFFER) + wave * 32;
 #pragma unroll
         for (int k16 = 0; k16 < 2; ++k16) {
           uint32_t bits[4];
@@ -679,29 +803,48 @@ __global__ __launch_bounds__(64 * WC) void attn_dkv_kernel(AttnArgs a) {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         keep = turn[lane & 31];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_sched_barrier(0);   // before the products: their registers are not yet in use
       }
-      f32x16_t ds;
+      f32x16_t s, dp;
+      zero(s);
+      zero(dp);
+#pragma unroll
+      for (int i = 0; i < Tl::STEPS; ++i) {
+        s = mfma32(Tl::straight(qt, 32 * b + (lane & 31), i, h), k[i], s);
+        dp = mfma32(Tl::straight(gt, 32 * b + (lane & 31), i, h), v[i], dp);
+      }
+      // the block has pairs that are hidden
+      const int before = key - (w.kv_len - w.q_len);      // tokens that do not see this lane's key
+      const bool hidden = a.causal && row0 < max(key0 + 31 - (w.kv_len - w.q_len), 0) * a.group;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const float4 l4 = *reinterpret_cast<const float4*>(lse_t + 32 * b + 8 * g + 4 * h);
+        const float ll[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[4 * g + j] = exp2_(fmaf(s[4 * g + j], c, -ll[j]));
+      }
+      if (hidden) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int r = row0 + 8 * (i >> 2) + 4 * h + (i & 3);
+          s[i] = r >= max(before, 0) * a.group ? s[i] : 0.f;
+        }
+      }
+      // dp becomes ds, and s what multiplies do
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
         const float4 d4 = *reinterpret_cast<const float4*>(delta_t + 32 * b + 8 * g + 4 * h);
-        const float ll[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
+        const float dd[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int i = 4 * g + j;
-          float p = exp2_(fmaf(s[i], c, -ll[j]));
-          if (a.causal) {
-            const int r = row0 + 8 * g + 4 * h + j;
-            if (row0 < (key0 + 31 - (w.kv_len - w.q_len)) * a.group)   // the block has hidden pairs
-              p = key < r / a.group + w.kv_len - w.q_len + 1 ? p : 0.f;
-          }
-          float d = dp[i], pm = p;
+          float d = dp[i], pm = s[i];
           if (DROP) {
             const bool kp = (keep >> (8 * g + 4 * h + j)) & 1;
             d = kp ? d * a.inv_keep : 0.f;
-            pm = kp ? p : 0.f;
+            pm = kp ? pm : 0.f;
           }
-          ds[i] = p * (d - dd[j]);
+          dp[i] = s[i] * (d - dd[j]);
           s[i] = pm;
         }
       }
@@ -709,7 +852,7 @@ __global__ __launch_bounds__(64 * WC) void attn_dkv_kernel(AttnArgs a) {
       for (int r16 = 0; r16 < 2; ++r16) {
         Frag<T> p, d;
         operand(s, r16, p);
-        operand(ds, r16, d);
+        operand(dp, r16, d);
 #pragma unroll
         for (int m = 0; m < DP / 32; ++m) {
           dv[m] = mfma32(Tl::across(gt, 32 * b + 16 * r16, 32 * m, lane), p, dv[m]);
@@ -727,8 +870,47 @@ __global__ __launch_bounds__(64 * WC) void attn_dkv_kernel(AttnArgs a) {
       zero(dv[m]);
     }
   }
-  store_row<T, DP>(at<T>(a.dk, a.k_stride, w.b, key, w.kvh), dk, a.scale, h, a.dim);
-  store_row<T, DP>(at<T>(a.dv, a.v_stride, w.b, key, w.kvh), dv, a.inv_keep, h, a.dim);
+  if (a.splits > 1) {
+    // [dk, dv][split][batch x key heads][keys][DP]
+    const int64_t bhs = static_cast<int64_t>(a.batch) * a.kv_heads;
+    float* const to = a.part + ((split * bhs + bh) * a.kv_len + key) * DP;
+    store_row<float, DP>(to, dk, a.scale, h, DP);
+    store_row<float, DP>(to + a.splits * bhs * a.kv_len * DP, dv, a.inv_keep, h, DP);
+  } else {
+    store_row<T, DP>(at<T>(a.dk, a.k_stride, w.b, key, w.kvh), dk, a.scale, h, a.dim);
+    store_row<T, DP>(at<T>(a.dv, a.v_stride, w.b, key, w.kvh), dv, a.inv_keep, h, a.dim);
+  }
+}
+
+// Adds the splits of a gradient, 4 channels a thread, in their order: rows of [batch x key heads][rows].
+struct SumArgs {
+  const float* part;
+  void* out;
+  int64_t stride[3];
+  int64_t items, step;   // rows x DP / 4, elements between splits
+  int rows, splits, kv_heads, group, dim;
+};
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void attn_sum_kernel(SumArgs a0, SumArgs a1) {
+  const SumArgs& a = blockIdx.y == 0 ? a0 : a1;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= a.items) return;
+  const int64_t r = i / (DP / 4);
+  const int d = static_cast<int>(i - r * (DP / 4)) * 4;
+  if (d >= a.dim) return;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int n = 0; n < a.splits; ++n) {
+    const float4 v = *reinterpret_cast<const float4*>(a.part + n * a.step + r * DP + d);
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  const int bh = static_cast<int>(r / a.rows), row = static_cast<int>(r - static_cast<int64_t>(bh) * a.rows);
+  const int b = bh / a.kv_heads, kvh = bh - b * a.kv_heads, token = row / a.group;
+  T* const to = at<T>(a.out, a.stride, b, token, kvh * a.group + row - token * a.group) + d;
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
+  else
+    *reinterpret_cast<float4*>(to) = s;
 }
 
 // ---------------------------------------------------------------------------
@@ -738,24 +920,49 @@ __global__ __launch_bounds__(64 * WC) void attn_dkv_kernel(AttnArgs a) {
 template <typename T> struct Shape { static constexpr int KB = 2; };
 template <> struct Shape<float> { static constexpr int KB = 1; };
 
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 template <typename T, int DP, bool DROP>
-void forward_by(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
+void forward_by(AttnArgs& a, const AttnPlan& p, hipStream_t s) {
   const int rows = a.q_len * a.group, bh = a.batch * a.kv_heads;
-  const dim3 grid((rows + p.row_tile - 1) / p.row_tile, bh, a.splits);
+  a.tiles = static_cast<int>(ceil_div(rows, p.row_tile));
+  a.splits = p.splits;
+  const unsigned grid = static_cast<unsigned>(a.tiles) * bh * a.splits;
   if (p.row_tile == 32)
-    attn_forward_kernel<T, DP, 1, 2, 1, DROP><<<grid, 128, 0, s>>>(a);
+    attn_forward_kernel<T, DP, 1, 2, 1, 1, DROP><<<grid, 128, 0, s>>>(a);
   else
-    attn_forward_kernel<T, DP, 4, 1, Shape<T>::KB, DROP><<<grid, 256, 0, s>>>(a);
+    attn_forward_kernel<T, DP, 4, 1, 1, Shape<T>::KB, DROP><<<grid, 256, 0, s>>>(a);
   if (a.splits > 1) attn_join_kernel<T, DP><<<dim3((rows + 3) / 4, bh), 256, 0, s>>>(a);
 }
 
 template <typename T, int DP, bool DROP>
-void backward_by(const AttnArgs& a, const AttnPlan&, hipStream_t s) {
+void backward_by(AttnArgs& a, const AttnPlan& p, hipStream_t s) {
   const int rows = a.q_len * a.group, bh = a.batch * a.kv_heads;
-  if (rows > 0)
-    attn_dq_kernel<T, DP, 4, Shape<T>::KB, DROP><<<dim3((rows + 127) / 128, bh), 256, 0, s>>>(a);
-  if (a.kv_len > 0)
-    attn_dkv_kernel<T, DP, 4, Shape<T>::KB, DROP><<<dim3((a.kv_len + 127) / 128, bh), 256, 0, s>>>(a);
+  auto sum = [&](void* out, const int64_t (&st)[3], int n, int splits, int group) {
+    SumArgs r{a.part, out, {st[0], st[1], st[2]}, static_cast<int64_t>(bh) * n * (DP / 4),
+              static_cast<int64_t>(bh) * n * DP, n, splits, a.kv_heads, group, a.dim};
+    return r;
+  };
+  if (rows > 0) {
+    a.tiles = (rows + 127) / 128;
+    a.splits = p.dq_splits;
+    attn_dq_kernel<T, DP, 4, Shape<T>::KB, DROP><<<static_cast<unsigned>(a.tiles) * bh * a.splits, 256, 0, s>>>(a);
+    if (a.splits > 1) {
+      const SumArgs r = sum(a.dq, a.q_stride, rows, a.splits, a.group);
+      attn_sum_kernel<T, DP><<<static_cast<unsigned>(ceil_div(r.items, 256)), 256, 0, s>>>(r, r);
+    }
+  }
+  if (a.kv_len > 0) {
+    a.tiles = (a.kv_len + 127) / 128;
+    a.splits = p.dkv_splits;
+    attn_dkv_kernel<T, DP, 4, Shape<T>::KB, DROP><<<static_cast<unsigned>(a.tiles) * bh * a.splits, 256, 0, s>>>(a);
+    if (a.splits > 1) {
+      const SumArgs rk = sum(a.dk, a.k_stride, a.kv_len, a.splits, 1);
+      SumArgs rv = sum(a.dv, a.v_stride, a.kv_len, a.splits, 1);
+      rv.part += a.splits * rv.step;
+      attn_sum_kernel<T, DP><<<dim3(static_cast<unsigned>(ceil_div(rk.items, 256)), 2), 256, 0, s>>>(rk, rv);
+    }
+  }
 }
 
 #define PETRA_BY_DIM(F, T)                                                       \
@@ -773,26 +980,35 @@ void backward_by(const AttnArgs& a, const AttnPlan&, hipStream_t s) {
 
 int padded(int dim) { return (dim + 31) / 32 * 32; }
 
+// Few workgroups for 256 CUs: their inner axis is split until there are about two a CU,
+// with at least `least` of `length` a split.
+int splits_for(int64_t blocks, int64_t length, int64_t least) {
+  if (blocks == 0 || blocks >= 384) return 1;
+  const int64_t want = ceil_div(512, blocks), most = ceil_div(length, least);
+  const int64_t n = want < most ? want : most;
+  return static_cast<int>(n < 1 ? 1 : n);
+}
+
 }  // namespace
 
 AttnPlan attn_plan(const AttnArgs& a, int) {
   AttnPlan p{};
   const int64_t rows = static_cast<int64_t>(a.q_len) * a.group, bh = static_cast<int64_t>(a.batch) * a.kv_heads;
   p.row_tile = rows <= 32 ? 32 : 128;
-  const int64_t blocks = (rows + p.row_tile - 1) / p.row_tile * bh;
-  // few workgroups: split the keys until the chip's 256 CUs have about two each, 128 keys a split at least
-  int64_t splits = blocks == 0 || blocks >= 256 ? 1 : (512 + blocks - 1) / blocks;
-  const int64_t most = (a.kv_len + 127) / 128;
-  splits = splits < most ? splits : most;
-  p.splits = static_cast<int>(splits < 1 ? 1 : splits);
-  p.fwd_bytes = p.splits > 1 ? static_cast<size_t>(p.splits) * bh * rows * (padded(a.dim) + 2) * 4 : 0;
-  p.bwd_bytes = static_cast<size_t>(a.batch) * a.heads * a.q_len * 4;
+  p.splits = splits_for(ceil_div(rows, p.row_tile) * bh, a.kv_len, 128);
+  const size_t row = static_cast<size_t>(padded(a.dim)) * 4;
+  p.fwd_bytes = p.splits > 1 ? p.splits * bh * rows * (row + 8) : 0;
+  p.dq_splits = splits_for(ceil_div(rows, 128) * bh, a.kv_len, 256);
+  p.dkv_splits = splits_for(ceil_div(a.kv_len, 128) * bh, rows, 256);
+  const size_t dq = p.dq_splits > 1 ? p.dq_splits * bh * rows * row : 0;
+  const size_t dkv = p.dkv_splits > 1 ? 2 * p.dkv_splits * bh * a.kv_len * row : 0;
+  p.stat_bytes = 2 * ((static_cast<size_t>(bh) * rows * 4 + 15) / 16 * 16);
+  p.bwd_bytes = p.stat_bytes + (dq > dkv ? dq : dkv);
   return p;
 }
 
 void attn_forward(const AttnArgs& args, const AttnPlan& p, int dtype, void* workspace, hipStream_t s) {
   AttnArgs a = args;
-  a.splits = p.splits;
   a.part = static_cast<float*>(workspace);
   a.part_ml = a.part + static_cast<size_t>(p.splits) * a.batch * a.heads * a.q_len * padded(a.dim);
   if (dtype == 1) {
@@ -804,7 +1020,9 @@ void attn_forward(const AttnArgs& args, const AttnPlan& p, int dtype, void* work
 
 void attn_backward(const AttnArgs& args, const AttnPlan& p, int dtype, void* workspace, hipStream_t s) {
   AttnArgs a = args;
-  a.delta = static_cast<float*>(workspace);
+  a.stat_lse = static_cast<float*>(workspace);
+  a.stat_delta = a.stat_lse + p.stat_bytes / 8;
+  a.part = a.stat_lse + p.stat_bytes / 4;
   if (dtype == 1) {
     PETRA_BY_DIM(backward_by, bf16_t)
   } else {

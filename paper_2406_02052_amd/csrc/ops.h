@@ -43,7 +43,8 @@ void dropout(const void* x, const void* residual, void* y, long n, float factor,
 struct AttnArgs {
   const void *q, *k, *v, *o, *d_o;
   void *out, *dq, *dk, *dv;
-  float *lse, *delta;                        // [batch][heads][q_len]
+  float* lse;                                // [batch][heads][q_len]
+  float *stat_lse, *stat_delta;              // backward: log2(e) lse (+inf without keys) and D, [batch x key heads][rows]
   const int32_t *q_lens, *kv_lens;
   const uint64_t* rng;                       // null: no dropout
   int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];   // batch, token, head
@@ -52,7 +53,7 @@ struct AttnArgs {
   uint32_t cut;
   // keys (forward, query gradient) or rows (key and value gradients) split over
   // `splits` workgroups, whose fp32 partial results go to `part`
-  int splits;
+  int splits, tiles;                         // tiles: of rows or keys, of one key head
   float *part, *part_ml;
 };
 
@@ -60,7 +61,7 @@ struct AttnPlan {
   int row_tile, splits;            // forward
   size_t fwd_bytes;
   int dq_splits, dkv_splits;       // backward
-  size_t bwd_bytes;
+  size_t stat_bytes, bwd_bytes;
 };
 
 AttnPlan attn_plan(const AttnArgs& a, int dtype);

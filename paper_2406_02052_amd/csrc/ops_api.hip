@@ -170,8 +170,14 @@ struct Attn {
     need(a.k_stride[1] < (1 << 22) && a.v_stride[1] < (1 << 22), PETRA_ERR_SHAPE,
          "token stride of k or v of 2^22 elements or more");
     const int64_t nq[3] = {a.batch, a.q_len, a.heads}, nk[3] = {a.batch, a.kv_len, a.kv_heads};
+    // tiles of keys, and in the backward of queries, are addressed by 32-bit offsets from their first row
+    need(a.kv_len <= 1 || (a.k_stride[1] >= a.dim && a.v_stride[1] >= a.dim), PETRA_ERR_SHAPE,
+         "token stride of k or v below head_dim");
     need_distinct(a.o_stride, nq, a.dim, "o");
     if (backward) {
+      for (const int64_t* st : {a.q_stride, a.o_stride})
+        need((64 * st[1] + a.group * st[2]) * static_cast<int64_t>(esz) < (int64_t{1} << 31), PETRA_ERR_SHAPE,
+             "heads that share a key head, or tokens of q or o, too far apart");
       need_distinct(a.q_stride, nq, a.dim, "dq");
       need_distinct(a.k_stride, nk, a.dim, "dk");
       need_distinct(a.v_stride, nk, a.dim, "dv");
