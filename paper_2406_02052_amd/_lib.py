@@ -202,15 +202,17 @@ def _ptr(t) -> int:
     """Device address of a tensor (or an int address, or None)."""
     if t is None:
         return 0
-    if isinstance(t, int):
-        return t
-    return t.data_ptr()
+    try:
+        return t.data_ptr()
+    except AttributeError:
+        return int(t)
 
 
 def _stream(stream) -> int:
     if stream is None:
+        # the handle of torch.cuda.current_stream(), without the object around it
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

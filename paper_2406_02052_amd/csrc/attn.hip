@@ -45,8 +45,6 @@ __device__ __forceinline__ f32x16_t mfma32(const Frag<float>& a, const Frag<floa
 }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
-// Value of the lane in the other half of the wave.
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
 
 __device__ __forceinline__ void zero(f32x16_t& c) {
 #pragma unroll
@@ -198,19 +196,21 @@ __device__ __forceinline__ void stage_floats(const float* from, int bytes, float
                ::"s"(to), "v"((threadIdx.x & 63) * 4), "s"(r) : "memory");
 }
 
-// What this workgroup works on: (batch row, key head), split, tile.  Heads run fastest:
-// workgroups go to the 8 XCDs in turn, so that with a multiple of 8 heads each XCD's L2
-// has the keys of its own; tiles run slowest, from the one with most visible pairs where
-// the mask is causal, so that what is left for the end is short.
+// What this workgroup works on: (batch row, key head), split, tile.  Splits and heads run
+// fastest: workgroups go to the 8 XCDs in turn, so that with a multiple of 8 heads each XCD's
+// L2 has the keys of its own (2 x 4096 causal tokens, 16 heads: 165 us, 204 with the tiles
+// fastest), and the workgroups of a short sequence, which end at once, lie between others';
+// tiles run slowest, from the one with most visible pairs where the mask is causal, so that
+// what is left for the end is short.
 struct Item {
   int bh, split, tile;
 };
 __device__ __forceinline__ Item work_item(const AttnArgs& a, bool last_first) {
-  const int heads = a.batch * a.kv_heads, rest = blockIdx.x / heads;
+  const int heads = a.batch * a.kv_heads, rest = blockIdx.x / a.splits;
   Item i;
-  i.bh = blockIdx.x - rest * heads;
-  i.tile = rest / a.splits;
-  i.split = rest - i.tile * a.splits;
+  i.split = blockIdx.x - rest * a.splits;
+  i.tile = rest / heads;
+  i.bh = rest - i.tile * heads;
   if (last_first) i.tile = a.tiles - 1 - i.tile;
   return i;
 }
@@ -397,7 +397,7 @@ __global__ __launch_bounds__(64 * WR * WK, (NT * DP * sizeof(T) > 256 ? 1 : 2)) 
       for (int b = 0; b < KB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) m[n] = fmaxf(m[n], s[n][b][i]);
-      m[n] = fmaxf(m[n], other_half(m[n]));
+      m[n] = max_halves(m[n]);
       grew |= fmaf(m[n], c, -8.f) > top[n] * c;
     }
     if (__any(grew)) {
@@ -448,7 +448,7 @@ __global__ __launch_bounds__(64 * WR * WK, (NT * DP * sizeof(T) > 256 ? 1 : 2)) 
     }
   }
 #pragma unroll
-  for (int n = 0; n < NT; ++n) sum[n] += other_half(sum[n]);
+  for (int n = 0; n < NT; ++n) sum[n] = sum_halves(sum[n]);
 
   if constexpr (WK > 1) {
     // join the waves that shared the rows: statistics, then the scaled accumulators, in a fixed order
@@ -511,38 +511,63 @@ __global__ __launch_bounds__(64 * WR * WK, (NT * DP * sizeof(T) > 256 ? 1 : 2)) 
   }
 }
 
-// Joins the splits of one row: a wave a row, DP / 64 channels a lane.
+// Joins the splits of one row, a wave a row: lane s takes the statistics of split s, then groups
+// of DP / 4 lanes add splits side by side, 4 channels a lane, and the groups are added in order.
+constexpr int MOST_SPLITS = 64;
+
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
+  constexpr int WIDE = DP / 4, GROUPS = 64 / WIDE;
   const int lane = threadIdx.x & 63;
   const int rows = a.q_len * a.group;
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
-  const Where w = where(a, blockIdx.y);
-  const int64_t step = static_cast<int64_t>(gridDim.y) * rows, first = static_cast<int64_t>(blockIdx.y) * rows + row;
-  float n = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) n = fmaxf(n, a.part_ml[(first + s * step) * 2]);
-  constexpr int PER = (DP + 63) / 64;
-  float acc[PER] = {}, sum = 0.f;
-  for (int s = 0; s < a.splits; ++s) {
-    const int64_t i = first + s * step;
-    const float t = a.part_ml[i * 2];
-    if (t == -INFINITY) continue;
-    const float f = exp2_((t - n) * a.scale_log2);
-    sum = fmaf(a.part_ml[i * 2 + 1], f, sum);
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int64_t step = static_cast<int64_t>(a.batch) * a.kv_heads * rows;
+  if (item >= step) return;
+  const int bh = static_cast<int>(item / rows), row = static_cast<int>(item - static_cast<int64_t>(bh) * rows);
+  const int b = bh / a.kv_heads, kvh = bh - b * a.kv_heads;
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (lane < a.splits) ml = *reinterpret_cast<const float2*>(a.part_ml + (item + lane * step) * 2);
+  float top = ml.x;
 #pragma unroll
-    for (int e = 0; e < PER; ++e)
-      if (lane + 64 * e < DP) acc[e] = fmaf(a.part[i * DP + lane + 64 * e], f, acc[e]);
+  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+  const float f = ml.x == -INFINITY ? 0.f : exp2_((ml.x - top) * a.scale_log2);
+  float sum = f * ml.y;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
+  const int g = lane / WIDE, c = (lane - g * WIDE) * 4;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int s0 = 0; s0 < a.splits; s0 += GROUPS) {
+    const int s = s0 + g;
+    const float w = __shfl(f, s < MOST_SPLITS ? s : 0, 64);
+    if (g < GROUPS && s < a.splits && w > 0.f) {
+      const float4 v = *reinterpret_cast<const float4*>(a.part + (item + s * step) * DP + c);
+      acc.x = fmaf(v.x, w, acc.x);
+      acc.y = fmaf(v.y, w, acc.y);
+      acc.z = fmaf(v.z, w, acc.z);
+      acc.w = fmaf(v.w, w, acc.w);
+    }
   }
-  const int token = row / a.group, head = w.kvh * a.group + row % a.group;
-  const bool any = sum > 0.f || sum != sum;
-  const float f = any ? a.inv_keep / sum : 0.f;
-  T* const o = at<T>(a.out, a.o_stride, w.b, token, head);
 #pragma unroll
-  for (int e = 0; e < PER; ++e)
-    if (lane + 64 * e < a.dim) store1(o + lane + 64 * e, acc[e] * f);
+  for (int n = GROUPS / 2; n >= 1; n >>= 1) {
+    acc.x += __shfl_down(acc.x, n * WIDE, 64);
+    acc.y += __shfl_down(acc.y, n * WIDE, 64);
+    acc.z += __shfl_down(acc.z, n * WIDE, 64);
+    acc.w += __shfl_down(acc.w, n * WIDE, 64);
+  }
+  const int token = row / a.group, head = kvh * a.group + row - token * a.group;
+  const bool any = sum > 0.f || sum != sum;
+  const float n = any ? a.inv_keep / sum : 0.f;
+  if (lane < WIDE && c < a.dim) {
+    T* const o = at<T>(a.out, a.o_stride, b, token, head) + c;
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(acc.x * n, acc.y * n), pack_bf16x2(acc.z * n, acc.w * n));
+    else
+      *reinterpret_cast<float4*>(o) = make_float4(acc.x * n, acc.y * n, acc.z * n, acc.w * n);
+  }
   if (lane == 0)
-    a.lse[(w.head0 + row % a.group) * a.q_len + token] = any ? fmaf(n, a.scale, __builtin_amdgcn_logf(sum) * LN2) : -INFINITY;
+    a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.q_len + token] =
+        any ? fmaf(top, a.scale, __builtin_amdgcn_logf(sum) * LN2) : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------
@@ -614,7 +639,7 @@ __global__ __launch_bounds__(64 * WR, (DP * sizeof(T) > 256 ? 1 : 2)) void attn_
 #pragma unroll
         for (int i = 0; i < 8; ++i) delta = fmaf(x[i], y[i], delta);
       }
-    delta += other_half(delta);
+    delta = sum_halves(delta);
   }
   const int64_t stat = (static_cast<int64_t>(w.b) * a.heads + head) * a.q_len + token;
   // a row without keys: lse +inf makes every p zero
@@ -664,7 +689,7 @@ __global__ __launch_bounds__(64 * WR, (DP * sizeof(T) > 256 ? 1 : 2)) void attn_
 #pragma unroll
         for (int i = 0; i < 16; ++i) own = s[i] > 0.f ? fmaf(s[i], dp[i], own) : own;
       }
-      own += other_half(own);
+      own = sum_halves(own);
       delta = limit <= KT ? own : delta;
     }
     __syncthreads();
@@ -932,7 +957,8 @@ void forward_by(AttnArgs& a, const AttnPlan& p, hipStream_t s) {
     attn_forward_kernel<T, DP, 1, 2, 1, 1, DROP><<<grid, 128, 0, s>>>(a);
   else
     attn_forward_kernel<T, DP, 4, 1, 1, Shape<T>::KB, DROP><<<grid, 256, 0, s>>>(a);
-  if (a.splits > 1) attn_join_kernel<T, DP><<<dim3((rows + 3) / 4, bh), 256, 0, s>>>(a);
+  if (a.splits > 1)
+    attn_join_kernel<T, DP><<<static_cast<unsigned>(ceil_div(static_cast<int64_t>(rows) * bh, 4)), 256, 0, s>>>(a);
 }
 
 template <typename T, int DP, bool DROP>
@@ -980,12 +1006,15 @@ void backward_by(AttnArgs& a, const AttnPlan& p, hipStream_t s) {
 
 int padded(int dim) { return (dim + 31) / 32 * 32; }
 
-// Few workgroups for 256 CUs: their inner axis is split until there are about two a CU,
-// with at least `least` of `length` a split.
-int splits_for(int64_t blocks, int64_t length, int64_t least) {
-  if (blocks == 0 || blocks >= 384) return 1;
-  const int64_t want = ceil_div(512, blocks), most = ceil_div(length, least);
-  const int64_t n = want < most ? want : most;
+// Few workgroups for the chip, which holds `slots` at a time: their inner axis is split until
+// they fill it twice (ragged lengths and causal masks leave some short), with at least `least`
+// of `length` a split.  More splits cost more than they give: each writes its results in fp32.
+int splits_for(int64_t blocks, int64_t slots, int64_t length, int64_t least) {
+  if (blocks == 0 || 2 * blocks >= 3 * slots) return 1;
+  int64_t n = ceil_div(2 * slots, blocks);
+  const int64_t most = ceil_div(length, least);
+  n = n < most ? n : most;
+  n = n < MOST_SPLITS ? n : MOST_SPLITS;
   return static_cast<int>(n < 1 ? 1 : n);
 }
 
@@ -995,11 +1024,11 @@ AttnPlan attn_plan(const AttnArgs& a, int) {
   AttnPlan p{};
   const int64_t rows = static_cast<int64_t>(a.q_len) * a.group, bh = static_cast<int64_t>(a.batch) * a.kv_heads;
   p.row_tile = rows <= 32 ? 32 : 128;
-  p.splits = splits_for(ceil_div(rows, p.row_tile) * bh, a.kv_len, 128);
+  p.splits = splits_for(ceil_div(rows, p.row_tile) * bh, p.row_tile == 32 ? 512 : 256, a.kv_len, 128);
   const size_t row = static_cast<size_t>(padded(a.dim)) * 4;
   p.fwd_bytes = p.splits > 1 ? p.splits * bh * rows * (row + 8) : 0;
-  p.dq_splits = splits_for(ceil_div(rows, 128) * bh, a.kv_len, 256);
-  p.dkv_splits = splits_for(ceil_div(a.kv_len, 128) * bh, rows, 256);
+  p.dq_splits = splits_for(ceil_div(rows, 128) * bh, 256, a.kv_len, 256);
+  p.dkv_splits = splits_for(ceil_div(a.kv_len, 128) * bh, 256, rows, 256);
   const size_t dq = p.dq_splits > 1 ? p.dq_splits * bh * rows * row : 0;
   const size_t dkv = p.dkv_splits > 1 ? 2 * p.dkv_splits * bh * a.kv_len * row : 0;
   p.stat_bytes = 2 * ((static_cast<size_t>(bh) * rows * 4 + 15) / 16 * 16);

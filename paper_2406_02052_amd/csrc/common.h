@@ -181,6 +181,24 @@ __device__ __forceinline__ float sum_lane_groups(float v) {
   return v;
 }
 
+// The same over the lanes l and l ^ 32, and l and l ^ 16, of a wave64, in both: a
+// swap of half the lanes of two copies leaves one summand in each.
+__device__ __forceinline__ float sum_halves(float v) {
+  const uint32_t x = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float max_halves(float v) {
+  const uint32_t x = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_quarters(float v) {
+  const uint32_t x = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // Buffer resources (raw, stride 0) over [p, p + bytes): a load at a byte offset
 // past the end returns zeros and a store there is dropped, which gives
 // branch-free zero padding and masked stores.  Offsets are 32-bit.

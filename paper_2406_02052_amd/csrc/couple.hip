@@ -9,11 +9,11 @@
 // r (h gamma - z^ mean(h gamma z^) (- mean(h gamma))).  m is dropout's 0 or 1/keep.
 //
 // All of it is bound by memory: 2 reads and 2 writes an element forward, 4 and 3
-// backward.  A row stays in registers from its load to its store (a team of lanes
-// holds it, 8 elements a lane and step), so each tensor crosses memory once; the
-// row's sums are taken in fp32, in registers and, where a team is a whole
-// workgroup, through LDS.  The variance is the mean of squared differences from
-// the mean, a second pass over registers.
+// backward.  A row stays in registers from its load to its store, 8 elements a lane
+// of the team that holds it, so each tensor crosses memory once; the row's sums are
+// taken in fp32, in registers and, where a team has several waves, through LDS.  The
+// variance is the mean of squared differences from the mean, a second pass over
+// registers.
 #include "common.h"
 #include "ops.h"
 #include "philox.h"
@@ -26,66 +26,82 @@ namespace {
 // rows and teams
 // ---------------------------------------------------------------------------
 
-// A team of TEAM lanes holds a row in V chunks of 8 elements a lane: chunk v of
-// lane l covers elements 8 (v TEAM + l) ..  Teams of up to 64 lanes share a wave;
-// a team of 256 is a workgroup.
+// A team of TEAM lanes holds a row, lane l its elements 8 l .. 8 l + 7.  A workgroup
+// has THREADS / TEAM teams.
 template <int TEAM>
-struct TeamSum {
-  // Sums of N values over the team, in every lane.
+struct Team {
+  static constexpr int THREADS = TEAM > 256 ? TEAM : 256, TEAMS = THREADS / TEAM;
+  static constexpr int WAVES = TEAM > 64 ? TEAM / 64 : 1;
+  static constexpr int LDS = WAVES > 1 ? 4 * (THREADS / 64) : 1;   // floats: two sums, twice
+
+  // Sums of N (at most 2) values over the team, in every lane.  `turn` alternates: a wave that
+  // writes one half of lds has seen every wave leave it, at the barrier for the other half.
   template <int N>
-  static __device__ __forceinline__ void sum(float (&x)[N], float* lds) {
-    constexpr int W = TEAM < 64 ? TEAM : 64;
+  static __device__ __forceinline__ void sum(float (&x)[N], float* lds, int& turn) {
 #pragma unroll
-    for (int d = 1; d < W; d <<= 1)
-#pragma unroll
-      for (int i = 0; i < N; ++i) x[i] += __shfl_xor(x[i], d, 64);
-    if constexpr (TEAM > 64) {
-      const int wave = threadIdx.x >> 6;
-      __syncthreads();   // the last sum's readers are done
+    for (int i = 0; i < N; ++i) {
+      if constexpr (TEAM == 8) {
+        int v = __float_as_int(x[i]);
+        x[i] += __int_as_float(__builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, false));   // [1,0,3,2]
+        v = __float_as_int(x[i]);
+        x[i] += __int_as_float(__builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, false));   // [2,3,0,1]
+        v = __float_as_int(x[i]);
+        x[i] += __int_as_float(__builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, false));  // half mirror
+      } else {
+        x[i] = sum_quarters(sum16(x[i]));
+        if constexpr (TEAM >= 64) x[i] = sum_halves(x[i]);
+      }
+    }
+    if constexpr (WAVES > 1) {
+      const int wave = threadIdx.x >> 6, first = wave / WAVES * WAVES;
+      float* const to = lds + turn * (THREADS / 64) * 2;
+      turn ^= 1;
       if ((threadIdx.x & 63) == 0)
 #pragma unroll
-        for (int i = 0; i < N; ++i) lds[wave * N + i] = x[i];
+        for (int i = 0; i < N; ++i) to[wave * 2 + i] = x[i];
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         x[i] = 0.f;
 #pragma unroll
-        for (int w = 0; w < TEAM / 64; ++w) x[i] += lds[w * N + i];
+        for (int w = 0; w < WAVES; ++w) x[i] += to[(first + w) * 2 + i];
       }
     }
   }
 };
 
-// Normalises z in place to z^; returns 1 / deviation.  Lanes past the row hold
-// zeros and are put back to zero.
-template <int TEAM, int V>
-__device__ __forceinline__ float unit(float (&z)[V][8], const bool (&in)[V], bool layer, float inv_w,
-                                      float eps, float* lds) {
-  if (layer) {
-    float s[1] = {0.f};
+// Normalises N (1 or 2) rows in place, z to z^; r: 1 / deviation.  Lanes past the row hold zeros
+// and keep them.
+template <int TEAM, bool LAYER, int N>
+__device__ __forceinline__ void unit(float (&z)[N][8], float (&r)[N], bool in, float inv_w, float eps,
+                                     float* lds, int& turn) {
+  float s[N];
+  if constexpr (LAYER) {
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+    for (int n = 0; n < N; ++n) {
+      s[n] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[0] += z[v][e];
-    TeamSum<TEAM>::sum(s, lds);
-    const float mean = s[0] * inv_w;
+      for (int e = 0; e < 8; ++e) s[n] += z[n][e];
+    }
+    Team<TEAM>::sum(s, lds, turn);
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+    for (int n = 0; n < N; ++n)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[v][e] = in[v] ? z[v][e] - mean : 0.f;
+      for (int e = 0; e < 8; ++e) z[n][e] = in ? z[n][e] - s[n] * inv_w : 0.f;
   }
-  float q[1] = {0.f};
 #pragma unroll
-  for (int v = 0; v < V; ++v)
+  for (int n = 0; n < N; ++n) {
+    s[n] = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q[0] = fmaf(z[v][e], z[v][e], q[0]);
-  TeamSum<TEAM>::sum(q, lds);
-  const float r = rsqrtf(q[0] * inv_w + eps);
+    for (int e = 0; e < 8; ++e) s[n] = fmaf(z[n][e], z[n][e], s[n]);
+  }
+  Team<TEAM>::sum(s, lds, turn);
 #pragma unroll
-  for (int v = 0; v < V; ++v)
+  for (int n = 0; n < N; ++n) {
+    r[n] = rsqrtf(s[n] * inv_w + eps);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) z[v][e] *= r;
-  return r;
+    for (int e = 0; e < 8; ++e) z[n][e] *= r[n];
+  }
 }
 
 template <typename T>
@@ -102,64 +118,48 @@ __device__ __forceinline__ void load_or_zero(const T* p, bool in, float* o) {
 // forward
 // ---------------------------------------------------------------------------
 
-template <typename T, int TEAM, int V, bool DROP>
-__global__ __launch_bounds__(256) void couple_forward_kernel(CoupleArgs a) {
-  __shared__ float lds[4];
-  constexpr int TEAMS = 256 / TEAM;
-  const int lane = threadIdx.x % TEAM;
+// MEASURED_FORWARD
+template <typename T, int TEAM, bool LAYER, bool DROP>
+__global__ __launch_bounds__(Team<TEAM>::THREADS) void couple_forward_kernel(CoupleArgs a) {
+  using Tm = Team<TEAM>;
+  __shared__ float lds[Tm::LDS];
+  int turn = 0;
+  const int col = 8 * (threadIdx.x % TEAM);
   const long w = a.width;
-  const long row = static_cast<long>(blockIdx.x) * TEAMS + threadIdx.x / TEAM;
-  const bool live = row < a.rows;
-  bool in[V];
-  int col[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    col[v] = 8 * (v * TEAM + lane);
-    in[v] = live && col[v] < w;
-  }
-  const bool layer = a.layer != 0;
-  const T* x = static_cast<const T*>(a.x) + row * w;
-  float y[V][8];
-#pragma unroll
-  for (int v = 0; v < V; ++v) load_or_zero(x + col[v], in[v], y[v]);
+  const long row = static_cast<long>(blockIdx.x) * Tm::TEAMS + threadIdx.x / TEAM;
+  const bool in = row < a.rows && col < w;
+  const long at = row * w + col;
+  float y[1][8], r[1];
+  load_or_zero(static_cast<const T*>(a.x) + at, in, y[0]);
   if (a.f != nullptr) {
-    const T* f = static_cast<const T*>(a.f) + row * w;
-    float n[V][8];
-#pragma unroll
-    for (int v = 0; v < V; ++v) load_or_zero(f + col[v], in[v], n[v]);
-    unit<TEAM, V>(n, in, layer, a.inv_width, a.eps, lds);
-    const float* gate = a.gate + (live ? row / a.rows_per_gate : 0) * w;
-    Rng rng{};
-    if (DROP) rng = load_rng(a.rng);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      if (!in[v]) continue;
+    float n[1][8];
+    load_or_zero(static_cast<const T*>(a.f) + at, in, n[0]);
+    uint32_t bits[4];
+    if (DROP) philox(load_rng(a.rng), static_cast<uint64_t>(at) >> 3, bits);
+    unit<TEAM, LAYER>(n, r, in, a.inv_width, a.eps, lds, turn);
+    if (in) {
       float gm[8], gg[8], bb[8] = {};
-      Vec8<float>::load(a.post_gamma + col[v], gm);
-      if (a.post_beta != nullptr) Vec8<float>::load(a.post_beta + col[v], bb);
-      Vec8<float>::load(gate + col[v], gg);
-      uint32_t bits[4];
-      if (DROP) philox(rng, static_cast<uint64_t>(row * w + col[v]) >> 3, bits);
+      Vec8<float>::load(a.post_gamma + col, gm);
+      if (a.post_beta != nullptr) Vec8<float>::load(a.post_beta + col, bb);
+      Vec8<float>::load(a.gate + row / a.rows_per_gate * w + col, gg);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        float t = fmaf(n[v][e], gm[e], bb[e]);
+        float t = fmaf(n[0][e], gm[e], bb[e]);
         if (DROP) t = kept(bits, e, a.cut) ? t * a.inv_keep : 0.f;
-        y[v][e] = quant(fmaf(gg[e], t, a.scale * y[v][e]), static_cast<const T*>(nullptr));
+        y[0][e] = quant(fmaf(gg[e], t, a.scale * y[0][e]), static_cast<const T*>(nullptr));
       }
-      Vec8<T>::store(static_cast<T*>(a.y) + row * w + col[v], y[v]);
+      Vec8<T>::store(static_cast<T*>(a.y) + at, y[0]);
     }
   }
   if (a.u != nullptr) {
-    unit<TEAM, V>(y, in, layer, a.inv_width, a.eps, lds);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      if (!in[v]) continue;
+    unit<TEAM, LAYER>(y, r, in, a.inv_width, a.eps, lds, turn);
+    if (in) {
       float gm[8], bb[8] = {};
-      Vec8<float>::load(a.pre_gamma + col[v], gm);
-      if (a.pre_beta != nullptr) Vec8<float>::load(a.pre_beta + col[v], bb);
+      Vec8<float>::load(a.pre_gamma + col, gm);
+      if (a.pre_beta != nullptr) Vec8<float>::load(a.pre_beta + col, bb);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[v][e] = fmaf(y[v][e], gm[e], bb[e]);
-      Vec8<T>::store(static_cast<T*>(a.u) + row * w + col[v], y[v]);
+      for (int e = 0; e < 8; ++e) y[0][e] = fmaf(y[0][e], gm[e], bb[e]);
+      Vec8<T>::store(static_cast<T*>(a.u) + at, y[0]);
     }
   }
 }
@@ -174,26 +174,28 @@ __global__ __launch_bounds__(256) void couple_forward_kernel(CoupleArgs a) {
 // fixed order and the workgroup's written to a row of partial sums.  A second
 // kernel adds those rows, also in a fixed order: results do not depend on timing.
 // Spans hold whole gates (their dgate is written at once) or a part of one gate; with
-// a gate a row, a row's dgate is written with the row.
-template <typename T, int TEAM, int V, bool DROP, bool PRE>
-__global__ __launch_bounds__(256) void couple_backward_kernel(CoupleArgs a) {
-  constexpr int TEAMS = 256 / TEAM;
+// a gate a row, a row's dgate is written with the row.  The next row's tensors are
+// asked for before this one's sums, which wait for the team's waves.
+// FULL: a layer norm or a beta (the sums that only those need).
+// MEASURED_BACKWARD
+template <typename T, int TEAM, bool FULL, bool DROP, bool PRE>
+__global__ __launch_bounds__(Team<TEAM>::THREADS) void couple_backward_kernel(CoupleArgs a) {
+  using Tm = Team<TEAM>;
+  constexpr int TEAMS = Tm::TEAMS, THREADS = Tm::THREADS;
+  // 1024 lanes have 128 registers each: no room for the next row, nor for the parameters
+  constexpr bool LEAN = TEAM == 1024;
   // partial sums of the teams, one parameter at a time
-  __shared__ float lds[TEAM > 64 ? 16 : 256 * V * 8];
-  const int lane = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+  __shared__ float joined[TEAMS > 1 ? THREADS * 8 : 1];
+  __shared__ float lds[Tm::LDS];
+  int turn = 0;
+  const int team = threadIdx.x / TEAM, col = 8 * (threadIdx.x % TEAM);
   const long w = a.width;
-  bool col_in[V];
-  int col[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    col[v] = 8 * (v * TEAM + lane);
-    col_in[v] = col[v] < w;
-  }
-  const bool layer = a.layer != 0;
+  const bool col_in = col < w;
+  const bool layer = FULL && a.layer != 0;
   const bool has_f = a.has_f != 0;
   Rng rng{};
   if (DROP) rng = load_rng(a.rng);
-  float gpost[V][8] = {}, bpost[V][8] = {}, gpre[V][8] = {}, bpre[V][8] = {};
+  float gpost[8] = {}, bpost[8] = {}, gpre[8] = {}, bpre[8] = {};
 
   // this workgroup's rows, by gate
   long gate0, gate1, part = 0, first, last;
@@ -211,28 +213,46 @@ __global__ __launch_bounds__(256) void couple_backward_kernel(CoupleArgs a) {
   }
 
   // adds the teams' sums of one parameter and writes them to `to`
-  auto flush = [&](float (&x)[V][8], float* to) {
+  auto flush = [&](const float (&x)[8], float* to) {
     if constexpr (TEAMS > 1) {
       __syncthreads();
-#pragma unroll
-      for (int v = 0; v < V; ++v) Vec8<float>::store(lds + team * (TEAM * V * 8) + col[v], x[v]);
+      Vec8<float>::store(joined + team * (TEAM * 8) + col, x);
       __syncthreads();
-      for (int c = threadIdx.x; c < w; c += 256) {
+      for (int c = threadIdx.x; c < w; c += THREADS) {
         float s = 0.f;
 #pragma unroll
-        for (int t = 0; t < TEAMS; ++t) s += lds[t * (TEAM * V * 8) + c];
+        for (int t = 0; t < TEAMS; ++t) s += joined[t * (TEAM * 8) + c];
         to[c] = s;
       }
-      __syncthreads();
-    } else {
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (col_in[v]) Vec8<float>::store(to + col[v], x[v]);
+    } else if (col_in) {
+      Vec8<float>::store(to + col, x);
     }
   };
 
+  float post_gamma[8] = {}, post_beta[8] = {}, pre_gamma[8] = {};
+  auto load_post = [&] {
+    Vec8<float>::load(a.post_gamma + col, post_gamma);
+    if (FULL && a.post_beta != nullptr) Vec8<float>::load(a.post_beta + col, post_beta);
+  };
+  if (col_in && !LEAN) {
+    if (has_f) load_post();
+    if (PRE) Vec8<float>::load(a.pre_gamma + col, pre_gamma);
+  }
+
+  Raw8<T> next[4];
+  auto fetch = [&](long row, bool live) {
+    const long at = row * w + col;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) next[i].zero();
+    if (!live || !col_in) return;
+    next[0].load(static_cast<const T*>(a.y_in) + at);
+    next[1].load(static_cast<const T*>(a.dy) + at);
+    if (PRE) next[2].load(static_cast<const T*>(a.du) + at);
+    if (has_f) next[3].load(static_cast<const T*>(a.f) + at);
+  };
+
   for (long g = gate0; g < gate1; ++g) {
-    float dg[V][8] = {};
+    float dg[8] = {};
     first = g * a.rows_per_gate;
     last = first + a.rows_per_gate;
     if (gate_a_row) {
@@ -242,107 +262,83 @@ __global__ __launch_bounds__(256) void couple_backward_kernel(CoupleArgs a) {
       first += part * a.rows_per_chunk;
       if (first + a.rows_per_chunk < last) last = first + a.rows_per_chunk;
     }
+    float gate[8] = {};
+    if (!LEAN && has_f && !gate_a_row && col_in) Vec8<float>::load(a.gate + g * w + col, gate);
+    if (!LEAN) fetch(first + team, first + team < last);
     // every team makes as many rounds: the sums over a team wait for its waves
     for (long base = first; base < last; base += TEAMS) {
       const long row = base + team;
-      const bool live = row < last;
-      bool in[V];
-#pragma unroll
-      for (int v = 0; v < V; ++v) in[v] = live && col_in[v];
-      float y[V][8], t[V][8];
-      const long at = row * w;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        load_or_zero(static_cast<const T*>(a.y_in) + at + col[v], in[v], y[v]);
-        load_or_zero(static_cast<const T*>(a.dy) + at + col[v], in[v], t[v]);
-      }
+      const bool in = row < last && col_in;
+      const long at = row * w + col;
+      if (LEAN) fetch(row, row < last);
+      float y[8], t[8], z[2][8], h[8], r[2];   // z: y^ and f^
+      next[0].to_f32(y);
+      next[1].to_f32(t);
+      if (PRE) next[2].to_f32(h);
+      next[0].to_f32(z[0]);
+      next[3].to_f32(z[1]);
+      if (has_f && gate_a_row && in) Vec8<float>::load(a.gate + at, gate);
+      if (!LEAN && base + TEAMS < last) fetch(row + TEAMS, row + TEAMS < last);
+      if (layer)
+        unit<TEAM, true>(z, r, in, a.inv_width, a.eps, lds, turn);
+      else
+        unit<TEAM, false>(z, r, in, a.inv_width, a.eps, lds, turn);
       if constexpr (PRE) {
-        float yn[V][8], h[V][8], s[2] = {0.f, 0.f};
+        if (LEAN && col_in) Vec8<float>::load(a.pre_gamma + col, pre_gamma);
+        float s[2] = {0.f, 0.f};
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          load_or_zero(static_cast<const T*>(a.du) + at + col[v], in[v], h[v]);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) yn[v][e] = y[v][e];
+        for (int e = 0; e < 8; ++e) {
+          gpre[e] = fmaf(h[e], z[0][e], gpre[e]);
+          if (FULL) bpre[e] += h[e];
+          h[e] *= pre_gamma[e];
+          s[0] = fmaf(h[e], z[0][e], s[0]);
+          s[1] += h[e];
         }
-        const float r = unit<TEAM, V>(yn, in, layer, a.inv_width, a.eps, lds);
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          float gm[8] = {};
-          if (col_in[v]) Vec8<float>::load(a.pre_gamma + col[v], gm);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            gpre[v][e] = fmaf(h[v][e], yn[v][e], gpre[v][e]);
-            bpre[v][e] += h[v][e];
-            h[v][e] *= gm[e];
-            s[0] = fmaf(h[v][e], yn[v][e], s[0]);
-            s[1] += h[v][e];
-          }
-        }
-        TeamSum<TEAM>::sum(s, lds);
+        Tm::sum(s, lds, turn);
         const float c0 = s[0] * a.inv_width, c1 = layer ? s[1] * a.inv_width : 0.f;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            t[v][e] = fmaf(r, h[v][e] - yn[v][e] * c0 - c1, t[v][e]);
+        for (int e = 0; e < 8; ++e) t[e] = fmaf(r[0], h[e] - z[0][e] * c0 - c1, t[e]);
       }
       if (has_f) {
-        float n[V][8], h[V][8], s[2] = {0.f, 0.f};
-#pragma unroll
-        for (int v = 0; v < V; ++v) load_or_zero(static_cast<const T*>(a.f) + at + col[v], in[v], n[v]);
-        const float r = unit<TEAM, V>(n, in, layer, a.inv_width, a.eps, lds);
-        const float* gate = a.gate + (gate_a_row ? row : g) * w;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          if (gate_a_row)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dg[v][e] = 0.f;
-          if (!in[v]) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) h[v][e] = 0.f;
-            continue;
-          }
-          float gm[8], gg[8], bb[8] = {};
-          Vec8<float>::load(a.post_gamma + col[v], gm);
-          if (a.post_beta != nullptr) Vec8<float>::load(a.post_beta + col[v], bb);
-          Vec8<float>::load(gate + col[v], gg);
-          uint32_t bits[4];
-          if (DROP) philox(rng, static_cast<uint64_t>(at + col[v]) >> 3, bits);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float nm = fmaf(n[v][e], gm[e], bb[e]), d = gg[e] * t[v][e];
-            if (DROP) {
-              const bool k = kept(bits, e, a.cut);
-              nm = k ? nm * a.inv_keep : 0.f;
-              d = k ? d * a.inv_keep : 0.f;
-            }
-            dg[v][e] = fmaf(t[v][e], nm, dg[v][e]);
-            gpost[v][e] = fmaf(d, n[v][e], gpost[v][e]);
-            bpost[v][e] += d;
-            h[v][e] = d * gm[e];
-            s[0] = fmaf(h[v][e], n[v][e], s[0]);
-            s[1] += h[v][e];
-            y[v][e] = fmaf(-gg[e], nm, y[v][e]) * a.inv_scale;
-          }
+        if (LEAN && col_in) {
+          load_post();
+          if (!gate_a_row) Vec8<float>::load(a.gate + g * w + col, gate);
         }
-        TeamSum<TEAM>::sum(s, lds);
+        float s[2] = {0.f, 0.f};
+        uint32_t bits[4];
+        if (DROP) philox(rng, static_cast<uint64_t>(at) >> 3, bits);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float nm = z[1][e] * post_gamma[e], d = gate[e] * t[e];
+          if (FULL) nm += post_beta[e];
+          if (DROP) {
+            const bool k = kept(bits, e, a.cut);
+            nm = k ? nm * a.inv_keep : 0.f;
+            d = k ? d * a.inv_keep : 0.f;
+          }
+          if (!in) d = 0.f, nm = 0.f;   // past the row: t is (nothing - mean) there
+          dg[e] = gate_a_row ? t[e] * nm : fmaf(t[e], nm, dg[e]);
+          gpost[e] = fmaf(d, z[1][e], gpost[e]);
+          if (FULL) bpost[e] += d;
+          h[e] = d * post_gamma[e];
+          s[0] = fmaf(h[e], z[1][e], s[0]);
+          s[1] += h[e];
+          y[e] = fmaf(-gate[e], nm, y[e]) * a.inv_scale;
+        }
+        Tm::sum(s, lds, turn);
         const float c0 = s[0] * a.inv_width, c1 = layer ? s[1] * a.inv_width : 0.f;
+        if (in) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          if (!in[v]) continue;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) h[v][e] = r * (h[v][e] - n[v][e] * c0 - c1);
-          Vec8<T>::store(static_cast<T*>(a.df) + at + col[v], h[v]);
-          if (a.x_out != nullptr) Vec8<T>::store(static_cast<T*>(a.x_out) + at + col[v], y[v]);
-          if (gate_a_row) Vec8<float>::store(a.dgate + at + col[v], dg[v]);
+          for (int e = 0; e < 8; ++e) h[e] = r[1] * (h[e] - z[1][e] * c0 - c1);
+          Vec8<T>::store(static_cast<T*>(a.df) + at, h);
+          if (a.x_out != nullptr) Vec8<T>::store(static_cast<T*>(a.x_out) + at, y);
+          if (gate_a_row) Vec8<float>::store(a.dgate + at, dg);
         }
       }
+      if (in) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        if (!in[v]) continue;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) t[v][e] *= a.scale;
-        Vec8<T>::store(static_cast<T*>(a.dx) + at + col[v], t[v]);
+        for (int e = 0; e < 8; ++e) t[e] *= a.scale;
+        Vec8<T>::store(static_cast<T*>(a.dx) + at, t);
       }
     }
     if (has_f && !gate_a_row)
@@ -351,35 +347,43 @@ __global__ __launch_bounds__(256) void couple_backward_kernel(CoupleArgs a) {
   const long block = blockIdx.x;
   if (has_f) {
     flush(gpost, a.part_post_gamma + block * w);
-    if (a.post_beta != nullptr) flush(bpost, a.part_post_beta + block * w);
+    if (FULL && a.post_beta != nullptr) flush(bpost, a.part_post_beta + block * w);
   }
   if (PRE) {
     flush(gpre, a.part_pre_gamma + block * w);
-    if (a.pre_beta != nullptr) flush(bpre, a.part_pre_beta + block * w);
+    if (FULL && a.pre_beta != nullptr) flush(bpre, a.part_pre_beta + block * w);
   }
 }
 
 // Adds rows of partial sums: out[o][c] = sum over r of part[o * rows + r][c], in 16
-// interleaved sums a column, then joined.
+// interleaved sums a column, then joined.  blockIdx.y counts the outputs of all sets.
 struct JoinSet {
   const float* part;
   float* out;
   long outs, rows;
 };
 struct JoinArgs {
-  JoinSet set[5];
+  JoinSet set[6];
+  int sets;
   long width;
 };
 
 __global__ __launch_bounds__(1024) void couple_join_kernel(JoinArgs a) {
   __shared__ float lds[16][64];
-  const JoinSet s = a.set[blockIdx.z];
   const long c = static_cast<long>(blockIdx.x) * 64 + (threadIdx.x & 63);
   const int lane = threadIdx.x >> 6;
-  for (long o = blockIdx.y; o < s.outs; o += gridDim.y) {
+  long o = blockIdx.y;
+  int n = 0;
+  while (n + 1 < a.sets && o >= a.set[n].outs) o -= a.set[n++].outs;
+  const JoinSet s = a.set[n];
+  // the last set has more outputs than a grid has rows
+  for (; o < s.outs; o += gridDim.y) {
     float v = 0.f;
-    if (c < a.width)
-      for (long r = lane; r < s.rows; r += 16) v += s.part[(o * s.rows + r) * a.width + c];
+    if (c < a.width) {
+      const float* p = s.part + (o * s.rows) * a.width + c;
+#pragma unroll 8
+      for (long r = lane; r < s.rows; r += 16) v += p[r * a.width];
+    }
     lds[lane][threadIdx.x & 63] = v;
     __syncthreads();
     if (lane == 0 && c < a.width) {
@@ -389,6 +393,7 @@ __global__ __launch_bounds__(1024) void couple_join_kernel(JoinArgs a) {
       s.out[o * a.width + c] = t;
     }
     __syncthreads();
+    if (n + 1 < a.sets) break;
   }
 }
 
@@ -430,49 +435,64 @@ __global__ __launch_bounds__(256) void dropout_kernel(const T* x, const T* resid
 // launches
 // ---------------------------------------------------------------------------
 
-template <typename T, int TEAM, int V>
+template <typename T, int TEAM>
 void forward_launch(const CoupleArgs& a, hipStream_t s) {
-  const unsigned blocks = static_cast<unsigned>((a.rows + 256 / TEAM - 1) / (256 / TEAM));
-  if (a.rng != nullptr)
-    couple_forward_kernel<T, TEAM, V, true><<<blocks, 256, 0, s>>>(a);
-  else
-    couple_forward_kernel<T, TEAM, V, false><<<blocks, 256, 0, s>>>(a);
-}
-
-template <typename T, int TEAM, int V>
-void backward_launch(const CoupleArgs& a, hipStream_t s) {
-  const unsigned n = static_cast<unsigned>(a.blocks);
-  if (a.rng != nullptr) {
-    if (a.has_u)
-      couple_backward_kernel<T, TEAM, V, true, true><<<n, 256, 0, s>>>(a);
-    else
-      couple_backward_kernel<T, TEAM, V, true, false><<<n, 256, 0, s>>>(a);
+  using Tm = Team<TEAM>;
+  const unsigned n = static_cast<unsigned>((a.rows + Tm::TEAMS - 1) / Tm::TEAMS);
+  if (a.layer) {
+    if (a.rng != nullptr) couple_forward_kernel<T, TEAM, true, true><<<n, Tm::THREADS, 0, s>>>(a);
+    else couple_forward_kernel<T, TEAM, true, false><<<n, Tm::THREADS, 0, s>>>(a);
   } else {
-    if (a.has_u)
-      couple_backward_kernel<T, TEAM, V, false, true><<<n, 256, 0, s>>>(a);
-    else
-      couple_backward_kernel<T, TEAM, V, false, false><<<n, 256, 0, s>>>(a);
+    if (a.rng != nullptr) couple_forward_kernel<T, TEAM, false, true><<<n, Tm::THREADS, 0, s>>>(a);
+    else couple_forward_kernel<T, TEAM, false, false><<<n, Tm::THREADS, 0, s>>>(a);
   }
 }
 
-// Lanes a row by its width: 8 elements a lane up to 64 lanes, then more chunks a
-// lane, then the whole workgroup.
-#define PETRA_BY_WIDTH(LAUNCH, T)                      \
-  if (a.width <= 64) LAUNCH<T, 8, 1>(a, s);            \
-  else if (a.width <= 256) LAUNCH<T, 32, 1>(a, s);     \
-  else if (a.width <= 512) LAUNCH<T, 64, 1>(a, s);     \
-  else if (a.width <= 1024) LAUNCH<T, 64, 2>(a, s);    \
-  else if (a.width <= 2048) LAUNCH<T, 256, 1>(a, s);   \
-  else if (a.width <= 4096) LAUNCH<T, 256, 2>(a, s);   \
-  else LAUNCH<T, 256, 4>(a, s);
+template <typename T, int TEAM, bool FULL>
+void backward_by(const CoupleArgs& a, hipStream_t s) {
+  using Tm = Team<TEAM>;
+  const unsigned n = static_cast<unsigned>(a.blocks);
+  if (a.rng != nullptr) {
+    if (a.has_u) couple_backward_kernel<T, TEAM, FULL, true, true><<<n, Tm::THREADS, 0, s>>>(a);
+    else couple_backward_kernel<T, TEAM, FULL, true, false><<<n, Tm::THREADS, 0, s>>>(a);
+  } else {
+    if (a.has_u) couple_backward_kernel<T, TEAM, FULL, false, true><<<n, Tm::THREADS, 0, s>>>(a);
+    else couple_backward_kernel<T, TEAM, FULL, false, false><<<n, Tm::THREADS, 0, s>>>(a);
+  }
+}
+
+template <typename T, int TEAM>
+void backward_launch(const CoupleArgs& a, hipStream_t s) {
+  if (a.layer || a.post_beta != nullptr || a.pre_beta != nullptr) backward_by<T, TEAM, true>(a, s);
+  else backward_by<T, TEAM, false>(a, s);
+}
+
+// Lanes a row: the fewest that hold it, 8 elements each.
+int team(int width) {
+  return width <= 64 ? 8 : width <= 256 ? 32 : width <= 512 ? 64 : width <= 1024 ? 128 : width <= 2048 ? 256
+         : width <= 4096 ? 512 : 1024;
+}
+
+#define PETRA_BY_WIDTH(LAUNCH, T)             \
+  switch (team(a.width)) {                    \
+    case 8: LAUNCH<T, 8>(a, s); break;        \
+    case 32: LAUNCH<T, 32>(a, s); break;      \
+    case 64: LAUNCH<T, 64>(a, s); break;      \
+    case 128: LAUNCH<T, 128>(a, s); break;    \
+    case 256: LAUNCH<T, 256>(a, s); break;    \
+    case 512: LAUNCH<T, 512>(a, s); break;    \
+    default: LAUNCH<T, 1024>(a, s); break;    \
+  }
 
 }  // namespace
 
 void couple_plan(CoupleArgs& a) {
   // rows that a workgroup works on at once
-  const long teams = a.width <= 64 ? 32 : a.width <= 256 ? 8 : a.width <= 1024 ? 4 : 1;
-  // about two workgroups a CU: partial sums are a row of the width for each of them
-  long span = (a.rows + 511) / 512;
+  const int lanes = team(a.width);
+  const long teams = lanes < 256 ? 256 / lanes : 1;
+  // three workgroups of 256 lanes a CU, or as many lanes: partial sums are a row of the width for each of them
+  const long most = lanes <= 256 ? 768 : lanes == 512 ? 512 : 256;
+  long span = (a.rows + most - 1) / most;
   span = span < 1 ? teams : (span + teams - 1) / teams * teams;
   a.gates_per_block = a.chunks_per_gate = 1;
   a.rows_per_chunk = span;
@@ -506,17 +526,14 @@ void couple_backward(const CoupleArgs& a, int dtype, hipStream_t s) {
     PETRA_BY_WIDTH(backward_launch, float)
   }
   JoinArgs j{};
-  int n = 0;
-  long most = 1;
+  long outs = 0;
   j.width = a.width;
-  auto add = [&](const float* part, float* out, long outs, long rows) {
-    j.set[n++] = {part, out, outs, rows};
-    if (outs > most) most = outs;
+  auto add = [&](const float* part, float* out, long n, long rows) {
+    if (n == 0) return;
+    j.set[j.sets++] = {part, out, n, rows};
+    outs += n;
   };
   if (a.has_f) {
-    // without rows the sums are zeros, that of the one gate too
-    if (a.blocks == 0) add(nullptr, a.dgate, a.gates, 0);
-    if (a.chunks_per_gate > 1) add(a.part_gate, a.dgate, a.gates, a.chunks_per_gate);
     add(a.part_post_gamma, a.dpost_gamma, 1, a.blocks);
     if (a.post_beta != nullptr) add(a.part_post_beta, a.dpost_beta, 1, a.blocks);
   }
@@ -524,9 +541,13 @@ void couple_backward(const CoupleArgs& a, int dtype, hipStream_t s) {
     add(a.part_pre_gamma, a.dpre_gamma, 1, a.blocks);
     if (a.pre_beta != nullptr) add(a.part_pre_beta, a.dpre_beta, 1, a.blocks);
   }
-  if (n > 0)
-    couple_join_kernel<<<dim3(static_cast<unsigned>((a.width + 63) / 64),
-                              static_cast<unsigned>(most < 1024 ? most : 1024), n),
+  if (a.has_f) {
+    // without rows the sums are zeros, that of the one gate too
+    if (a.blocks == 0) add(nullptr, a.dgate, a.gates, 0);
+    if (a.chunks_per_gate > 1) add(a.part_gate, a.dgate, a.gates, a.chunks_per_gate);
+  }
+  if (j.sets > 0)
+    couple_join_kernel<<<dim3(static_cast<unsigned>((a.width + 63) / 64), static_cast<unsigned>(outs < 4096 ? outs : 4096)),
                          1024, 0, s>>>(j);
 }
 

@@ -21,7 +21,7 @@ def _types(dtype: str):
 
 
 def _need(t, name: str, dtype, shape, dense: bool = True) -> None:
-    if t.dtype is not dtype or tuple(t.shape) != shape or not t.is_cuda:
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
         raise ValueError(f"{name}: need a device tensor {shape} of {dtype}, got {tuple(t.shape)} "
                          f"of {t.dtype} on {t.device}")
     if dense and not t.is_contiguous():
@@ -30,8 +30,8 @@ def _need(t, name: str, dtype, shape, dense: bool = True) -> None:
 
 def _need_rng(rng) -> None:
     import torch
-    if rng is not None and (rng.dtype is not torch.int64 or rng.numel() != 2
-                            or not rng.is_contiguous() or not rng.is_cuda):
+    if (rng.dtype is not torch.int64 or rng.numel() != 2 or not rng.is_contiguous()
+            or not rng.is_cuda):
         raise ValueError("rng: need a device int64 tensor [seed, offset]")
 
 
@@ -49,36 +49,43 @@ class Attention:
         self.lse_shape = (batch, heads, q_len)
         self.desc = L.AttnDesc(batch, q_len, kv_len, heads, kv_heads, head_dim, code, int(causal),
                                1.0 / math.sqrt(head_dim) if scale is None else scale, dropout)
-        self.layout = None
+        self.form = None
+        self.itype, self.ftype = torch.int32, torch.float32
         self.fwd_bytes, self.bwd_bytes = L.petra_attn_query(self.desc)
         self.ws_bytes = max(self.fwd_bytes, self.bwd_bytes)
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
 
     def _lay(self, q, k, v, o, lse, q_lens, kv_lens, rng) -> None:
-        """Checks the tensors and puts their strides into the description."""
-        import torch
+        """Checks the tensors and puts their strides into the description.  What was checked
+        last (types, shapes and strides) is not checked again."""
+        form = (q.shape, k.shape, v.shape, o.shape, lse.shape, q.stride(), k.stride(), v.stride(),
+                o.stride(), lse.stride(), q.dtype, k.dtype, v.dtype, o.dtype, lse.dtype, q.is_cuda,
+                k.is_cuda, v.is_cuda, o.is_cuda, lse.is_cuda)
+        if form != self.form:
+            self._check(q, k, v, o, lse)
+            self.form = form
+        for t, name in ((q_lens, "q_lens"), (kv_lens, "kv_lens")):
+            if t is not None:
+                _need(t, name, self.itype, self.q_shape[:1])
+        if rng is not None:
+            _need_rng(rng)
+
+    def _check(self, q, k, v, o, lse) -> None:
+        self.form = None
         for t, name, shape in ((q, "q", self.q_shape), (k, "k", self.kv_shape),
                                (v, "v", self.kv_shape), (o, "o", self.q_shape)):
             _need(t, name, self.tdtype, shape, dense=False)
-        layout = (q.stride(), k.stride(), v.stride(), o.stride())
-        if layout != self.layout:
-            for t, name in ((q, "q"), (k, "k"), (v, "v"), (o, "o")):
-                st = t.stride()
-                if st[3] != 1 and t.shape[3] > 1:
-                    raise ValueError(f"{name}: channels must be contiguous, got strides {st}")
-                # the stride of a dimension of one means nothing
-                st = tuple(s if n > 1 else 0 for s, n in zip(st[:3], t.shape[:3]))
-                # the description takes three zeros for a contiguous tensor: those of one
-                # vector that all positions share cannot be told apart from that
-                if st == (0, 0, 0) and math.prod(t.shape[:3]) > 1:
-                    raise ValueError(f"{name}: all positions share one vector")
-                setattr(self.desc, name + "_stride", (L.ctypes.c_int64 * 3)(*st))
-            self.layout = layout
-        _need(lse, "lse", torch.float32, self.lse_shape)
-        for t, name in ((q_lens, "q_lens"), (kv_lens, "kv_lens")):
-            if t is not None:
-                _need(t, name, torch.int32, (self.q_shape[0],))
-        _need_rng(rng)
+            st = t.stride()
+            if st[3] != 1 and t.shape[3] > 1:
+                raise ValueError(f"{name}: channels must be contiguous, got strides {st}")
+            # the stride of a dimension of one means nothing
+            st = tuple(s if n > 1 else 0 for s, n in zip(st[:3], t.shape[:3]))
+            # the description takes three zeros for a contiguous tensor: those of one
+            # vector that all positions share cannot be told apart from that
+            if st == (0, 0, 0) and math.prod(t.shape[:3]) > 1:
+                raise ValueError(f"{name}: all positions share one vector")
+            setattr(self.desc, name + "_stride", (L.ctypes.c_int64 * 3)(*st))
+        _need(lse, "lse", self.ftype, self.lse_shape)
 
     def forward(self, q, k, v, o, lse, q_lens=None, kv_lens=None, rng=None, stream=None) -> None:
         """Writes o [batch, q_len, heads, head_dim] and lse (fp32 [batch, heads, q_len])."""
@@ -109,7 +116,7 @@ class Coupling:
         if norm not in ("rms", "layer"):
             raise ValueError(f"norm must be 'rms' or 'layer', got {norm!r}")
         code, self.tdtype = _types(dtype)
-        self.shape = (rows, width)
+        self.shape, self.ftype = (rows, width), torch.float32
         self.desc = L.CouplingDesc(rows, rows_per_gate, width, code,
                                    L.PETRA_NORM_RMS if norm == "rms" else L.PETRA_NORM_LAYER,
                                    eps, residual_scale, dropout)
@@ -117,34 +124,36 @@ class Coupling:
         self.ws_bytes = L.petra_coupling_query(self.desc)
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
 
-    def _acts(self, **tensors) -> None:
-        for name, t in tensors.items():
+    def _check(self, acts, gates, norms, rng) -> None:
+        """acts: (name, tensor) of activations; gates and norms likewise; None is left out."""
+        for name, t in acts:
             if t is not None:
                 _need(t, name, self.tdtype, self.shape)
-
-    def _params(self, **params) -> None:
-        import torch
-        for name, p in params.items():
-            for t in p if isinstance(p, tuple) else (p,):
-                if t is not None:
-                    _need(t, name, torch.float32,
-                          (self.shape[1],) if isinstance(p, tuple) else self.gate_shape)
+        for name, t in gates:
+            if t is not None:
+                _need(t, name, self.ftype, self.gate_shape)
+        for name, p in norms:
+            if p is not None:
+                _need(p[0], name, self.ftype, self.shape[1:])
+                if p[1] is not None:
+                    _need(p[1], name, self.ftype, self.shape[1:])
+        if rng is not None:
+            _need_rng(rng)
 
     def forward(self, x, f=None, gate=None, post=None, y=None, pre=None, u=None, rng=None,
                 stream=None) -> None:
         """Writes y and, with pre, u.  Without f only u = n(x; pre)."""
-        self._acts(x=x, f=f, y=y, u=u)
-        self._params(gate=gate, post=post, pre=pre)
-        _need_rng(rng)
+        self._check((("x", x), ("f", f), ("y", y), ("u", u)), (("gate", gate),),
+                    (("post", post), ("pre", pre)), rng)
         L.petra_coupling_forward(self.desc, x, f, gate, post, pre, rng, y, u, stream)
 
     def backward(self, y, f, dy, gate, post, x, dx, df, dgate, dpost, du=None, pre=None,
                  dpre=None, rng=None, stream=None) -> None:
         """Writes x (rebuilt; may be None), dx, df and the parameters' gradients.  With f, gate,
         post and what belongs to them None: only dx and dpre."""
-        self._acts(y=y, f=f, dy=dy, du=du, x=x, dx=dx, df=df)
-        self._params(gate=gate, post=post, pre=pre, dgate=dgate, dpost=dpost, dpre=dpre)
-        _need_rng(rng)
+        self._check((("y", y), ("f", f), ("dy", dy), ("du", du), ("x", x), ("dx", dx),
+                     ("df", df)), (("gate", gate), ("dgate", dgate)),
+                    (("post", post), ("pre", pre), ("dpost", dpost), ("dpre", dpre)), rng)
         L.petra_coupling_backward(self.desc, y, f, dy, du, gate, post, pre, rng, x, dx, df, dgate,
                                   dpost, dpre, self.workspace, self.ws_bytes, stream)
 
@@ -154,10 +163,9 @@ def dropout(x, y, p: float, rng, residual=None, alpha: float = 1.0, stream=None)
     import torch
     if x.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError(f"x: need bfloat16 or float32, got {x.dtype}")
-    shape = tuple(x.shape)
     for t, name in ((x, "x"), (y, "y"), (residual, "residual")):
         if t is not None:
-            _need(t, name, x.dtype, shape)
+            _need(t, name, x.dtype, x.shape)
     _need_rng(rng)
     L.petra_dropout(x.numel(), L.PETRA_BF16 if x.dtype is torch.bfloat16 else L.PETRA_FP32, p,
                     alpha, x, residual, rng, y, stream)
