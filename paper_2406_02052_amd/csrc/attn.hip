@@ -196,6 +196,18 @@ __device__ __forceinline__ void stage_floats(const float* from, int bytes, float
                ::"s"(to), "v"((threadIdx.x & 63) * 4), "s"(r) : "memory");
 }
 
+// Runs body(t, buffer) for t0 <= t < t1 with the buffers 0 and 1 in turn.  The buffer is a constant
+// in each of the two copies: LDS addresses differ by immediates, where a variable buffer costs an
+// addition for every operand read.
+template <int N> struct Const { static constexpr int value = N; };
+template <typename F>
+__device__ __forceinline__ void in_turn(int t0, int t1, F body) {
+  for (int t = t0; t < t1; t += 2) {
+    body(t, Const<0>{});
+    if (t + 1 < t1) body(t + 1, Const<1>{});
+  }
+}
+
 // What this workgroup works on: (batch row, key head), split, tile.  Splits and heads run
 // fastest: workgroups go to the 8 XCDs in turn, so that with a multiple of 8 heads each XCD's
 // L2 has the keys of its own (2 x 4096 causal tokens, 16 heads: 165 us, 204 with the tiles
@@ -294,7 +306,7 @@ __device__ __forceinline__ void store_row(T* p, const f32x16_t (&acc)[DP / 32], 
 
 // WR waves side by side over rows (32 NT each), WK over keys (KB blocks of 32 each in a tile).
 template <typename T, int DP, int WR, int WK, int NT, int KB, bool DROP>
-__global__ __launch_bounds__(64 * WR * WK, (NT * DP * sizeof(T) > 256 ? 1 : 2)) void attn_forward_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * WR * WK, (NT * DP * sizeof(T) > 256 ? 1 : sizeof(T) * DP == 256 && KB == 1 && WR == 4 ? 3 : 2)) void attn_forward_kernel(AttnArgs a) {
   using Tl = Tile<T, DP>;
   constexpr int THREADS = 64 * WR * WK, ROWS = 32 * NT * WR, KT = 32 * KB * WK;
   constexpr int TILE_BYTES = KT * Tl::ROW_BYTES;
@@ -351,16 +363,17 @@ __global__ __launch_bounds__(64 * WR * WK, (NT * DP * sizeof(T) > 256 ? 1 : 2)) 
   Stager<T, DP, KT, THREADS> sk, sv;
   sk.keys(a.k_stride[1], a.dim);
   sv.keys(a.v_stride[1], a.dim);
-  auto stage = [&](int t) {
-    char* const to = lds + (t & 1) * 2 * TILE_BYTES;
+  auto stage = [&](int t, int buffer) {
+    char* const to = lds + buffer * 2 * TILE_BYTES;
     sk.load_keys(kb, a.k_stride[1], t * KT, end, a.dim, to);
     sv.load_keys(vb, a.v_stride[1], t * KT, end, a.dim, to + TILE_BYTES);
   };
-  if (t0 < t1) stage(t0);
-  for (int t = t0; t < t1; ++t) {
+  if (t0 < t1) stage(t0, 0);
+  in_turn(t0, t1, [&](int t, auto buffer) {
+    constexpr int B = decltype(buffer)::value;
     arrived();
-    if (t + 1 < t1) stage(t + 1);
-    char* const kt = lds + (t & 1) * 2 * TILE_BYTES;
+    if (t + 1 < t1) stage(t + 1, 1 - B);
+    char* const kt = lds + B * 2 * TILE_BYTES;
     char* const vt = kt + TILE_BYTES;
     const int at0 = wk * 32 * KB;          // this wave's keys in the tile
     const int key0 = t * KT + at0;
@@ -446,7 +459,7 @@ __global__ __launch_bounds__(64 * WR * WK, (NT * DP * sizeof(T) > 256 ? 1 : 2)) 
         }
       }
     }
-  }
+  });
 #pragma unroll
   for (int n = 0; n < NT; ++n) sum[n] = sum_halves(sum[n]);
 
@@ -702,10 +715,11 @@ __global__ __launch_bounds__(64 * WR, (DP * sizeof(T) > 256 ? 1 : 2)) void attn_
   f32x16_t acc[DP / 32];
 #pragma unroll
   for (int m = 0; m < DP / 32; ++m) zero(acc[m]);
-  for (int t = t0; t < t1; ++t) {
+  in_turn(t0, t1, [&](int t, auto buffer) {
+    constexpr int B = decltype(buffer)::value;
     arrived();
-    if (t + 1 < t1) stage(t + 1, (t + 1 - t0) & 1);
-    char* const kt = lds + ((t - t0) & 1) * 2 * TILE_BYTES;
+    if (t + 1 < t1) stage(t + 1, 1 - B);
+    char* const kt = lds + B * 2 * TILE_BYTES;
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
       f32x16_t s, dp;
@@ -721,7 +735,7 @@ __global__ __launch_bounds__(64 * WR, (DP * sizeof(T) > 256 ? 1 : 2)) void attn_
           acc[d] = mfma32(Tl::across(kt, 32 * b + 16 * k16, 32 * d, lane), p, acc[d]);
       }
     }
-  }
+  });
   if (!in_q) return;
   const float f = limit > 0 ? a.scale : 0.f;
   if (a.splits > 1)
@@ -956,7 +970,7 @@ void forward_by(AttnArgs& a, const AttnPlan& p, hipStream_t s) {
   if (p.row_tile == 32)
     attn_forward_kernel<T, DP, 1, 2, 1, 1, DROP><<<grid, 128, 0, s>>>(a);
   else
-    attn_forward_kernel<T, DP, 4, 1, 1, Shape<T>::KB, DROP><<<grid, 256, 0, s>>>(a);
+    attn_forward_kernel<T, DP, 4, 1, 1, DP == 128 ? 1 : Shape<T>::KB, DROP><<<grid, 256, 0, s>>>(a);
   if (a.splits > 1)
     attn_join_kernel<T, DP><<<static_cast<unsigned>(ceil_div(static_cast<int64_t>(rows) * bh, 4)), 256, 0, s>>>(a);
 }
