@@ -507,12 +507,13 @@ __global__ __launch_bounds__(64 * WR * WK, (NT * DP * sizeof(T) > 256 ? 1 : size
     const int row = wave0 + 32 * n + (lane & 31);
     if (row >= rows) continue;
     if (a.splits > 1) {
-      // [split][batch x key heads][rows][DP], and the statistics as [..][rows][2]
+      // [split][batch x key heads][rows][DP], and the statistics as [..][rows][2]; nothing for a row without keys
+      if (limit[n] == 0) continue;
       const int64_t at_part = (static_cast<int64_t>(split) * a.batch * a.kv_heads + bh) * rows + row;
       store_row<float, DP>(a.part + at_part * DP, acc[n], 1.f, h, DP);
-      if (h == 0) {   // a row without keys: as if it had met none
-        a.part_ml[at_part * 2] = limit[n] > 0 ? top[n] : -INFINITY;
-        a.part_ml[at_part * 2 + 1] = limit[n] > 0 ? sum[n] : 0.f;
+      if (h == 0) {
+        a.part_ml[at_part * 2] = top[n];
+        a.part_ml[at_part * 2 + 1] = sum[n];
       }
       continue;
     }
@@ -537,29 +538,44 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   const int64_t step = static_cast<int64_t>(a.batch) * a.kv_heads * rows;
   if (item >= step) return;
   const int bh = static_cast<int>(item / rows), row = static_cast<int>(item - static_cast<int64_t>(bh) * rows);
-  const int b = bh / a.kv_heads, kvh = bh - b * a.kv_heads;
+  const Where w = where(a, bh);
+  const int token = row / a.group, head = w.kvh * a.group + row - token * a.group;
+  const bool keys = seen(a, w, token) > 0;
+  const int g = lane / WIDE, c = (lane - g * WIDE) * 4;
+  const float* const part = a.part + item * DP + c;
+  // the first splits' values are asked for with the statistics
+  constexpr int AHEAD = 4;
+  float4 v[AHEAD] = {};
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (keys && g < GROUPS && i * GROUPS + g < a.splits)
+      v[i] = *reinterpret_cast<const float4*>(part + (i * GROUPS + g) * step * DP);
   float2 ml = make_float2(-INFINITY, 0.f);
-  if (lane < a.splits) ml = *reinterpret_cast<const float2*>(a.part_ml + (item + lane * step) * 2);
+  if (keys && lane < a.splits) ml = *reinterpret_cast<const float2*>(a.part_ml + (item + lane * step) * 2);
   float top = ml.x;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+  for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+  top = fmaxf(top, __shfl_xor(top, 16, 64));
+  top = max_halves(top);
   const float f = ml.x == -INFINITY ? 0.f : exp2_((ml.x - top) * a.scale_log2);
-  float sum = f * ml.y;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
-  const int g = lane / WIDE, c = (lane - g * WIDE) * 4;
+  const float sum = sum_halves(sum_quarters(sum16(f * ml.y)));
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int s0 = 0; s0 < a.splits; s0 += GROUPS) {
-    const int s = s0 + g;
-    const float w = __shfl(f, s < MOST_SPLITS ? s : 0, 64);
-    if (g < GROUPS && s < a.splits && w > 0.f) {
-      const float4 v = *reinterpret_cast<const float4*>(a.part + (item + s * step) * DP + c);
-      acc.x = fmaf(v.x, w, acc.x);
-      acc.y = fmaf(v.y, w, acc.y);
-      acc.z = fmaf(v.z, w, acc.z);
-      acc.w = fmaf(v.w, w, acc.w);
+  auto add = [&](int s, const float4& x) {
+    const float f_s = __shfl(f, s < MOST_SPLITS ? s : 0, 64);
+    if (g < GROUPS && s < a.splits && f_s > 0.f) {
+      acc.x = fmaf(x.x, f_s, acc.x);
+      acc.y = fmaf(x.y, f_s, acc.y);
+      acc.z = fmaf(x.z, f_s, acc.z);
+      acc.w = fmaf(x.w, f_s, acc.w);
     }
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) add(i * GROUPS + g, v[i]);
+#pragma unroll 4
+  for (int s0 = AHEAD * GROUPS; s0 < a.splits; s0 += GROUPS) {
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (keys && g < GROUPS && s0 + g < a.splits) x = *reinterpret_cast<const float4*>(part + (s0 + g) * step * DP);
+    add(s0 + g, x);
   }
 #pragma unroll
   for (int n = GROUPS / 2; n >= 1; n >>= 1) {
@@ -568,18 +584,73 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
     acc.z += __shfl_down(acc.z, n * WIDE, 64);
     acc.w += __shfl_down(acc.w, n * WIDE, 64);
   }
-  const int token = row / a.group, head = kvh * a.group + row - token * a.group;
   const bool any = sum > 0.f || sum != sum;
   const float n = any ? a.inv_keep / sum : 0.f;
   if (lane < WIDE && c < a.dim) {
-    T* const o = at<T>(a.out, a.o_stride, b, token, head) + c;
+    T* const o = at<T>(a.out, a.o_stride, w.b, token, head) + c;
     if constexpr (sizeof(T) == 2)
       *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(acc.x * n, acc.y * n), pack_bf16x2(acc.z * n, acc.w * n));
     else
       *reinterpret_cast<float4*>(o) = make_float4(acc.x * n, acc.y * n, acc.z * n, acc.w * n);
   }
   if (lane == 0)
-    a.lse[(static_cast<int64_t>(b) * a.heads + head) * a.q_len + token] =
+    a.lse[(static_cast<int64_t>(w.b) * a.heads + head) * a.q_len + token] =
+        any ? fmaf(top, a.scale, __builtin_amdgcn_logf(sum) * LN2) : -INFINITY;
+}
+
+// The same for up to FEW_SPLITS splits, 4 channels a thread, which takes the row's statistics itself: the
+// exchange between lanes above costs more than reading a few of them again (30000 rows of 80 channels in
+// 3 splits: 15 us against 7).
+constexpr int FEW_SPLITS = 8;
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a) {
+  constexpr int WIDE = DP / 4;
+  const int rows = a.q_len * a.group;
+  const int64_t step = static_cast<int64_t>(a.batch) * a.kv_heads * rows;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  const int64_t item = i / WIDE;
+  if (item >= step) return;
+  const int c = static_cast<int>(i - item * WIDE) * 4;
+  const int bh = static_cast<int>(item / rows), row = static_cast<int>(item - static_cast<int64_t>(bh) * rows);
+  const Where w = where(a, bh);
+  const int token = row / a.group, head = w.kvh * a.group + row - token * a.group;
+  float top = -INFINITY, sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (seen(a, w, token) > 0) {
+    float2 ml[FEW_SPLITS];
+    float4 v[FEW_SPLITS];
+#pragma unroll
+    for (int s = 0; s < FEW_SPLITS; ++s) {
+      ml[s] = make_float2(-INFINITY, 0.f);
+      if (s < a.splits) {
+        ml[s] = *reinterpret_cast<const float2*>(a.part_ml + (item + s * step) * 2);
+        v[s] = *reinterpret_cast<const float4*>(a.part + (item + s * step) * DP + c);
+        top = fmaxf(top, ml[s].x);
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < FEW_SPLITS; ++s) {
+      if (s >= a.splits || ml[s].x == -INFINITY) continue;
+      const float f = exp2_((ml[s].x - top) * a.scale_log2);
+      sum = fmaf(ml[s].y, f, sum);
+      acc.x = fmaf(v[s].x, f, acc.x);
+      acc.y = fmaf(v[s].y, f, acc.y);
+      acc.z = fmaf(v[s].z, f, acc.z);
+      acc.w = fmaf(v[s].w, f, acc.w);
+    }
+  }
+  const bool any = sum > 0.f || sum != sum;
+  const float n = any ? a.inv_keep / sum : 0.f;
+  if (c < a.dim) {
+    T* const o = at<T>(a.out, a.o_stride, w.b, token, head) + c;
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(acc.x * n, acc.y * n), pack_bf16x2(acc.z * n, acc.w * n));
+    else
+      *reinterpret_cast<float4*>(o) = make_float4(acc.x * n, acc.y * n, acc.z * n, acc.w * n);
+  }
+  if (c == 0)
+    a.lse[(static_cast<int64_t>(w.b) * a.heads + head) * a.q_len + token] =
         any ? fmaf(top, a.scale, __builtin_amdgcn_logf(sum) * LN2) : -INFINITY;
 }
 
@@ -738,10 +809,12 @@ __global__ __launch_bounds__(64 * WR, (DP * sizeof(T) > 256 ? 1 : 2)) void attn_
   });
   if (!in_q) return;
   const float f = limit > 0 ? a.scale : 0.f;
-  if (a.splits > 1)
-    store_row<float, DP>(a.part + ((static_cast<int64_t>(split) * a.batch * a.kv_heads + bh) * rows + row) * DP, acc, f, h, DP);
-  else
+  if (a.splits > 1) {
+    if (live)
+      store_row<float, DP>(a.part + ((static_cast<int64_t>(split) * a.batch * a.kv_heads + bh) * rows + row) * DP, acc, f, h, DP);
+  } else {
     store_row<T, DP>(at<T>(a.dq, a.q_stride, w.b, token, head), acc, f, h, a.dim);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -757,7 +830,7 @@ __global__ __launch_bounds__(64 * WC, (DP * sizeof(T) > 128 ? 1 : 2)) void attn_
   constexpr int THREADS = 64 * WC, KEYS = 32 * WC, RT = 32 * RB;
   constexpr int TILE_BYTES = RT * Tl::ROW_BYTES, STAT_BYTES = 512;
   constexpr int BUFFER = 2 * TILE_BYTES + STAT_BYTES;
-  __shared__ __attribute__((aligned(16))) char lds[2 * BUFFER + (DROP ? WC * 32 * 4 : 0)];
+  __shared__ __attribute__((aligned(16))) char lds[2 * BUFFER];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const Item item = work_item(a, false);
   const int bh = item.bh, split = item.split, tile = item.tile;
@@ -826,7 +899,7 @@ __global__ __launch_bounds__(64 * WC, (DP * sizeof(T) > 128 ? 1 : 2)) void attn_
         const int r = row0 + (lane & 31);
         const int token = r / a.group, head = w.kvh * a.group + r - token * a.group;
         const int64_t drop_row = (static_cast<int64_t>(w.b) * a.heads + head) * a.q_len + token;
-        uint32_t* const turn = reinterpret_cast<uint32_t*>(lds + 2 * BUFFER) + wave * 32;
+        int turned = 0;   // lane n < 32: the bits of key n
 #pragma unroll
         for (int k16 = 0; k16 < 2; ++k16) {
           uint32_t bits[4];
@@ -835,13 +908,12 @@ __global__ __launch_bounds__(64 * WC, (DP * sizeof(T) > 128 ? 1 : 2)) void attn_
           for (int j = 0; j < 8; ++j) {
             const uint64_t m = __ballot(kept(bits, j, a.cut));
             const int n = 16 * k16 + 8 * (j >> 2) + (j & 3);   // key of the lower half
-            if (lane == 0) turn[n] = static_cast<uint32_t>(m);
-            if (lane == 32) turn[n + 4] = static_cast<uint32_t>(m >> 32);
+            // (two wait states after the compare that wrote m)
+            asm("s_nop 1\n\tv_writelane_b32 %0, %1, %3\n\tv_writelane_b32 %0, %2, %4"
+                : "+v"(turned) : "s"(static_cast<int>(m)), "s"(static_cast<int>(m >> 32)), "i"(n), "i"(n + 4));
           }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        keep = turn[lane & 31];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        keep = __builtin_amdgcn_permlane32_swap(turned, turned, false, false)[0];   // the lower half's, in both
         __builtin_amdgcn_sched_barrier(0);   // before the products: their registers are not yet in use
       }
       f32x16_t s, dp;
@@ -911,6 +983,7 @@ __global__ __launch_bounds__(64 * WC, (DP * sizeof(T) > 128 ? 1 : 2)) void attn_
   }
   if (a.splits > 1) {
     // [dk, dv][split][batch x key heads][keys][DP]
+    if (!live) return;
     const int64_t bhs = static_cast<int64_t>(a.batch) * a.kv_heads;
     float* const to = a.part + ((split * bhs + bh) * a.kv_len + key) * DP;
     store_row<float, DP>(to, dk, a.scale, h, DP);
@@ -926,6 +999,7 @@ struct SumArgs {
   const float* part;
   void* out;
   int64_t stride[3];
+  const int32_t* lens;   // of the rows' tokens: those past them have no partial results
   int64_t items, step;   // rows x DP / 4, elements between splits
   int rows, splits, kv_heads, group, dim;
 };
@@ -938,13 +1012,15 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(SumArgs a0, SumArgs a1) {
   const int64_t r = i / (DP / 4);
   const int d = static_cast<int>(i - r * (DP / 4)) * 4;
   if (d >= a.dim) return;
-  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int n = 0; n < a.splits; ++n) {
-    const float4 v = *reinterpret_cast<const float4*>(a.part + n * a.step + r * DP + d);
-    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-  }
   const int bh = static_cast<int>(r / a.rows), row = static_cast<int>(r - static_cast<int64_t>(bh) * a.rows);
   const int b = bh / a.kv_heads, kvh = bh - b * a.kv_heads, token = row / a.group;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (a.lens == nullptr || token < a.lens[b])
+#pragma unroll 4
+    for (int n = 0; n < a.splits; ++n) {
+      const float4 v = *reinterpret_cast<const float4*>(a.part + n * a.step + r * DP + d);
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
   T* const to = at<T>(a.out, a.stride, b, token, kvh * a.group + row - token * a.group) + d;
   if constexpr (sizeof(T) == 2)
     *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
@@ -969,36 +1045,45 @@ void forward_by(AttnArgs& a, const AttnPlan& p, hipStream_t s) {
   const unsigned grid = static_cast<unsigned>(a.tiles) * bh * a.splits;
   if (p.row_tile == 32)
     attn_forward_kernel<T, DP, 1, 2, 1, 1, DROP><<<grid, 128, 0, s>>>(a);
+  else if (p.row_tile == 64)
+    attn_forward_kernel<T, DP, 2, 1, 1, Shape<T>::KB, DROP><<<grid, 128, 0, s>>>(a);
   else
     attn_forward_kernel<T, DP, 4, 1, 1, DP == 128 ? 1 : Shape<T>::KB, DROP><<<grid, 256, 0, s>>>(a);
-  if (a.splits > 1)
-    attn_join_kernel<T, DP><<<static_cast<unsigned>(ceil_div(static_cast<int64_t>(rows) * bh, 4)), 256, 0, s>>>(a);
+  const int64_t out = static_cast<int64_t>(rows) * bh;
+  if (a.splits > FEW_SPLITS)
+    attn_join_kernel<T, DP><<<static_cast<unsigned>(ceil_div(out, 4)), 256, 0, s>>>(a);
+  else if (a.splits > 1)
+    attn_join_few_kernel<T, DP><<<static_cast<unsigned>(ceil_div(out * (DP / 4), 256)), 256, 0, s>>>(a);
 }
 
 template <typename T, int DP, bool DROP>
 void backward_by(AttnArgs& a, const AttnPlan& p, hipStream_t s) {
   const int rows = a.q_len * a.group, bh = a.batch * a.kv_heads;
-  auto sum = [&](void* out, const int64_t (&st)[3], int n, int splits, int group) {
-    SumArgs r{a.part, out, {st[0], st[1], st[2]}, static_cast<int64_t>(bh) * n * (DP / 4),
+  auto sum = [&](void* out, const int64_t (&st)[3], const int32_t* lens, int n, int splits, int group) {
+    SumArgs r{a.part, out, {st[0], st[1], st[2]}, lens, static_cast<int64_t>(bh) * n * (DP / 4),
               static_cast<int64_t>(bh) * n * DP, n, splits, a.kv_heads, group, a.dim};
     return r;
   };
   if (rows > 0) {
-    a.tiles = (rows + 127) / 128;
+    a.tiles = static_cast<int>(ceil_div(rows, p.dq_tile));
     a.splits = p.dq_splits;
-    attn_dq_kernel<T, DP, 4, Shape<T>::KB, DROP><<<static_cast<unsigned>(a.tiles) * bh * a.splits, 256, 0, s>>>(a);
+    const unsigned grid = static_cast<unsigned>(a.tiles) * bh * a.splits;
+    if (p.dq_tile == 64) attn_dq_kernel<T, DP, 2, Shape<T>::KB, DROP><<<grid, 128, 0, s>>>(a);
+    else attn_dq_kernel<T, DP, 4, Shape<T>::KB, DROP><<<grid, 256, 0, s>>>(a);
     if (a.splits > 1) {
-      const SumArgs r = sum(a.dq, a.q_stride, rows, a.splits, a.group);
+      const SumArgs r = sum(a.dq, a.q_stride, a.q_lens, rows, a.splits, a.group);
       attn_sum_kernel<T, DP><<<static_cast<unsigned>(ceil_div(r.items, 256)), 256, 0, s>>>(r, r);
     }
   }
   if (a.kv_len > 0) {
-    a.tiles = (a.kv_len + 127) / 128;
+    a.tiles = static_cast<int>(ceil_div(a.kv_len, p.key_tile));
     a.splits = p.dkv_splits;
-    attn_dkv_kernel<T, DP, 4, Shape<T>::KB, DROP><<<static_cast<unsigned>(a.tiles) * bh * a.splits, 256, 0, s>>>(a);
+    const unsigned grid = static_cast<unsigned>(a.tiles) * bh * a.splits;
+    if (p.key_tile == 64) attn_dkv_kernel<T, DP, 2, Shape<T>::KB, DROP><<<grid, 128, 0, s>>>(a);
+    else attn_dkv_kernel<T, DP, 4, Shape<T>::KB, DROP><<<grid, 256, 0, s>>>(a);
     if (a.splits > 1) {
-      const SumArgs rk = sum(a.dk, a.k_stride, a.kv_len, a.splits, 1);
-      SumArgs rv = sum(a.dv, a.v_stride, a.kv_len, a.splits, 1);
+      const SumArgs rk = sum(a.dk, a.k_stride, a.kv_lens, a.kv_len, a.splits, 1);
+      SumArgs rv = sum(a.dv, a.v_stride, a.kv_lens, a.kv_len, a.splits, 1);
       rv.part += a.splits * rv.step;
       attn_sum_kernel<T, DP><<<dim3(static_cast<unsigned>(ceil_div(rk.items, 256)), 2), 256, 0, s>>>(rk, rv);
     }
@@ -1037,12 +1122,16 @@ int splits_for(int64_t blocks, int64_t slots, int64_t length, int64_t least) {
 AttnPlan attn_plan(const AttnArgs& a, int) {
   AttnPlan p{};
   const int64_t rows = static_cast<int64_t>(a.q_len) * a.group, bh = static_cast<int64_t>(a.batch) * a.kv_heads;
-  p.row_tile = rows <= 32 ? 32 : 128;
+  // 128 rows or keys a workgroup share what it brings to LDS; more small workgroups in place of splits
+  // are slower (5 x 1000 ragged tokens: dk and dv 72 us by 64 keys, 46 by 128), unless 64 is all there is
+  p.row_tile = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   p.splits = splits_for(ceil_div(rows, p.row_tile) * bh, p.row_tile == 32 ? 512 : 256, a.kv_len, 128);
+  p.dq_tile = rows <= 64 ? 64 : 128;
+  p.key_tile = a.kv_len <= 64 ? 64 : 128;
   const size_t row = static_cast<size_t>(padded(a.dim)) * 4;
   p.fwd_bytes = p.splits > 1 ? p.splits * bh * rows * (row + 8) : 0;
-  p.dq_splits = splits_for(ceil_div(rows, 128) * bh, 256, a.kv_len, 256);
-  p.dkv_splits = splits_for(ceil_div(a.kv_len, 128) * bh, 256, rows, 256);
+  p.dq_splits = splits_for(ceil_div(rows, p.dq_tile) * bh, 256, a.kv_len, 256);
+  p.dkv_splits = splits_for(ceil_div(a.kv_len, p.key_tile) * bh, 256, rows, 256);
   const size_t dq = p.dq_splits > 1 ? p.dq_splits * bh * rows * row : 0;
   const size_t dkv = p.dkv_splits > 1 ? 2 * p.dkv_splits * bh * a.kv_len * row : 0;
   p.stat_bytes = 2 * ((static_cast<size_t>(bh) * rows * 4 + 15) / 16 * 16);

@@ -60,7 +60,7 @@ struct AttnArgs {
 struct AttnPlan {
   int row_tile, splits;            // forward
   size_t fwd_bytes;
-  int dq_splits, dkv_splits;       // backward
+  int dq_tile, key_tile, dq_splits, dkv_splits;   // backward
   size_t stat_bytes, bwd_bytes;
 };
 
