@@ -304,11 +304,16 @@ __device__ __forceinline__ void store_row(T* p, const f32x16_t (&acc)[DP / 32], 
 // forward
 // ---------------------------------------------------------------------------
 
-// WR waves side by side over rows (32 NT each), WK over keys (KB blocks of 32 each in a tile).
-template <typename T, int DP, int WR, int WK, int NT, int KB, bool DROP>
-__global__ __launch_bounds__(64 * WR * WK, (NT * DP * sizeof(T) > 256 ? 1 : sizeof(T) * DP == 256 && KB == 1 && WR == 4 ? 3 : 2)) void attn_forward_kernel(AttnArgs a) {
+// Bound by the exponentials beside the products: a block of 32 x 32 pairs of 128 channels has 512 cycles of
+// matrix instructions a wave and about 640 of other vector ones, which overlap between waves only.  With 128
+// channels of bf16 three waves a SIMD, of 32 keys at a time, take 151 us for 2 x 4096 causal tokens and 16
+// heads, two waves of 64 keys 162; buffers at constant addresses then save 7.  Two blocks of rows a wave,
+// which halve the reads of LDS, leave one wave a SIMD: 241 us.
+// WR waves side by side over rows (32 each), WK over keys (KB blocks of 32 each in a tile).
+template <typename T, int DP, int WR, int WK, int KB, bool DROP>
+__global__ __launch_bounds__(64 * WR * WK, (DP * sizeof(T) > 256 ? 1 : DP * sizeof(T) == 256 && KB == 1 && WR == 4 ? 3 : 2)) void attn_forward_kernel(AttnArgs a) {
   using Tl = Tile<T, DP>;
-  constexpr int THREADS = 64 * WR * WK, ROWS = 32 * NT * WR, KT = 32 * KB * WK;
+  constexpr int THREADS = 64 * WR * WK, ROWS = 32 * WR, KT = 32 * KB * WK;
   constexpr int TILE_BYTES = KT * Tl::ROW_BYTES;
   constexpr int JOIN_BYTES = WK > 1 ? WK * ROWS * (DP + 2) * 4 : 0;
   __shared__ __attribute__((aligned(16))) char lds[4 * TILE_BYTES > JOIN_BYTES ? 4 * TILE_BYTES : JOIN_BYTES];
@@ -318,18 +323,13 @@ __global__ __launch_bounds__(64 * WR * WK, (NT * DP * sizeof(T) > 256 ? 1 : size
   const int bh = item.bh, split = item.split, tile = item.tile;
   const Where w = where(a, bh);
   const int rows = a.q_len * a.group;
-  const int row0 = tile * ROWS, wave0 = row0 + wr * 32 * NT;
-  int token[NT], head[NT], limit[NT];
-  Frag<T> q[NT][Tl::STEPS];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int row = wave0 + 32 * n + (lane & 31);
-    token[n] = row / a.group;
-    head[n] = w.kvh * a.group + row - token[n] * a.group;
-    const bool in_q = row < rows;
-    limit[n] = in_q ? seen(a, w, token[n]) : 0;
-    load_row<T, DP>(at<T>(a.q, a.q_stride, w.b, in_q ? token[n] : 0, head[n]), in_q && token[n] < w.q_len, h, a.dim, q[n]);
-  }
+  const int row0 = tile * ROWS, wave0 = row0 + wr * 32;
+  const int row = wave0 + (lane & 31);
+  const int token = row / a.group, head = w.kvh * a.group + row - token * a.group;
+  const bool in_q = row < rows;
+  const int limit = in_q ? seen(a, w, token) : 0;
+  Frag<T> q[Tl::STEPS];
+  load_row<T, DP>(at<T>(a.q, a.q_stride, w.b, in_q ? token : 0, head), in_q && token < w.q_len, h, a.dim, q);
 
   // keys that any row of the workgroup sees, and that every row of the wave sees
   const int last_row = (row0 + ROWS < rows ? row0 + ROWS : rows) - 1;
@@ -345,18 +345,14 @@ __global__ __launch_bounds__(64 * WR * WK, (NT * DP * sizeof(T) > 256 ? 1 : size
   const int per = (tiles + a.splits - 1) / a.splits;
   const int t0 = split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
-  f32x16_t acc[NT][DP / 32];
-  float top[NT], sum[NT];
+  f32x16_t acc[DP / 32];
+  float top = -INFINITY, sum = 0.f;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    top[n] = -INFINITY;
-    sum[n] = 0.f;
-#pragma unroll
-    for (int m = 0; m < DP / 32; ++m) zero(acc[n][m]);
-  }
+  for (int m = 0; m < DP / 32; ++m) zero(acc[m]);
   const float c = a.scale_log2;
   Rng rng{};
   if (DROP) rng = load_rng(a.rng);
+  const int64_t stat = (static_cast<int64_t>(w.b) * a.heads + head) * a.q_len + token;   // of lse, and the generator's row
 
   const T* const kb = at<T>(a.k, a.k_stride, w.b, 0, w.kvh);
   const T* const vb = at<T>(a.v, a.v_stride, w.b, 0, w.kvh);
@@ -377,152 +373,119 @@ __global__ __launch_bounds__(64 * WR * WK, (NT * DP * sizeof(T) > 256 ? 1 : size
     char* const vt = kt + TILE_BYTES;
     const int at0 = wk * 32 * KB;          // this wave's keys in the tile
     const int key0 = t * KT + at0;
-    f32x16_t s[NT][KB];
+    f32x16_t s[KB];
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
+      zero(s[b]);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) zero(s[n][b]);
-#pragma unroll
-      for (int i = 0; i < Tl::STEPS; ++i) {
-        const Frag<T> k = Tl::straight(kt, at0 + 32 * b + (lane & 31), i, h);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) s[n][b] = mfma32(k, q[n][i], s[n][b]);
-      }
+      for (int i = 0; i < Tl::STEPS; ++i)
+        s[b] = mfma32(Tl::straight(kt, at0 + 32 * b + (lane & 31), i, h), q[i], s[b]);
     }
     if (key0 + 32 * KB > all) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = key0 + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3);
-            s[n][b][i] = key < limit[n] ? s[n][b][i] : -INFINITY;
-          }
-    }
-    // the running maximum moves only when some row's grew by more than 2^8: exp stays far inside fp32
-    float m[NT];
-    bool grew = false;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      m[n] = s[n][0][0];
-#pragma unroll
       for (int b = 0; b < KB; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) m[n] = fmaxf(m[n], s[n][b][i]);
-      m[n] = max_halves(m[n]);
-      grew |= fmaf(m[n], c, -8.f) > top[n] * c;
+        for (int i = 0; i < 16; ++i) {
+          const int key = key0 + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3);
+          s[b][i] = key < limit ? s[b][i] : -INFINITY;
+        }
     }
-    if (__any(grew)) {
+    // the running maximum moves only when some row's grew by more than 2^8: exp stays far inside fp32
+    float m = s[0][0];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const float to = fmaxf(top[n], m[n]);
-        const float f = to == -INFINITY ? 1.f : exp2_((top[n] - to) * c);
-        top[n] = to;
-        sum[n] *= f;
+    for (int b = 0; b < KB; ++b)
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
+      for (int i = 0; i < 16; ++i) m = fmaxf(m, s[b][i]);
+    m = max_halves(m);
+    if (__any(fmaf(m, c, -8.f) > top * c)) {
+      const float to = fmaxf(top, m);
+      const float f = to == -INFINITY ? 1.f : exp2_((top - to) * c);
+      top = to;
+      sum *= f;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[n][d][i] *= f;
-      }
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] *= f;
     }
+    const float base = top == -INFINITY ? 0.f : top * c;
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const float base = top[n] == -INFINITY ? 0.f : top[n] * c;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[n][b][i] = exp2_(fmaf(s[n][b][i], c, -base));
-          sum[n] += s[n][b][i];
-        }
+      for (int i = 0; i < 16; ++i) {
+        s[b][i] = exp2_(fmaf(s[b][i], c, -base));
+        sum += s[b][i];
       }
 #pragma unroll
       for (int k16 = 0; k16 < 2; ++k16) {
-        Frag<T> p[NT];
+        if (DROP) {
+          uint32_t bits[4];
+          drop_bits(a, rng, stat, ((key0 + 32 * b) >> 4) + k16, h, bits);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          if (DROP) {
-            uint32_t bits[4];
-            drop_bits(a, rng, (static_cast<int64_t>(w.b) * a.heads + head[n]) * a.q_len + token[n],
-                      ((key0 + 32 * b) >> 4) + k16, h, bits);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s[n][b][8 * k16 + i] = kept(bits, i, a.cut) ? s[n][b][8 * k16 + i] : 0.f;
-          }
-          operand(s[n][b], k16, p[n]);
+          for (int i = 0; i < 8; ++i) s[b][8 * k16 + i] = kept(bits, i, a.cut) ? s[b][8 * k16 + i] : 0.f;
         }
+        Frag<T> p;
+        operand(s[b], k16, p);
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d) {
-          const Frag<T> v = Tl::across(vt, at0 + 32 * b + 16 * k16, 32 * d, lane);
-#pragma unroll
-          for (int n = 0; n < NT; ++n) acc[n][d] = mfma32(v, p[n], acc[n][d]);
-        }
+        for (int d = 0; d < DP / 32; ++d)
+          acc[d] = mfma32(Tl::across(vt, at0 + 32 * b + 16 * k16, 32 * d, lane), p, acc[d]);
       }
     }
   });
-#pragma unroll
-  for (int n = 0; n < NT; ++n) sum[n] = sum_halves(sum[n]);
+  sum = sum_halves(sum);
 
   if constexpr (WK > 1) {
     // join the waves that shared the rows: statistics, then the scaled accumulators, in a fixed order
-    static_assert(WK == 1 || NT == 1, "one block of rows a wave");
     float* const stat = reinterpret_cast<float*>(lds);              // [WK][ROWS][2]
     float* const part = stat + WK * ROWS * 2;                       // [WK][ROWS][DP]
     const int at_row = wr * 32 + (lane & 31);
     __syncthreads();
     if (h == 0) {
-      stat[(wk * ROWS + at_row) * 2] = top[0];
-      stat[(wk * ROWS + at_row) * 2 + 1] = sum[0];
+      stat[(wk * ROWS + at_row) * 2] = top;
+      stat[(wk * ROWS + at_row) * 2 + 1] = sum;
     }
     __syncthreads();
     float to = -INFINITY;
 #pragma unroll
     for (int i = 0; i < WK; ++i) to = fmaxf(to, stat[(i * ROWS + at_row) * 2]);
-    const float f = to == -INFINITY ? 0.f : exp2_((top[0] - to) * c);
-    sum[0] = 0.f;
+    const float f = to == -INFINITY ? 0.f : exp2_((top - to) * c);
+    sum = 0.f;
 #pragma unroll
     for (int i = 0; i < WK; ++i) {
       const float ti = stat[(i * ROWS + at_row) * 2];
-      sum[0] += ti == -INFINITY ? 0.f : stat[(i * ROWS + at_row) * 2 + 1] * exp2_((ti - to) * c);
+      sum += ti == -INFINITY ? 0.f : stat[(i * ROWS + at_row) * 2 + 1] * exp2_((ti - to) * c);
     }
-    top[0] = to;
-    if (wk > 0) store_row<float, DP>(part + (wk * ROWS + at_row) * DP, acc[0], f, h, DP);
+    top = to;
+    if (wk > 0) store_row<float, DP>(part + (wk * ROWS + at_row) * DP, acc, f, h, DP);
     __syncthreads();
     if (wk > 0) return;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        float4 v = make_float4(acc[0][d][4 * g] * f, acc[0][d][4 * g + 1] * f, acc[0][d][4 * g + 2] * f, acc[0][d][4 * g + 3] * f);
+        float4 v = make_float4(acc[d][4 * g] * f, acc[d][4 * g + 1] * f, acc[d][4 * g + 2] * f, acc[d][4 * g + 3] * f);
 #pragma unroll
         for (int i = 1; i < WK; ++i) {
           const float4 u = *reinterpret_cast<const float4*>(part + (i * ROWS + at_row) * DP + 32 * d + 8 * g + 4 * h);
           v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
         }
-        acc[0][d][4 * g] = v.x; acc[0][d][4 * g + 1] = v.y; acc[0][d][4 * g + 2] = v.z; acc[0][d][4 * g + 3] = v.w;
+        acc[d][4 * g] = v.x; acc[d][4 * g + 1] = v.y; acc[d][4 * g + 2] = v.z; acc[d][4 * g + 3] = v.w;
       }
   }
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int row = wave0 + 32 * n + (lane & 31);
-    if (row >= rows) continue;
-    if (a.splits > 1) {
-      // [split][batch x key heads][rows][DP], and the statistics as [..][rows][2]; nothing for a row without keys
-      if (limit[n] == 0) continue;
-      const int64_t at_part = (static_cast<int64_t>(split) * a.batch * a.kv_heads + bh) * rows + row;
-      store_row<float, DP>(a.part + at_part * DP, acc[n], 1.f, h, DP);
-      if (h == 0) {
-        a.part_ml[at_part * 2] = top[n];
-        a.part_ml[at_part * 2 + 1] = sum[n];
-      }
-      continue;
+  if (row >= rows) return;
+  if (a.splits > 1) {
+    // [split][batch x key heads][rows][DP], and the statistics as [..][rows][2]; nothing for a row without keys
+    if (limit == 0) return;
+    const int64_t at_part = (static_cast<int64_t>(split) * a.batch * a.kv_heads + bh) * rows + row;
+    store_row<float, DP>(a.part + at_part * DP, acc, 1.f, h, DP);
+    if (h == 0) {
+      a.part_ml[at_part * 2] = top;
+      a.part_ml[at_part * 2 + 1] = sum;
     }
-    const bool any = limit[n] > 0 && (sum[n] > 0.f || sum[n] != sum[n]);
-    store_row<T, DP>(at<T>(a.out, a.o_stride, w.b, token[n], head[n]), acc[n], any ? a.inv_keep / sum[n] : 0.f, h, a.dim);
-    if (h == 0)
-      a.lse[(static_cast<int64_t>(w.b) * a.heads + head[n]) * a.q_len + token[n]] =
-          any ? fmaf(top[n], a.scale, __builtin_amdgcn_logf(sum[n]) * LN2) : -INFINITY;
+    return;
   }
+  const bool any = limit > 0 && (sum > 0.f || sum != sum);
+  store_row<T, DP>(at<T>(a.out, a.o_stride, w.b, token, head), acc, any ? a.inv_keep / sum : 0.f, h, a.dim);
+  if (h == 0) a.lse[stat] = any ? fmaf(top, a.scale, __builtin_amdgcn_logf(sum) * LN2) : -INFINITY;
 }
 
 // Joins the splits of one row, a wave a row: lane s takes the statistics of split s, then groups
@@ -1044,11 +1007,11 @@ void forward_by(AttnArgs& a, const AttnPlan& p, hipStream_t s) {
   a.splits = p.splits;
   const unsigned grid = static_cast<unsigned>(a.tiles) * bh * a.splits;
   if (p.row_tile == 32)
-    attn_forward_kernel<T, DP, 1, 2, 1, 1, DROP><<<grid, 128, 0, s>>>(a);
+    attn_forward_kernel<T, DP, 1, 2, 1, DROP><<<grid, 128, 0, s>>>(a);
   else if (p.row_tile == 64)
-    attn_forward_kernel<T, DP, 2, 1, 1, Shape<T>::KB, DROP><<<grid, 128, 0, s>>>(a);
+    attn_forward_kernel<T, DP, 2, 1, Shape<T>::KB, DROP><<<grid, 128, 0, s>>>(a);
   else
-    attn_forward_kernel<T, DP, 4, 1, 1, DP == 128 ? 1 : Shape<T>::KB, DROP><<<grid, 256, 0, s>>>(a);
+    attn_forward_kernel<T, DP, 4, 1, DP == 128 ? 1 : Shape<T>::KB, DROP><<<grid, 256, 0, s>>>(a);
   const int64_t out = static_cast<int64_t>(rows) * bh;
   if (a.splits > FEW_SPLITS)
     attn_join_kernel<T, DP><<<static_cast<unsigned>(ceil_div(out, 4)), 256, 0, s>>>(a);

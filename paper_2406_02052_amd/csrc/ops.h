@@ -11,6 +11,7 @@ namespace petra {
 // --- coupling ---------------------------------------------------------------
 struct CoupleArgs {
   long rows, rows_per_gate, gates;
+  long row0;                                 // forward: the launch's first row
   int width, layer;
   int has_f, has_u;                          // backward: which parts it has
   float eps, scale, inv_scale, inv_width, inv_keep;

@@ -501,7 +501,6 @@ petra_status petra_dropout(int64_t n, int32_t dtype, float p, float alpha, const
     need(n >= 0 && n < (int64_t{1} << 46), PETRA_ERR_SHAPE, "negative or too large size");
     need(std::isfinite(alpha), PETRA_ERR_INVALID_ARG, "alpha must be finite");
     const uint32_t cut = need_dropout(p, rng, true);
-    need(rng != nullptr, PETRA_ERR_INVALID_ARG, "dropout without rng");
     need_ptr(x, "x", n == 0);
     need_ptr(y, "y", n == 0);
     need_ptr(residual, "residual", n == 0 || residual == nullptr);

@@ -166,6 +166,7 @@ def dropout(x, y, p: float, rng, residual=None, alpha: float = 1.0, stream=None)
     for t, name in ((x, "x"), (y, "y"), (residual, "residual")):
         if t is not None:
             _need(t, name, x.dtype, x.shape)
-    _need_rng(rng)
+    if rng is not None:
+        _need_rng(rng)
     L.petra_dropout(x.numel(), L.PETRA_BF16 if x.dtype is torch.bfloat16 else L.PETRA_FP32, p,
                     alpha, x, residual, rng, y, stream)

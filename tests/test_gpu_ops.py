@@ -124,6 +124,13 @@ def test_attention_head_widths(dim, dtype):
     check(*attention(dtype, 1, 45, 70, 2, 1, dim, True, seed=dim), dtype)
 
 
+@pytest.mark.parametrize("heads,kv_heads", [(96, 1), (14, 2), (5, 1)])
+def test_attention_head_groups_that_divide_no_tile(heads, kv_heads):
+    print("case", heads, kv_heads, flush=True)
+    check(*attention("bf16", 2, 9, 70, heads, kv_heads, 32, True, ([9, 4], [70, 33]), poison=True), "bf16")
+    check(*attention("fp32", 1, 37, 200, heads, kv_heads, 40, True, p=0.2), "fp32")
+
+
 LENS = [([1, 70, 33], [97, 0, 64]), ([70, 70, 69], [1, 96, 97]), ([0, 5, 70], [97, 97, 2]), ([64, 65, 1], [63, 64, 65])]
 
 
@@ -461,6 +468,15 @@ def test_dropout(n, p, dtype):
     torch.cuda.synchronize()
     big = np.abs(T.dropout(x, p, RNG)) + np.abs(r)
     assert (np.abs(host(tr) - r) <= 2 * big * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -22)).all()
+
+
+def test_dropout_of_nothing_needs_no_rng():
+    from paper_2406_02052_amd import dropout
+
+    x = torch.randn(1001, device="cuda")
+    y = torch.empty_like(x)
+    dropout(x, y, 0.0, None)
+    assert torch.equal(x, y)
 
 
 def test_dropout_offsets_and_seeds_differ():
