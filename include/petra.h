@@ -421,7 +421,9 @@ petra_status petra_net_backprop_step(petra_net* net, const void* images, const i
  * Visible are the keys j < kv_lens[b], and with `causal` j <= i + kv_lens[b] -
  * q_lens[b] (the last query sees every key).  A query without visible keys, or
  * at or past q_lens[b], has o = 0, lse = -inf and takes no part in any gradient.
- * Nothing at or past the lengths is used, whatever it holds.  m is dropout's 0
+ * Nothing at or past the lengths is used, whatever it holds; keys that the
+ * causal mask alone hides from a query enter its sums times zero and have to be
+ * finite.  m is dropout's 0
  * or 1 / (share kept); its groups are, for each row (b, h, i), the keys 16 a +
  * 4 c + {0, 1, 2, 3, 8, 9, 10, 11} for c = 0, 1, in the order (b, h, i, a, c).
  *

@@ -315,7 +315,8 @@ __global__ __launch_bounds__(64 * WR * WK, (DP * sizeof(T) > 256 ? 1 : DP * size
   using Tl = Tile<T, DP>;
   constexpr int THREADS = 64 * WR * WK, ROWS = 32 * WR, KT = 32 * KB * WK;
   constexpr int TILE_BYTES = KT * Tl::ROW_BYTES;
-  constexpr int JOIN_BYTES = WK > 1 ? WK * ROWS * (DP + 2) * 4 : 0;
+  constexpr int JOIN_ROW = DP + 4;   // floats: rows 16 bytes apart in the banks
+  constexpr int JOIN_BYTES = WK > 1 ? WK * ROWS * (JOIN_ROW + 2) * 4 : 0;
   __shared__ __attribute__((aligned(16))) char lds[4 * TILE_BYTES > JOIN_BYTES ? 4 * TILE_BYTES : JOIN_BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int wr = wave % WR, wk = wave / WR;
@@ -436,7 +437,7 @@ __global__ __launch_bounds__(64 * WR * WK, (DP * sizeof(T) > 256 ? 1 : DP * size
   if constexpr (WK > 1) {
     // join the waves that shared the rows: statistics, then the scaled accumulators, in a fixed order
     float* const stat = reinterpret_cast<float*>(lds);              // [WK][ROWS][2]
-    float* const part = stat + WK * ROWS * 2;                       // [WK][ROWS][DP]
+    float* const part = stat + WK * ROWS * 2;                       // [WK][ROWS][JOIN_ROW]
     const int at_row = wr * 32 + (lane & 31);
     __syncthreads();
     if (h == 0) {
@@ -455,7 +456,7 @@ __global__ __launch_bounds__(64 * WR * WK, (DP * sizeof(T) > 256 ? 1 : DP * size
       sum += ti == -INFINITY ? 0.f : stat[(i * ROWS + at_row) * 2 + 1] * exp2_((ti - to) * c);
     }
     top = to;
-    if (wk > 0) store_row<float, DP>(part + (wk * ROWS + at_row) * DP, acc, f, h, DP);
+    if (wk > 0) store_row<float, DP>(part + (wk * ROWS + at_row) * JOIN_ROW, acc, f, h, DP);
     __syncthreads();
     if (wk > 0) return;
 #pragma unroll
@@ -465,7 +466,7 @@ __global__ __launch_bounds__(64 * WR * WK, (DP * sizeof(T) > 256 ? 1 : DP * size
         float4 v = make_float4(acc[d][4 * g] * f, acc[d][4 * g + 1] * f, acc[d][4 * g + 2] * f, acc[d][4 * g + 3] * f);
 #pragma unroll
         for (int i = 1; i < WK; ++i) {
-          const float4 u = *reinterpret_cast<const float4*>(part + (i * ROWS + at_row) * DP + 32 * d + 8 * g + 4 * h);
+          const float4 u = *reinterpret_cast<const float4*>(part + (i * ROWS + at_row) * JOIN_ROW + 32 * d + 8 * g + 4 * h);
           v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
         }
         acc[d][4 * g] = v.x; acc[d][4 * g + 1] = v.y; acc[d][4 * g + 2] = v.z; acc[d][4 * g + 3] = v.w;
@@ -621,6 +622,9 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a) {
 // backward: query gradient
 // ---------------------------------------------------------------------------
 
+// Three products a pair, each with one operand in registers (q, do, or what the last two left) and one from
+// LDS; two waves a SIMD.  2 x 4096 causal tokens, 16 heads of 128 over 4: 213 us, 970 TFLOP/s, matrix
+// instructions busy 60 % of the time.
 template <typename T, int DP, int WR, int KB, bool DROP>
 __global__ __launch_bounds__(64 * WR, (DP * sizeof(T) > 256 ? 1 : 2)) void attn_dq_kernel(AttnArgs a) {
   using Tl = Tile<T, DP>;
@@ -664,9 +668,10 @@ __global__ __launch_bounds__(64 * WR, (DP * sizeof(T) > 256 ? 1 : 2)) void attn_
   };
   // A row that sees at most the first tile takes D from that tile's own products: with few keys
   // p is large and o's rounding, which do . o would bring in, does not average out over them.
-  const bool few = sizeof(T) == 2 && all < KT && tiles > 0;
+  const bool few = sizeof(T) == 2 && all <= KT && tiles > 0;
   const bool few_any = sizeof(T) == 2 && tiles > 0 && (w.kv_len <= KT || (a.causal && row0 / a.group + w.kv_len - w.q_len < KT));
-  if (few_any) stage(0, 1);
+  const int few_buffer = t0 == 0 ? 0 : 1;   // the first split has that tile anyway
+  if (few_any && few_buffer == 1) stage(0, 1);
   if (t0 < t1) stage(t0, 0);
 
   Frag<T> q[Tl::STEPS], g[Tl::STEPS];
@@ -732,14 +737,13 @@ __global__ __launch_bounds__(64 * WR, (DP * sizeof(T) > 256 ? 1 : 2)) void attn_
 #pragma unroll
       for (int b = 0; b < KB; ++b) {
         f32x16_t s, dp;
-        products(lds + 2 * TILE_BYTES, b, 32 * b, s, dp);
+        products(lds + few_buffer * 2 * TILE_BYTES, b, 32 * b, s, dp);
 #pragma unroll
         for (int i = 0; i < 16; ++i) own = s[i] > 0.f ? fmaf(s[i], dp[i], own) : own;
       }
       own = sum_halves(own);
       delta = limit <= KT ? own : delta;
     }
-    __syncthreads();
   }
   if (in_q && h == 0 && split == 0) {   // for the key gradients, by row
     a.stat_lse[static_cast<int64_t>(bh) * rows + row] = lse;
@@ -786,7 +790,8 @@ __global__ __launch_bounds__(64 * WR, (DP * sizeof(T) > 256 ? 1 : 2)) void attn_
 
 // One wave a SIMD above 64 channels of bf16: its key and value rows, and their gradients, take 192
 // registers.  With the value rows in LDS and two waves a SIMD it has too few left to ask for its
-// operands early: 890 us against 356 for 2 x 4096 causal tokens, 16 heads of 128 over 4.
+// operands early: 439 us against 353 for 2 x 4096 causal tokens, 16 heads of 128 over 4, where the
+// matrix instructions are busy 40 % of the time (780 TFLOP/s).
 template <typename T, int DP, int WC, int RB, bool DROP>
 __global__ __launch_bounds__(64 * WC, (DP * sizeof(T) > 128 ? 1 : 2)) void attn_dkv_kernel(AttnArgs a) {
   using Tl = Tile<T, DP>;
