@@ -178,8 +178,8 @@ __global__ __launch_bounds__(Team<TEAM>::THREADS) void couple_forward_kernel(Cou
 // a gate a row, a row's dgate is written with the row.  The next row's tensors are
 // asked for before this one's sums, which wait for the team's waves.
 // FULL: a layer norm or a beta (the sums that only those need).
-// 4 reads and 3 writes an element: 16384 x 2048 bf16 with dropout in 112 us and 6.6 for the second
-// kernel, 4.0 TB/s; without the next row fetched ahead, and with a barrier more for each sum, 188.
+// 4 reads and 3 writes an element: 16384 x 2048 bf16 with dropout in 95 us and 4.8 for the second
+// kernel, 4.7 TB/s; without the next row fetched ahead, and with a barrier more for each sum, 188.
 template <typename T, int TEAM, bool FULL, bool DROP, bool PRE>
 __global__ __launch_bounds__(Team<TEAM>::THREADS) void couple_backward_kernel(CoupleArgs a) {
   using Tm = Team<TEAM>;
@@ -499,8 +499,10 @@ void couple_plan(CoupleArgs& a) {
   // rows that a workgroup works on at once
   const int lanes = team(a.width);
   const long teams = lanes < 256 ? 256 / lanes : 1;
-  // three workgroups of 256 lanes a CU, or as many lanes: partial sums are a row of the width for each of them
-  const long most = lanes <= 256 ? 768 : lanes == 512 ? 512 : 256;
+  // two workgroups a CU (one of 1024 lanes): partial sums are a row of the width for each of them, and a count
+  // that the 256 CUs do not share evenly ends late (16384 x 2048 bf16: 512 workgroups 95 us, 256 115, 640
+  // 115, 768 112, 1024 97 and a longer join)
+  const long most = lanes <= 512 ? 512 : 256;
   long span = (a.rows + most - 1) / most;
   span = span < 1 ? teams : (span + teams - 1) / teams * teams;
   a.gates_per_block = a.chunks_per_gate = 1;
