@@ -34,21 +34,24 @@ struct Team {
   static constexpr int WAVES = TEAM > 64 ? TEAM / 64 : 1;
   static constexpr int LDS = WAVES > 1 ? 4 * (THREADS / 64) : 1;   // floats: two sums, twice
 
+  template <int DPP>
+  static __device__ __forceinline__ float swapped(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), DPP, 0xF, 0xF, false));
+  }
+
   // Sums of N (at most 2) values over the team, in every lane.  `turn` alternates: a wave that
   // writes one half of lds has seen every wave leave it, at the barrier for the other half.
   template <int N>
   static __device__ __forceinline__ void sum(float (&x)[N], float* lds, int& turn) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if constexpr (TEAM == 8) {
-        int v = __float_as_int(x[i]);
-        x[i] += __int_as_float(__builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, false));   // [1,0,3,2]
-        v = __float_as_int(x[i]);
-        x[i] += __int_as_float(__builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, false));   // [2,3,0,1]
-        v = __float_as_int(x[i]);
-        x[i] += __int_as_float(__builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, false));  // half mirror
+      if constexpr (TEAM < 16) {
+        if constexpr (TEAM >= 2) x[i] += swapped<0xB1>(x[i]);    // [1,0,3,2]
+        if constexpr (TEAM >= 4) x[i] += swapped<0x4E>(x[i]);    // [2,3,0,1]
+        if constexpr (TEAM >= 8) x[i] += swapped<0x141>(x[i]);   // half mirror
       } else {
-        x[i] = sum_quarters(sum16(x[i]));
+        x[i] = sum16(x[i]);
+        if constexpr (TEAM >= 32) x[i] = sum_quarters(x[i]);
         if constexpr (TEAM >= 64) x[i] = sum_halves(x[i]);
       }
     }
@@ -476,15 +479,21 @@ void backward_launch(const CoupleArgs& a, hipStream_t s) {
   else backward_by<T, TEAM, false>(a, s);
 }
 
-// Lanes a row: the fewest that hold it, 8 elements each.
+// Lanes a row: the fewest powers of two that hold it, 8 elements each (2159903 x 8 bf16 with a gate a row:
+// 88 us backward, 242 by 8 lanes).
 int team(int width) {
-  return width <= 64 ? 8 : width <= 256 ? 32 : width <= 512 ? 64 : width <= 1024 ? 128 : width <= 2048 ? 256
-         : width <= 4096 ? 512 : 1024;
+  int n = 1;
+  while (8 * n < width) n *= 2;
+  return n;
 }
 
 #define PETRA_BY_WIDTH(LAUNCH, T)             \
   switch (team(a.width)) {                    \
+    case 1: LAUNCH<T, 1>(a, s); break;        \
+    case 2: LAUNCH<T, 2>(a, s); break;        \
+    case 4: LAUNCH<T, 4>(a, s); break;        \
     case 8: LAUNCH<T, 8>(a, s); break;        \
+    case 16: LAUNCH<T, 16>(a, s); break;      \
     case 32: LAUNCH<T, 32>(a, s); break;      \
     case 64: LAUNCH<T, 64>(a, s); break;      \
     case 128: LAUNCH<T, 128>(a, s); break;    \

@@ -393,7 +393,8 @@ def coupling(dtype, rows, width, norm="rms", per_gate=0, scale=1.0, p=0.0, pre=T
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("norm", ["rms", "layer"])
 @pytest.mark.parametrize("rows,width", [(1, 8), (3, 64), (33, 72), (9, 256), (5, 264), (7, 512), (70, 520), (4, 1024),
-                                        (3, 1032), (600, 48), (2, 2048), (5, 2056), (3, 4104), (2, 8192), (1500, 16)])
+                                        (3, 1032), (600, 48), (2, 2048), (5, 2056), (3, 4104), (2, 8192), (1500, 16),
+                                        (3000, 8), (1025, 24), (700, 32), (513, 128), (300, 136)])
 def test_coupling_sizes(rows, width, norm, dtype):
     print("case", rows, width, norm, dtype, flush=True)
     coupling(dtype, rows, width, norm)
