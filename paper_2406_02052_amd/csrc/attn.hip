@@ -453,7 +453,8 @@ __global__ __launch_bounds__(64 * WR * WK, (DP * sizeof(T) > 256 ? 1 : DP * size
 #pragma unroll
     for (int i = 0; i < WK; ++i) {
       const float ti = stat[(i * ROWS + at_row) * 2];
-      sum += ti == -INFINITY ? 0.f : stat[(i * ROWS + at_row) * 2 + 1] * exp2_((ti - to) * c);
+      const float si = stat[(i * ROWS + at_row) * 2 + 1];
+      sum += ti == -INFINITY ? si : si * exp2_((ti - to) * c);   // NaN (a maximum leaves it out) or 0 beside -inf
     }
     top = to;
     if (wk > 0) store_row<float, DP>(part + (wk * ROWS + at_row) * JOIN_ROW, acc, f, h, DP);
@@ -595,8 +596,9 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a) {
     }
 #pragma unroll
     for (int s = 0; s < FEW_SPLITS; ++s) {
-      if (s >= a.splits || ml[s].x == -INFINITY) continue;
-      const float f = exp2_((ml[s].x - top) * a.scale_log2);
+      // nothing seen is a sum of 0: the maximum of scores that are all NaN is -inf too
+      if (s >= a.splits || (ml[s].x == -INFINITY && ml[s].y == 0.f)) continue;
+      const float f = ml[s].x == -INFINITY ? 0.f : exp2_((ml[s].x - top) * a.scale_log2);
       sum = fmaf(ml[s].y, f, sum);
       acc.x = fmaf(v[s].x, f, acc.x);
       acc.y = fmaf(v[s].y, f, acc.y);
