@@ -150,13 +150,14 @@ struct Stager {
     }
   }
   // Rows of a key head's queries from row `first`, of `left` rows: token row / group, head row % group.
-  __device__ __forceinline__ void queries(int64_t st, int64_t sh, int first, int left, int group, int dim) {
+  // Zeros in place of the first `dead` rows.
+  __device__ __forceinline__ void queries(int64_t st, int64_t sh, int first, int dead, int left, int group, int dim) {
     const int token0 = first / group;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int c = chunk_offset(i, dim), r = first + row(i), token = r / group;
       const int64_t o = ((token - token0) * st + (r - token * group) * sh) * static_cast<int64_t>(sizeof(T));
-      off[i] = c < 0 || row(i) >= left ? BUF_OOB : static_cast<uint32_t>(o) + c;
+      off[i] = c < 0 || row(i) < dead || row(i) >= left ? BUF_OOB : static_cast<uint32_t>(o) + c;
     }
   }
   // The loads are written out: the compiler would let every later transposing LDS read wait for them,
@@ -486,6 +487,10 @@ __global__ __launch_bounds__(64 * WR * WK, (DP * sizeof(T) > 256 ? 1 : DP * size
     return;
   }
   const bool any = limit > 0 && (sum > 0.f || sum != sum);
+  if (!any) {   // not zero times them: what others see may be infinite
+#pragma unroll
+    for (int m = 0; m < DP / 32; ++m) zero(acc[m]);
+  }
   store_row<T, DP>(at<T>(a.out, a.o_stride, w.b, token, head), acc, any ? a.inv_keep / sum : 0.f, h, a.dim);
   if (h == 0) a.lse[stat] = any ? fmaf(top, a.scale, __builtin_amdgcn_logf(sum) * LN2) : -INFINITY;
 }
@@ -641,8 +646,9 @@ __global__ __launch_bounds__(64 * WR, (DP * sizeof(T) > 256 ? 1 : 2)) void attn_
   const int row0 = tile * ROWS, wave0 = row0 + wave * 32;
   const int row = wave0 + (lane & 31);
   const int token = row / a.group, head = w.kvh * a.group + row - token * a.group;
-  const bool in_q = row < rows, live = in_q && token < w.q_len;
+  const bool in_q = row < rows;
   const int limit = in_q ? seen(a, w, token) : 0;
+  const bool live = limit > 0;   // a row without keys counts as zeros, whatever it holds
   const int from = in_q ? token : 0;
 
   const int last_row = (row0 + ROWS < rows ? row0 + ROWS : rows) - 1;
@@ -777,12 +783,15 @@ __global__ __launch_bounds__(64 * WR, (DP * sizeof(T) > 256 ? 1 : 2)) void attn_
     }
   });
   if (!in_q) return;
-  const float f = limit > 0 ? a.scale : 0.f;
+  if (!live) {
+#pragma unroll
+    for (int m = 0; m < DP / 32; ++m) zero(acc[m]);
+  }
   if (a.splits > 1) {
-    if (live)
-      store_row<float, DP>(a.part + ((static_cast<int64_t>(split) * a.batch * a.kv_heads + bh) * rows + row) * DP, acc, f, h, DP);
+    if (token < w.q_len)
+      store_row<float, DP>(a.part + ((static_cast<int64_t>(split) * a.batch * a.kv_heads + bh) * rows + row) * DP, acc, a.scale, h, DP);
   } else {
-    store_row<T, DP>(at<T>(a.dq, a.q_stride, w.b, token, head), acc, f, h, a.dim);
+    store_row<T, DP>(at<T>(a.dq, a.q_stride, w.b, token, head), acc, a.scale, h, a.dim);
   }
 }
 
@@ -826,12 +835,14 @@ __global__ __launch_bounds__(64 * WC, (DP * sizeof(T) > 128 ? 1 : 2)) void attn_
   const T* const gb = at<T>(a.d_o, a.o_stride, w.b, 0, w.kvh * a.group);
   Stager<T, DP, RT, THREADS> sq, sg;
   const bool same = RT % a.group == 0;   // every whole tile has the same offsets
+  // rows that see no key at all, staged as zeros: only the first tile can have such
+  const int blind = a.causal && w.q_len > w.kv_len ? (w.q_len - w.kv_len) * a.group : 0;
   const int64_t stat0 = static_cast<int64_t>(bh) * a.q_len * a.group;
   auto stage = [&](int t, bool offsets) {
     const int r0 = t * RT, left = rows - r0, token0 = r0 / a.group;
-    if (offsets || !same || left < RT) {
-      sq.queries(a.q_stride[1], a.q_stride[2], r0, left, a.group, a.dim);
-      sg.queries(a.o_stride[1], a.o_stride[2], r0, left, a.group, a.dim);
+    if (offsets || !same || left < RT || r0 - RT < blind) {
+      sq.queries(a.q_stride[1], a.q_stride[2], r0, blind - r0, left, a.group, a.dim);
+      sg.queries(a.o_stride[1], a.o_stride[2], r0, blind - r0, left, a.group, a.dim);
     }
     char* const to = lds + (t & 1) * BUFFER;
     sq.load(qb + token0 * a.q_stride[1], 0x7fffffffu, to);

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from oracle import tokens as T
-from test_gpu_ops import BAR, attention, check, dev, draw, host, like, near
+from test_gpu_ops import BAR, RNG, attention, check, dev, draw, host, like, near, rng_tensor
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +58,65 @@ def test_attention_over_nan_keys_is_nan(nq, nk, dtype):
         got = _forward(q, k, v, dtype, 2)
         assert np.isnan(got[0][0, :, 2:]).all() and np.isnan(got[1][0, 2:]).all()
         _like_oracle(got, q, k, v, dtype)
+
+
+# causal with more queries than keys: the first ones see none.  (batch, q_len, kv_len, heads, kv_heads, dim),
+# lengths; row tiles that such queries end inside of, head groups that divide no tile, splits of rows and keys
+BLIND = [((2, 70, 20, 4, 2, 64), None), ((1, 90, 37, 3, 1, 40), None), ((3, 70, 97, 4, 2, 64), ([60, 70, 33], [41, 0, 64])),
+         ((1, 900, 300, 4, 1, 128), None), ((2, 33, 5, 2, 2, 32), ([33, 20], [5, 1]))]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("p", [0.0, 0.2])
+@pytest.mark.parametrize("shape,lens", BLIND, ids=str)
+def test_attention_queries_without_keys_may_hold_anything(shape, lens, p, dtype):
+    """NaN and infinities in queries that see no key, and in their d_o, reach nothing."""
+    from paper_2406_02052_amd import Attention
+
+    print("case", shape, lens, p, dtype, flush=True)
+    b, nq, nk, h, kvh, d = shape
+    lq, lk = lens or ([nq] * b, [nk] * b)
+    q, k, v, g = draw(nq, (b, nq, h, d), (b, nk, kvh, d), (b, nk, kvh, d), (b, nq, h, d), dtype=dtype)
+    mask = T.factor_attention(RNG, p, b, h, nq, nk) if p else None
+    want = T.attention(q, k, v, 1 / math.sqrt(d), True, lq, lk, mask, g)
+    for i in range(b):
+        blind = max(0, lq[i] - lk[i])
+        assert i or blind
+        for t in (q, g):
+            t[i, :blind] = np.array([math.nan, math.inf, -math.inf])[np.arange(blind) % 3, None, None]
+            t[i, lq[i]:] = math.nan
+    t = [dev(x, dtype) for x in (q, k, v, g)]
+    op = Attention(b, nq, nk, h, kvh, d, dtype, causal=True, dropout=p)
+    more = dict(rng=rng_tensor() if p else None)
+    if lens:
+        more.update(q_lens=torch.tensor(lq, dtype=torch.int32, device="cuda"), kv_lens=torch.tensor(lk, dtype=torch.int32, device="cuda"))
+    o, lse, grads = like(t[0]), torch.full((b, h, nq), math.nan, device="cuda"), [like(x) for x in t[:3]]
+    op.forward(*t[:3], o, lse, **more)
+    op.backward(*t[:3], o, lse, t[3], *grads, **more)
+    torch.cuda.synchronize()
+    check([o, lse, *grads], want, dtype)
+    for x in (o, grads[0]):
+        for i in range(b):
+            assert (x[i, :max(0, lq[i] - lk[i])] == 0).all() and (x[i, lq[i]:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("nk", [60, 700])
+@pytest.mark.parametrize("nq", [6, 40, 200])
+def test_attention_infinities_stay_out_of_rows_past_the_length(nq, nk, dtype):
+    """A value that is infinite where the queries within the length see it."""
+    from paper_2406_02052_amd import Attention
+
+    print("case", nq, nk, dtype, flush=True)
+    q, k, v, g = (dev(x, dtype) for x in draw(nq, (1, nq, 2, 64), (1, nk, 2, 64), (1, nk, 2, 64), (1, nq, 2, 64), dtype=dtype))
+    v[0, nk // 2] = math.inf
+    n = nq // 2
+    lens = dict(q_lens=torch.tensor([n], dtype=torch.int32, device="cuda"))
+    op = Attention(1, nq, nk, 2, 2, 64, dtype)
+    o, lse, grads = like(q), torch.full((1, 2, nq), math.nan, device="cuda"), [like(x) for x in (q, k, v)]
+    op.forward(q, k, v, o, lse, **lens)
+    op.backward(q, k, v, o, lse, g, *grads, **lens)
+    torch.cuda.synchronize()
+    for x in (o, grads[0]):
+        assert not torch.isfinite(x[0, :n]).any() and (x[0, n:] == 0).all()
+    assert torch.isfinite(lse[:, :, :n]).all() and torch.isneginf(lse[:, :, n:]).all()
