@@ -702,8 +702,9 @@ __global__ __launch_bounds__(64 * WR, (DP * sizeof(T) > 256 ? 1 : 2)) void attn_
     delta = sum_halves(delta);
   }
   const int64_t stat = (static_cast<int64_t>(w.b) * a.heads + head) * a.q_len + token;
-  // a row without keys: lse +inf makes every p zero
-  const float lse = limit > 0 ? a.lse[stat] * LOG2E : INFINITY;
+  // a row without keys, or whose scores are all -inf, which the forward took as such: lse +inf makes every p zero
+  float lse = limit > 0 ? a.lse[stat] * LOG2E : INFINITY;
+  if (lse == -INFINITY) lse = INFINITY;
   const float c = a.scale_log2;
   Rng rng{};
   if (DROP) rng = load_rng(a.rng);

@@ -120,3 +120,33 @@ def test_attention_infinities_stay_out_of_rows_past_the_length(nq, nk, dtype):
     for x in (o, grads[0]):
         assert not torch.isfinite(x[0, :n]).any() and (x[0, n:] == 0).all()
     assert torch.isfinite(lse[:, :, :n]).all() and torch.isneginf(lse[:, :, n:]).all()
+
+
+@pytest.mark.parametrize("nq,nk", [(3, 50), (40, 50), (200, 700)])
+def test_attention_gradients_of_scores_that_are_all_minus_infinity(nq, nk):
+    """fp32 products past the type's range: such a row has o = 0, lse = -inf and, its probabilities being
+    zero, no part in dv nor, as its q and k are finite, in dq and dk."""
+    from paper_2406_02052_amd import Attention
+
+    print("case", nq, nk, flush=True)
+    q, k, v, g = draw(nq, (1, nq, 2, 64), (1, nk, 2, 64), (1, nk, 2, 64), (1, nq, 2, 64))
+    k[:, :, 1] = -1e18 * np.abs(k[:, :, 1])
+    q[:, nq // 2:, 1] = 1e22 * (1 + np.abs(q[:, nq // 2:, 1]))     # every product below -1e39
+    k[:, :, 1] -= 1e18
+    q[:, :nq // 2, 1] *= 1e-18
+    q, k = (host(torch.tensor(x).float()) for x in (q, k))
+    keep = [x.copy() for x in (q, g)]
+    for t in keep:
+        t[:, nq // 2:, 1] = 0.0
+    want = T.attention(keep[0], k, v, 0.125, d_o=keep[1])           # those rows' d_o as zeros: no part in dk, dv
+    t = [dev(x, "fp32") for x in (q, k, v, g)]
+    op = Attention(1, nq, nk, 2, 2, 64, "fp32", scale=0.125)
+    o, lse, grads = like(t[0]), torch.full((1, 2, nq), math.nan, device="cuda"), [like(x) for x in t[:3]]
+    op.forward(*t[:3], o, lse)
+    op.backward(*t[:3], o, lse, t[3], *grads)
+    torch.cuda.synchronize()
+    assert (o[0, nq // 2:, 1] == 0).all() and torch.isneginf(lse[0, 1, nq // 2:]).all()
+    assert (grads[0][0, nq // 2:, 1] == 0).all()
+    for h in range(2):   # the heads' gradients differ by 2^60 in size
+        for x, y, name in zip(grads, want[2:], ("dq", "dk", "dv")):
+            near(x[:, :, h], y[:, :, h], BAR["fp32", "grad"], name)
