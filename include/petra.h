@@ -431,6 +431,10 @@ petra_status petra_net_backprop_step(petra_net* net, const void* images, const i
  * given strides, in elements, of the first three dimensions (all three zero:
  * contiguous); channels are contiguous.  o and d_o have o_stride; a gradient has
  * its tensor's strides.  lse is fp32 [batch][heads][q_len].
+ * A written tensor shares no element with another tensor of the call.  Interleaved ones are
+ * fine (slices of one tensor, such as the q, k and v of one product); two that are woven into
+ * each other with different strides, so that 2^16 pairs of their rows do not tell them apart,
+ * are refused.
  * Limits: heads a multiple of kv_heads; head_dim a multiple of 8, at most 128;
  * strides not negative and multiples of 16 bytes, those of written tensors such
  * that no elements share memory, a token stride of k and v below 2^22 elements;

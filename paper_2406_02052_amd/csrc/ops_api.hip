@@ -115,6 +115,16 @@ void strides(const int64_t in[3], int64_t out[3], int64_t len, int64_t heads, in
   }
 }
 
+// The bytes from a tensor's first element to its last lie within the address space, so that
+// sums of its strides fit 64 bits.
+void need_reach(const int64_t st[3], const int64_t n[3], int64_t dim, size_t esz, const char* name) {
+  __int128 extent = dim;
+  for (int i = 0; i < 3; ++i)
+    if (n[i] > 0) extent += static_cast<__int128>(n[i] - 1) * st[i];
+  if (extent * static_cast<__int128>(esz) >= __int128{1} << 47)
+    throw Refused{PETRA_ERR_SHAPE, std::string("strides reach past the address space: ") + name};
+}
+
 // No two elements of a written tensor share memory: by growing stride, each dimension
 // steps past what the smaller ones cover.
 void need_distinct(const int64_t st[3], const int64_t n[3], int64_t dim, const char* name) {
@@ -127,6 +137,74 @@ void need_distinct(const int64_t st[3], const int64_t n[3], int64_t dim, const c
     if (st[i] < extent) throw Refused{PETRA_ERR_SHAPE, std::string("elements share memory: ") + name};
     extent += (n[i] - 1) * st[i];
   }
+}
+
+// The memory of a strided tensor: runs of `run` bytes, at n[i] positions step[i] bytes apart in
+// each of `dims` dimensions, the largest step first.
+struct Runs {
+  const void* p = nullptr;
+  const char* name = "";
+  int64_t run = 0, step[3] = {}, n[3] = {};
+  int dims = 0;
+
+  Runs() = default;
+  Runs(const Span& s) : p(s.p), name(s.name), run(static_cast<int64_t>(s.bytes)) {}
+  Runs(const void* at, const int64_t st[3], const int64_t count[3], int64_t dim, size_t esz, const char* what)
+      : p(at), name(what), run(dim * static_cast<int64_t>(esz)) {
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int x, int y) { return st[x] > st[y]; });
+    for (int i : order) {
+      if (count[i] <= 0) run = 0;
+      if (count[i] <= 1 || st[i] == 0) continue;   // (positions that share their memory are one)
+      step[dims] = st[i] * static_cast<int64_t>(esz);
+      n[dims++] = count[i];
+    }
+    // dimensions without gaps are one, and a run where they reach the channels
+    for (int i = dims - 2; i >= 0; --i)
+      if (step[i] == n[i + 1] * step[i + 1]) {
+        n[i] *= n[i + 1];
+        step[i] = step[i + 1];
+        for (int j = i + 1; j + 1 < dims; ++j) n[j] = n[j + 1], step[j] = step[j + 1];
+        --dims;
+      }
+    if (dims > 0 && step[dims - 1] == run) run *= n[--dims];
+  }
+  // Bytes from the first to the last, of the dimensions from d on.
+  int64_t extent(int d) const {
+    int64_t e = run;
+    for (; d < dims; ++d) e += (n[d] - 1) * step[d];
+    return e;
+  }
+};
+
+int64_t div_up(int64_t x, int64_t y) { return x > 0 ? (x + y - 1) / y : -(-x / y); }
+int64_t div_down(int64_t x, int64_t y) { return -div_up(-x, y); }
+
+// Whether a's dimensions from da on and b's from db on share a byte, b's first being `off` past a's.
+// Slices of one tensor have their steps in common, so that only the difference of two positions
+// matters and few are near enough; other pairs go by the positions of the larger step.  `budget`
+// bounds the pairs looked at: two tensors woven into each other past it count as sharing.
+bool meet(const Runs& a, int da, const Runs& b, int db, int64_t off, int& budget) {
+  const int64_t ea = a.extent(da), eb = b.extent(db);
+  if (off >= ea || -off >= eb) return false;
+  const bool more_a = da < a.dims, more_b = db < b.dims;
+  if (!more_a && !more_b) return true;
+  if (--budget < 0) return true;
+  const int64_t sa = more_a ? a.step[da] : 0, sb = more_b ? b.step[db] : 0, s = std::max(sa, sb);
+  const bool in_a = sa == s, in_b = sb == s;
+  // off + k s for k = (b's position, where it has this step) - (a's)
+  const int64_t first = std::max(in_a ? 1 - a.n[da] : 0, div_up(1 - off - (in_b ? b.extent(db + 1) : eb), s));
+  const int64_t last = std::min(in_b ? b.n[db] - 1 : 0, div_down((in_a ? a.extent(da + 1) : ea) - 1 - off, s));
+  for (int64_t k = first; k <= last; ++k)
+    if (meet(a, da + in_a, b, db + in_b, off + k * s, budget)) return true;
+  return false;
+}
+
+void need_apart(const Runs& a, const Runs& b) {
+  if (a.p == nullptr || b.p == nullptr || a.run == 0 || b.run == 0) return;
+  int budget = 1 << 16;
+  if (meet(a, 0, b, 0, static_cast<int64_t>(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)), budget))
+    throw Refused{PETRA_ERR_ALIAS, std::string("buffers overlap: ") + a.name + " and " + b.name};
 }
 
 struct Attn {
@@ -170,6 +248,10 @@ struct Attn {
     need(a.k_stride[1] < (1 << 22) && a.v_stride[1] < (1 << 22), PETRA_ERR_SHAPE,
          "token stride of k or v of 2^22 elements or more");
     const int64_t nq[3] = {a.batch, a.q_len, a.heads}, nk[3] = {a.batch, a.kv_len, a.kv_heads};
+    need_reach(a.q_stride, nq, a.dim, esz, "q");
+    need_reach(a.k_stride, nk, a.dim, esz, "k");
+    need_reach(a.v_stride, nk, a.dim, esz, "v");
+    need_reach(a.o_stride, nq, a.dim, esz, "o");
     // tiles of keys, and in the backward of queries, are addressed by 32-bit offsets from their first row
     need(a.kv_len <= 1 || (a.k_stride[1] >= a.dim && a.v_stride[1] >= a.dim), PETRA_ERR_SHAPE,
          "token stride of k or v below head_dim");
@@ -185,15 +267,12 @@ struct Attn {
     plan = petra::attn_plan(a, d->dtype);
   }
 
-  // From a tensor's first element to its last; zero bytes for a strided one, whose
-  // elements may lie between another's.
-  Span dense(const void* p, const int64_t st[3], bool kv, const char* name) const {
-    const int64_t len = kv ? a.kv_len : a.q_len, heads = kv ? a.kv_heads : a.heads;
-    const int64_t n = a.batch * len * heads * a.dim;
-    int64_t extent = a.dim;
-    if (n > 0) extent += (a.batch - 1) * st[0] + (len - 1) * st[1] + (heads - 1) * st[2];
-    return {p, n > 0 && extent == n ? n * esz : n > 0 ? 1 : 0, name};
+  // The memory of q, k, v, o or what is laid out like it, and of lse.
+  Runs tensor(const void* p, const int64_t st[3], bool kv, const char* name) const {
+    const int64_t n[3] = {a.batch, kv ? a.kv_len : a.q_len, kv ? a.kv_heads : a.heads};
+    return {p, st, n, a.dim, esz, name};
   }
+  Runs stats(const float* p) const { return Span{p, static_cast<size_t>(a.batch) * a.heads * a.q_len * 4, "lse"}; }
 };
 
 }  // namespace
@@ -221,14 +300,13 @@ petra_status petra_attn_forward(const petra_attn_desc* desc, const void* q, cons
     need_ptr(lse, "lse", t.no_q());
     need_int_ptr(q_lens, "q_lens", 4);
     need_int_ptr(kv_lens, "kv_lens", 4);
-    const Span so = t.dense(o, t.a.o_stride, false, "o");
-    const Span sl{lse, static_cast<size_t>(t.a.batch) * t.a.heads * t.a.q_len * 4, "lse"};
-    for (const Span& in : {t.dense(q, t.a.q_stride, false, "q"), t.dense(k, t.a.k_stride, true, "k"),
-                           t.dense(v, t.a.v_stride, true, "v")}) {
-      need_apart(so, in);
-      need_apart(sl, in);
+    const Runs ro = t.tensor(o, t.a.o_stride, false, "o"), rl = t.stats(lse);
+    for (const Runs& in : {t.tensor(q, t.a.q_stride, false, "q"), t.tensor(k, t.a.k_stride, true, "k"),
+                           t.tensor(v, t.a.v_stride, true, "v")}) {
+      need_apart(ro, in);
+      need_apart(rl, in);
     }
-    need_apart(so, sl);
+    need_apart(ro, rl);
     need_workspace(workspace, workspace_bytes, t.plan.fwd_bytes);
     if (t.no_q()) return false;
     t.a.q = q;
@@ -261,14 +339,13 @@ petra_status petra_attn_backward(const petra_attn_desc* desc, const void* q, con
     need_ptr(dv, "dv", nk);
     need_int_ptr(q_lens, "q_lens", 4);
     need_int_ptr(kv_lens, "kv_lens", 4);
-    const Span in[6] = {t.dense(q, t.a.q_stride, false, "q"), t.dense(k, t.a.k_stride, true, "k"),
-                        t.dense(v, t.a.v_stride, true, "v"), t.dense(o, t.a.o_stride, false, "o"),
-                        t.dense(d_o, t.a.o_stride, false, "d_o"),
-                        {lse, static_cast<size_t>(t.a.batch) * t.a.heads * t.a.q_len * 4, "lse"}};
-    const Span out[3] = {t.dense(dq, t.a.q_stride, false, "dq"), t.dense(dk, t.a.k_stride, true, "dk"),
-                         t.dense(dv, t.a.v_stride, true, "dv")};
+    const Runs in[6] = {t.tensor(q, t.a.q_stride, false, "q"), t.tensor(k, t.a.k_stride, true, "k"),
+                        t.tensor(v, t.a.v_stride, true, "v"), t.tensor(o, t.a.o_stride, false, "o"),
+                        t.tensor(d_o, t.a.o_stride, false, "d_o"), t.stats(lse)};
+    const Runs out[3] = {t.tensor(dq, t.a.q_stride, false, "dq"), t.tensor(dk, t.a.k_stride, true, "dk"),
+                         t.tensor(dv, t.a.v_stride, true, "dv")};
     for (int i = 0; i < 3; ++i) {
-      for (const Span& s : in) need_apart(out[i], s);
+      for (const Runs& r : in) need_apart(out[i], r);
       for (int j = 0; j < i; ++j) need_apart(out[i], out[j]);
     }
     need_workspace(workspace, workspace_bytes, t.plan.bwd_bytes);
