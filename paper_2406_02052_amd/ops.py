@@ -4,7 +4,10 @@ the coupling of a residual function to its stream, and dropout.
 Marshalling only, as in stage.py.  Tensors are the caller's; their types, shapes
 and strides are checked here, everything else by the library.  A workspace holds
 nothing between calls, but calls of one owner that overlap in time (on other
-streams) need an owner each.
+streams) need an owner each.  An owner may be dropped while its calls still run:
+its workspace's memory is not given out again before the streams they were put on
+have passed them.  A stream that is given as a bare handle can't be waited for so;
+there the owner has to stay until the work is done.
 """
 from __future__ import annotations
 
@@ -35,7 +38,29 @@ def _need_rng(rng) -> None:
         raise ValueError("rng: need a device int64 tensor [seed, offset]")
 
 
-class Attention:
+class _Owner:
+    """A workspace, and the streams that have used it."""
+
+    def _own(self, ws_bytes: int, device) -> None:
+        import torch
+        self.ws_bytes = ws_bytes
+        self.workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=device)
+        # the allocator knows the stream that memory is taken on, and no other
+        self.streams = set()
+        if self.workspace.is_cuda:
+            self.streams.add(torch.cuda.current_stream(self.workspace.device).cuda_stream)
+
+    def _on(self, stream) -> int:
+        """The stream's handle; tells the allocator of a stream that is new to the workspace."""
+        handle = L._stream(stream)
+        if handle not in self.streams and not isinstance(stream, int):
+            import torch
+            self.workspace.record_stream(torch.cuda.current_stream() if stream is None else stream)
+            self.streams.add(handle)
+        return handle
+
+
+class Attention(_Owner):
     """Attention of [batch, q_len, heads, head_dim] over [batch, kv_len, kv_heads, head_dim]
     tensors (any strides of the first three dimensions; channels contiguous)."""
 
@@ -52,8 +77,7 @@ class Attention:
         self.form = None
         self.itype, self.ftype = torch.int32, torch.float32
         self.fwd_bytes, self.bwd_bytes = L.petra_attn_query(self.desc)
-        self.ws_bytes = max(self.fwd_bytes, self.bwd_bytes)
-        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+        self._own(max(self.fwd_bytes, self.bwd_bytes), device)
 
     def _lay(self, q, k, v, o, lse, q_lens, kv_lens, rng) -> None:
         """Checks the tensors and puts their strides into the description.  What was checked
@@ -91,7 +115,7 @@ class Attention:
         """Writes o [batch, q_len, heads, head_dim] and lse (fp32 [batch, heads, q_len])."""
         self._lay(q, k, v, o, lse, q_lens, kv_lens, rng)
         L.petra_attn_forward(self.desc, q, k, v, q_lens, kv_lens, rng, o, lse, self.workspace,
-                             self.ws_bytes, stream)
+                             self.ws_bytes, self._on(stream))
 
     def backward(self, q, k, v, o, lse, d_o, dq, dk, dv, q_lens=None, kv_lens=None, rng=None,
                  stream=None) -> None:
@@ -102,10 +126,10 @@ class Attention:
                 raise ValueError(f"{name}: need strides {like.stride()}, got {t.stride()}")
             _need(t, name, self.tdtype, tuple(like.shape), dense=False)
         L.petra_attn_backward(self.desc, q, k, v, o, lse, d_o, q_lens, kv_lens, rng, dq, dk, dv,
-                              self.workspace, self.ws_bytes, stream)
+                              self.workspace, self.ws_bytes, self._on(stream))
 
 
-class Coupling:
+class Coupling(_Owner):
     """y = residual_scale x + gate m n(f; post), u = n(y; pre) over [rows, width] tensors, and its
     backward, which also rebuilds x.  post and pre are (gamma, beta or None), fp32."""
 
@@ -121,8 +145,7 @@ class Coupling:
                                    L.PETRA_NORM_RMS if norm == "rms" else L.PETRA_NORM_LAYER,
                                    eps, residual_scale, dropout)
         self.gate_shape = (rows // rows_per_gate if rows_per_gate else 1, width)
-        self.ws_bytes = L.petra_coupling_query(self.desc)
-        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+        self._own(L.petra_coupling_query(self.desc), device)
 
     def _check(self, acts, gates, norms, rng) -> None:
         """acts: (name, tensor) of activations; gates and norms likewise; None is left out."""
@@ -155,7 +178,7 @@ class Coupling:
                      ("df", df)), (("gate", gate), ("dgate", dgate)),
                     (("post", post), ("pre", pre), ("dpost", dpost), ("dpre", dpre)), rng)
         L.petra_coupling_backward(self.desc, y, f, dy, du, gate, post, pre, rng, x, dx, df, dgate,
-                                  dpost, dpre, self.workspace, self.ws_bytes, stream)
+                                  dpost, dpre, self.workspace, self.ws_bytes, self._on(stream))
 
 
 def dropout(x, y, p: float, rng, residual=None, alpha: float = 1.0, stream=None) -> None:

@@ -150,3 +150,55 @@ def test_attention_gradients_of_scores_that_are_all_minus_infinity(nq, nk):
     for h in range(2):   # the heads' gradients differ by 2^60 in size
         for x, y, name in zip(grads, want[2:], ("dq", "dk", "dv")):
             near(x[:, :, h], y[:, :, h], BAR["fp32", "grad"], name)
+
+
+def _busy(stream):
+    """Some tens of milliseconds of products on a stream."""
+    with torch.cuda.stream(stream):
+        a = torch.randn(8192, 8192, device="cuda", dtype=torch.bfloat16)
+        for _ in range(40):
+            a = (a @ a).clamp_(-1, 1)
+
+
+@pytest.mark.parametrize("which", ["attention", "coupling"])
+@pytest.mark.parametrize("how", ["argument", "current"])
+def test_owner_dropped_while_its_call_runs_on_another_stream(how, which):
+    """Its workspace's memory is not given to the current stream before the call has ended."""
+    from paper_2406_02052_amd import Attention, Coupling
+
+    print("case", how, which, flush=True)
+    s = torch.cuda.Stream()
+    if which == "attention":
+        t = [dev(x, "bf16") for x in draw(5, (1, 4, 8, 64), (1, 4096, 8, 64), (1, 4096, 8, 64))]
+        out = [torch.empty_like(t[0]), torch.empty(1, 8, 4, device="cuda")]
+        make = lambda: Attention(1, 4, 4096, 8, 8, 64)  # noqa: E731
+        call = lambda op, **kw: op.forward(*t, *out, **kw)  # noqa: E731
+    else:
+        y, f, dy = (dev(x, "bf16") for x in draw(6, *[(700, 256)] * 3))
+        gate, post = torch.ones(1, 256, device="cuda"), (torch.ones(256, device="cuda"), None)
+        new = lambda: torch.empty_like(y)  # noqa: E731
+        out = [new(), new(), new(), torch.empty_like(gate), torch.empty_like(post[0])]
+        make = lambda: Coupling(700, 256)  # noqa: E731
+        call = lambda op, **kw: op.backward(y, f, dy, gate, post, *out[:4], (out[4], None), **kw)  # noqa: E731
+    call(make())
+    torch.cuda.synchronize()
+    want = [x.clone() for x in out]
+    for x in out:
+        x.zero_()
+    op = make()
+    assert op.ws_bytes > 0
+    at, n = op.workspace.data_ptr(), op.ws_bytes
+    torch.cuda.synchronize()
+    _busy(s)
+    if how == "argument":
+        call(op, stream=s)
+    else:
+        with torch.cuda.stream(s):
+            call(op)
+    del op
+    taken = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    assert not s.query()                 # the call still waits
+    assert all(x.data_ptr() >= at + n or x.data_ptr() + n <= at for x in taken)
+    torch.cuda.synchronize()
+    for x, y in zip(out, want):
+        assert torch.equal(x, y)
