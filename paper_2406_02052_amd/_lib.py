@@ -202,10 +202,9 @@ def _ptr(t) -> int:
     """Device address of a tensor (or an int address, or None)."""
     if t is None:
         return 0
-    try:
-        return t.data_ptr()
-    except AttributeError:
-        return int(t)
+    if isinstance(t, int):
+        return t
+    return t.data_ptr()
 
 
 def _stream(stream) -> int:

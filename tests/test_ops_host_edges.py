@@ -107,3 +107,20 @@ def test_overlap_is_that_of_the_elements():
         assert forward(d, o, k) == ("PETRA_ERR_ALIAS" if want else "PETRA_ERR_WORKSPACE"), (counts, kv_heads, dim, st, kst, o - k)
         seen[want] += 1
     assert min(seen.values()) > 100, seen
+
+
+@pytest.mark.parametrize("bad", [3.5, "4096", np.float32(16), np.array([4096]), [4096]], ids=repr)
+def test_what_is_no_address_is_refused(bad):
+    """A number or text that int() takes is no device address."""
+    with pytest.raises(AttributeError):
+        L._ptr(bad)
+    with pytest.raises(AttributeError):
+        L.petra_dropout(8, L.PETRA_FP32, 0.0, 1.0, bad, 0, 0, FAR[0], 0)
+
+
+def test_addresses():
+    class Tensor:
+        def data_ptr(self):
+            return 4096
+
+    assert (L._ptr(None), L._ptr(4096), L._ptr(Tensor())) == (0, 4096, 4096)
