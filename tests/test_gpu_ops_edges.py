@@ -202,3 +202,14 @@ def test_owner_dropped_while_its_call_runs_on_another_stream(how, which):
     torch.cuda.synchronize()
     for x, y in zip(out, want):
         assert torch.equal(x, y)
+
+
+def test_current_stream_is_torchs():
+    from paper_2406_02052_amd import _lib as L
+
+    s = torch.cuda.Stream()
+    assert L._stream(None) == torch.cuda.current_stream().cuda_stream
+    for stream in (s, torch.cuda.ExternalStream(torch.cuda.Stream().cuda_stream), torch.cuda.default_stream()):
+        with torch.cuda.stream(stream):
+            assert L._stream(None) == stream.cuda_stream == torch.cuda.current_stream().cuda_stream
+    assert L._stream(None) == torch.cuda.current_stream().cuda_stream

@@ -124,3 +124,15 @@ def test_addresses():
             return 4096
 
     assert (L._ptr(None), L._ptr(4096), L._ptr(Tensor())) == (0, 4096, 4096)
+
+
+def test_current_stream_by_the_public_call_where_torch_has_no_other(monkeypatch):
+    import torch
+
+    class Stream:
+        cuda_stream = 77
+
+    monkeypatch.setattr(torch.cuda, "current_stream", Stream)
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    assert L._stream(None) == 77
+    assert L._stream(Stream()) == 77 and L._stream(5) == 5
