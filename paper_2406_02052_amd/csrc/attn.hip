@@ -219,11 +219,11 @@ struct Item {
   int bh, split, tile;
 };
 __device__ __forceinline__ Item work_item(const AttnArgs& a, bool last_first) {
-  const int heads = a.batch * a.kv_heads, rest = blockIdx.x / a.splits;
+  const int rest = blockIdx.x / a.splits;
   Item i;
   i.split = blockIdx.x - rest * a.splits;
-  i.tile = rest / heads;
-  i.bh = rest - i.tile * heads;
+  i.tile = rest / a.bhs;
+  i.bh = a.bh0 + rest - i.tile * a.bhs;
   if (last_first) i.tile = a.tiles - 1 - i.tile;
   return i;
 }
@@ -1019,18 +1019,30 @@ template <> struct Shape<float> { static constexpr int KB = 1; };
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Launches tiles x splits workgroups for each (batch row, key head).  A grid has fewer than 2^32 lanes: more
+// heads than that holds go in several launches.  (One head always fits: 2^23 tiles at most, and splits only
+// where there are few workgroups.)
+void launch(AttnArgs& a, int64_t tiles, int splits, int threads, hipStream_t s, void (*kernel)(AttnArgs)) {
+  a.tiles = static_cast<int>(tiles);
+  a.splits = splits;
+  const int64_t bh = static_cast<int64_t>(a.batch) * a.kv_heads, most = 0xffffffffll / threads / (tiles * splits);
+  for (int64_t first = 0; first < bh; first += most) {
+    a.bh0 = static_cast<int>(first);
+    a.bhs = static_cast<int>(bh - first < most ? bh - first : most);
+    kernel<<<static_cast<unsigned>(tiles * splits * a.bhs), threads, 0, s>>>(a);
+  }
+}
+
 template <typename T, int DP, bool DROP>
 void forward_by(AttnArgs& a, const AttnPlan& p, hipStream_t s) {
   const int rows = a.q_len * a.group, bh = a.batch * a.kv_heads;
-  a.tiles = static_cast<int>(ceil_div(rows, p.row_tile));
-  a.splits = p.splits;
-  const unsigned grid = static_cast<unsigned>(a.tiles) * bh * a.splits;
+  const int64_t tiles = ceil_div(rows, p.row_tile);
   if (p.row_tile == 32)
-    attn_forward_kernel<T, DP, 1, 2, 1, DROP><<<grid, 128, 0, s>>>(a);
+    launch(a, tiles, p.splits, 128, s, attn_forward_kernel<T, DP, 1, 2, 1, DROP>);
   else if (p.row_tile == 64)
-    attn_forward_kernel<T, DP, 2, 1, Shape<T>::KB, DROP><<<grid, 128, 0, s>>>(a);
+    launch(a, tiles, p.splits, 128, s, attn_forward_kernel<T, DP, 2, 1, Shape<T>::KB, DROP>);
   else
-    attn_forward_kernel<T, DP, 4, 1, DP == 128 ? 1 : Shape<T>::KB, DROP><<<grid, 256, 0, s>>>(a);
+    launch(a, tiles, p.splits, 256, s, attn_forward_kernel<T, DP, 4, 1, DP == 128 ? 1 : Shape<T>::KB, DROP>);
   const int64_t out = static_cast<int64_t>(rows) * bh;
   if (a.splits > FEW_SPLITS)
     attn_join_kernel<T, DP><<<static_cast<unsigned>(ceil_div(out, 4)), 256, 0, s>>>(a);
@@ -1047,22 +1059,18 @@ void backward_by(AttnArgs& a, const AttnPlan& p, hipStream_t s) {
     return r;
   };
   if (rows > 0) {
-    a.tiles = static_cast<int>(ceil_div(rows, p.dq_tile));
-    a.splits = p.dq_splits;
-    const unsigned grid = static_cast<unsigned>(a.tiles) * bh * a.splits;
-    if (p.dq_tile == 64) attn_dq_kernel<T, DP, 2, Shape<T>::KB, DROP><<<grid, 128, 0, s>>>(a);
-    else attn_dq_kernel<T, DP, 4, Shape<T>::KB, DROP><<<grid, 256, 0, s>>>(a);
+    const int64_t tiles = ceil_div(rows, p.dq_tile);
+    if (p.dq_tile == 64) launch(a, tiles, p.dq_splits, 128, s, attn_dq_kernel<T, DP, 2, Shape<T>::KB, DROP>);
+    else launch(a, tiles, p.dq_splits, 256, s, attn_dq_kernel<T, DP, 4, Shape<T>::KB, DROP>);
     if (a.splits > 1) {
       const SumArgs r = sum(a.dq, a.q_stride, a.q_lens, rows, a.splits, a.group);
       attn_sum_kernel<T, DP><<<static_cast<unsigned>(ceil_div(r.items, 256)), 256, 0, s>>>(r, r);
     }
   }
   if (a.kv_len > 0) {
-    a.tiles = static_cast<int>(ceil_div(a.kv_len, p.key_tile));
-    a.splits = p.dkv_splits;
-    const unsigned grid = static_cast<unsigned>(a.tiles) * bh * a.splits;
-    if (p.key_tile == 64) attn_dkv_kernel<T, DP, 2, Shape<T>::KB, DROP><<<grid, 128, 0, s>>>(a);
-    else attn_dkv_kernel<T, DP, 4, Shape<T>::KB, DROP><<<grid, 256, 0, s>>>(a);
+    const int64_t tiles = ceil_div(a.kv_len, p.key_tile);
+    if (p.key_tile == 64) launch(a, tiles, p.dkv_splits, 128, s, attn_dkv_kernel<T, DP, 2, Shape<T>::KB, DROP>);
+    else launch(a, tiles, p.dkv_splits, 256, s, attn_dkv_kernel<T, DP, 4, Shape<T>::KB, DROP>);
     if (a.splits > 1) {
       const SumArgs rk = sum(a.dk, a.k_stride, a.kv_lens, a.kv_len, a.splits, 1);
       SumArgs rv = sum(a.dv, a.v_stride, a.kv_lens, a.kv_len, a.splits, 1);

@@ -55,6 +55,7 @@ struct AttnArgs {
   // keys (forward, query gradient) or rows (key and value gradients) split over
   // `splits` workgroups, whose fp32 partial results go to `part`
   int splits, tiles;                         // tiles: of rows or keys, of one key head
+  int bh0, bhs;                              // the launch's first (batch row, key head), and how many
   float *part, *part_ml;
 };
 

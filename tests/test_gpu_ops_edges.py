@@ -213,3 +213,36 @@ def test_current_stream_is_torchs():
         with torch.cuda.stream(stream):
             assert L._stream(None) == stream.cuda_stream == torch.cuda.current_stream().cuda_stream
     assert L._stream(None) == torch.cuda.current_stream().cuda_stream
+
+
+def test_attention_of_more_workgroups_than_one_launch_holds():
+    """65535 batch rows of 258 tiles of queries, 2^24 workgroups of 256 lanes and more: 2^32 lanes."""
+    from paper_2406_02052_amd import Attention
+
+    b, n, d = 65535, 33000, 8
+    if torch.cuda.mem_get_info()[0] < 130 << 30:
+        pytest.skip("needs 130 GB of device memory")
+    assert b * -(-n // 128) >= 1 << 24
+    base, k, v = (dev(x, "bf16") for x in draw(1, (1, n, 1, d), (b, 1, 1, d), (b, 1, 1, d)))
+    base = (base * 2).round_()                     # sums over the queries without a rounding
+    q = base.expand(b, -1, -1, -1).contiguous()
+    op = Attention(b, n, 1, 1, 1, d)
+    o, lse = torch.full_like(q, math.nan), torch.full((b, 1, n), math.nan, device="cuda")
+    op.forward(q, k, v, o, lse)
+    torch.cuda.synchronize()
+    for i in range(0, b, 4096):                    # one key: o = v, lse = its score
+        assert (o[i:i + 4096] == v[i:i + 4096]).all()
+        score = torch.matmul(k[i:i + 4096, 0, 0].float(), base[0, :, 0].float().t().contiguous()) / math.sqrt(d)
+        assert (lse[i:i + 4096, 0] - score).abs().max() <= 1e-5 * max(1.0, float(score.abs().max()))
+    dq, dk, dv = o, torch.full_like(k, math.nan), torch.full_like(v, math.nan)
+    # d_o = o = q: D is taken from the products where one tile holds the keys.  ds = 0, dv = the sum of d_o
+    dq.fill_(math.nan)
+    op.backward(q, k, v, q, lse, q, dq, dk, dv)
+    torch.cuda.synchronize()
+    want = base.double().sum(1).to(torch.bfloat16)[0, 0]
+    assert (dv[:, 0, 0] == want).all()
+    for i in range(0, b, 4096):
+        assert (dq[i:i + 4096].abs().amax() <= 1e-3).all()
+    assert (dk.float().abs() <= 1e-2 * math.sqrt(n)).all()
+    del q, o, lse, dq, op
+    torch.cuda.empty_cache()
