@@ -381,24 +381,19 @@ __global__ __launch_bounds__(1024) void couple_join_kernel(JoinArgs a) {
   int n = 0;
   while (n + 1 < a.sets && o >= a.set[n].outs) o -= a.set[n++].outs;
   const JoinSet s = a.set[n];
-  // the last set has more outputs than a grid has rows
-  for (; o < s.outs; o += gridDim.y) {
-    float v = 0.f;
-    if (c < a.width) {
-      const float* p = s.part + (o * s.rows) * a.width + c;
+  float v = 0.f;
+  if (c < a.width) {
+    const float* p = s.part + (o * s.rows) * a.width + c;
 #pragma unroll 8
-      for (long r = lane; r < s.rows; r += 16) v += p[r * a.width];
-    }
-    lds[lane][threadIdx.x & 63] = v;
-    __syncthreads();
-    if (lane == 0 && c < a.width) {
-      float t = 0.f;
+    for (long r = lane; r < s.rows; r += 16) v += p[r * a.width];
+  }
+  lds[lane][threadIdx.x & 63] = v;
+  __syncthreads();
+  if (lane == 0 && c < a.width) {
+    float t = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) t += lds[i][threadIdx.x & 63];
-      s.out[o * a.width + c] = t;
-    }
-    __syncthreads();
-    if (n + 1 < a.sets) break;
+    for (int i = 0; i < 16; ++i) t += lds[i][threadIdx.x & 63];
+    s.out[o * a.width + c] = t;
   }
 }
 
@@ -566,9 +561,9 @@ void couple_backward(const CoupleArgs& a, int dtype, hipStream_t s) {
     if (a.blocks == 0) add(nullptr, a.dgate, a.gates, 0);
     if (a.chunks_per_gate > 1) add(a.part_gate, a.dgate, a.gates, a.chunks_per_gate);
   }
+  // (gates are joined where each has more rows than a workgroup's share, a 512th of all: fewer than 512)
   if (j.sets > 0)
-    couple_join_kernel<<<dim3(static_cast<unsigned>((a.width + 63) / 64), static_cast<unsigned>(outs < 4096 ? outs : 4096)),
-                         1024, 0, s>>>(j);
+    couple_join_kernel<<<dim3(static_cast<unsigned>((a.width + 63) / 64), static_cast<unsigned>(outs)), 1024, 0, s>>>(j);
 }
 
 void dropout(const void* x, const void* residual, void* y, long n, float factor, uint32_t cut,

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from oracle import tokens as T
-from test_gpu_ops import BAR, RNG, attention, check, dev, draw, host, like, near, rng_tensor
+from test_gpu_ops import BAR, RNG, attention, check, coupling, dev, draw, host, like, near, rng_tensor
 
 pytestmark = pytest.mark.gpu
 
@@ -246,3 +246,9 @@ def test_attention_of_more_workgroups_than_one_launch_holds():
     assert (dk.float().abs() <= 1e-2 * math.sqrt(n)).all()
     del q, o, lse, dq, op
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_coupling_joins_as_many_gates_as_there_can_be(dtype):
+    """487 gates of 21 rows over workgroups of 20: each gate's gradient is joined from two of them."""
+    coupling(dtype, 487 * 21, 2048, "layer", 21)
