@@ -252,3 +252,24 @@ def test_attention_of_more_workgroups_than_one_launch_holds():
 def test_coupling_joins_as_many_gates_as_there_can_be(dtype):
     """487 gates of 21 rows over workgroups of 20: each gate's gradient is joined from two of them."""
     coupling(dtype, 487 * 21, 2048, "layer", 21)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("width", [4104, 8192])
+@pytest.mark.parametrize("over", [dict(), dict(norm="layer", per_gate=1, scale=0.75), dict(norm="layer", per_gate=3, p=0.1),
+                                  dict(pre=False, p=0.2), dict(per_gate=150, beta=True), dict(norm="layer", pre=False, in_place=True)],
+                         ids=str)
+def test_coupling_of_the_widest_rows_in_several_rounds(over, width, dtype):
+    """More rows than workgroups, so that each takes several."""
+    print("case", over, width, dtype, flush=True)
+    coupling(dtype, 300, width, **over)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dim", [32, 72, 96])
+@pytest.mark.parametrize("kv_len", [1500, 9000])
+def test_attention_single_tokens_over_many_splits(kv_len, dim, dtype):
+    """12 and 64 splits, most of them empty for the shorter requests."""
+    print("case", kv_len, dim, dtype, flush=True)
+    check(*attention(dtype, 3, 1, kv_len, 4, 2, dim, True, ([1, 1, 1], [kv_len, 0, 130]), poison=True, backward=False), dtype)
+    check(*attention(dtype, 1, 1, kv_len, 4, 2, dim, lens=([1], [kv_len - 77]), poison=True), dtype)
