@@ -273,3 +273,23 @@ def test_attention_single_tokens_over_many_splits(kv_len, dim, dtype):
     print("case", kv_len, dim, dtype, flush=True)
     check(*attention(dtype, 3, 1, kv_len, 4, 2, dim, True, ([1, 1, 1], [kv_len, 0, 130]), poison=True, backward=False), dtype)
     check(*attention(dtype, 1, 1, kv_len, 4, 2, dim, lens=([1], [kv_len - 77]), poison=True), dtype)
+
+
+def test_attention_gradient_strides_of_dimensions_of_one_mean_nothing():
+    from paper_2406_02052_amd import Attention
+
+    b, nk, h, kvh, d = 2, 70, 4, 2, 64
+    q, k, v, g = draw(9, (b, 1, h, d), (b, nk, kvh, d), (b, nk, kvh, d), (b, 1, h, d), dtype="bf16")
+    want = T.attention(q, k, v, 1 / math.sqrt(d), d_o=g)
+    tq, tk, tv, tg = (dev(x, "bf16") for x in (q, k, v, g))
+    tg = tg.reshape(b, h, 1, d).transpose(1, 2)          # the same memory, another stride of the one token
+    o, lse = torch.empty_like(tq, memory_format=torch.contiguous_format), torch.empty(b, h, 1, device="cuda")
+    assert tg.shape == o.shape and tg.stride() != o.stride() and tg.is_contiguous()
+    dq = torch.full((b, h, 1, d), math.nan, dtype=torch.bfloat16, device="cuda").transpose(1, 2)
+    dk, dv = like(tk), like(tv)
+    op = Attention(b, 1, nk, h, kvh, d)
+    op.forward(tq, tk, tv, o, lse)
+    op.backward(tq, tk, tv, o, lse, tg, dq, dk, dv)
+    check([o, lse, dq, dk, dv], want, "bf16")
+    with pytest.raises(ValueError):                      # another stride of the heads does mean something
+        op.backward(tq, tk, tv, o, lse, torch.empty(b, 1, h, 2 * d, dtype=torch.bfloat16, device="cuda")[..., :d], dq, dk, dv)
