@@ -462,8 +462,15 @@ petra_status petra_coupling_forward(const petra_coupling_desc* desc, const void*
     need_apart(sy, su);
     need_apart(su, sf, true);
     need_apart(su, sx);
-    need_apart(sy, sg);
-    need_apart(su, sg);
+    const Span params[5] = {sg,
+                            {f != nullptr ? post->gamma : nullptr, t.param, "post.gamma"},
+                            {f != nullptr ? post->beta : nullptr, t.param, "post.beta"},
+                            {u != nullptr ? pre->gamma : nullptr, t.param, "pre.gamma"},
+                            {u != nullptr ? pre->beta : nullptr, t.param, "pre.beta"}};
+    for (const Span& p : params) {
+      need_apart(sy, p);
+      need_apart(su, p);
+    }
     if (empty) return false;
     t.a.x = x;
     t.a.f = f;

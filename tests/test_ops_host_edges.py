@@ -136,3 +136,16 @@ def test_current_stream_by_the_public_call_where_torch_has_no_other(monkeypatch)
     monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
     assert L._stream(None) == 77
     assert L._stream(Stream()) == 77 and L._stream(5) == 5
+
+
+@pytest.mark.parametrize("out", ["y", "u"])
+@pytest.mark.parametrize("param", ["gate", "post.gamma", "post.beta", "pre.gamma", "pre.beta"])
+def test_coupling_outputs_over_parameters(param, out):
+    d = L.CouplingDesc(12, 0, 64, L.PETRA_BF16, L.PETRA_NORM_LAYER, 1e-5, 1.0, 0.0)
+    at = {"x": FAR[0], "f": FAR[1], "gate": FAR[2], "post.gamma": FAR[3], "post.beta": FAR[4], "pre.gamma": FAR[5],
+          "pre.beta": FAR[6], "y": FAR[7], "u": FAR[8]}
+    at[out] = at[param] - 12 * 64 * 2 + 16       # the last 8 of its elements over the first of the parameter
+    call = lambda: L.petra_coupling_forward(  # noqa: E731
+        d, at["x"], at["f"], at["gate"], (at["post.gamma"], at["post.beta"]), (at["pre.gamma"], at["pre.beta"]), 0,
+        at["y"], at["u"], 0)
+    assert status(call) == "PETRA_ERR_ALIAS"
