@@ -150,15 +150,20 @@ struct Stager {
     }
   }
   // Rows of a key head's queries from row `first`, of `left` rows: token row / group, head row % group.
-  // Zeros in place of the first `dead` rows.
-  __device__ __forceinline__ void queries(int64_t st, int64_t sh, int first, int dead, int left, int group, int dim) {
+  __device__ __forceinline__ void queries(int64_t st, int64_t sh, int first, int left, int group, int dim) {
     const int token0 = first / group;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int c = chunk_offset(i, dim), r = first + row(i), token = r / group;
       const int64_t o = ((token - token0) * st + (r - token * group) * sh) * static_cast<int64_t>(sizeof(T));
-      off[i] = c < 0 || row(i) < dead || row(i) >= left ? BUF_OOB : static_cast<uint32_t>(o) + c;
+      off[i] = c < 0 || row(i) >= left ? BUF_OOB : static_cast<uint32_t>(o) + c;
     }
+  }
+  // Zeros in place of the tile's first n rows.
+  __device__ __forceinline__ void skip(int n) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (row(i) < n) off[i] = BUF_OOB;
   }
   // The loads are written out: the compiler would let every later transposing LDS read wait for them,
   // those of the other buffer too.  They write no register, and arrived() waits for them.
@@ -836,14 +841,19 @@ __global__ __launch_bounds__(64 * WC, (DP * sizeof(T) > 128 ? 1 : 2)) void attn_
   const T* const gb = at<T>(a.d_o, a.o_stride, w.b, 0, w.kvh * a.group);
   Stager<T, DP, RT, THREADS> sq, sg;
   const bool same = RT % a.group == 0;   // every whole tile has the same offsets
-  // rows that see no key at all, staged as zeros: only the first tile can have such
-  const int blind = a.causal && w.q_len > w.kv_len ? (w.q_len - w.kv_len) * a.group : 0;
+  auto lay = [&](int r0, int left) {
+    sq.queries(a.q_stride[1], a.q_stride[2], r0, left, a.group, a.dim);
+    sg.queries(a.o_stride[1], a.o_stride[2], r0, left, a.group, a.dim);
+  };
   const int64_t stat0 = static_cast<int64_t>(bh) * a.q_len * a.group;
-  auto stage = [&](int t, bool offsets) {
+  auto stage = [&](int t, bool first_tile) {
     const int r0 = t * RT, left = rows - r0, token0 = r0 / a.group;
-    if (offsets || !same || left < RT || r0 - RT < blind) {
-      sq.queries(a.q_stride[1], a.q_stride[2], r0, blind - r0, left, a.group, a.dim);
-      sg.queries(a.o_stride[1], a.o_stride[2], r0, blind - r0, left, a.group, a.dim);
+    if (first_tile || !same || left < RT) lay(r0, left);
+    // rows that see no key at all are staged as zeros: only the first tile can have such
+    const int blind = first_tile && a.causal && w.q_len > w.kv_len ? (w.q_len - w.kv_len) * a.group - r0 : 0;
+    if (blind > 0) {
+      sq.skip(blind);
+      sg.skip(blind);
     }
     char* const to = lds + (t & 1) * BUFFER;
     sq.load(qb + token0 * a.q_stride[1], 0x7fffffffu, to);
@@ -852,6 +862,7 @@ __global__ __launch_bounds__(64 * WC, (DP * sizeof(T) > 128 ? 1 : 2)) void attn_
     const int bytes = (left < RT ? left : RT) * 4;
     if (wave == 0) stage_floats(a.stat_lse + stat0 + r0, bytes, st);
     if (wave == 1) stage_floats(a.stat_delta + stat0 + r0, bytes, st + 64);
+    if (blind > 0) lay(r0, left);
   };
   if (t0 < t1) stage(t0, true);
 
