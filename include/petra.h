@@ -420,12 +420,18 @@ petra_status petra_net_backprop_step(petra_net* net, const void* images, const i
  *   o_i = sum_j m_ij p_ij v_j
  * Visible are the keys j < kv_lens[b], and with `causal` j <= i + kv_lens[b] -
  * q_lens[b] (the last query sees every key).  A query without visible keys, or
- * at or past q_lens[b], has o = 0, lse = -inf and takes no part in any gradient.
- * Nothing at or past the lengths is used, whatever it holds; keys that the
- * causal mask alone hides from a query enter its sums times zero and have to be
- * finite.  m is dropout's 0
- * or 1 / (share kept); its groups are, for each row (b, h, i), the keys 16 a +
- * 4 c + {0, 1, 2, 3, 8, 9, 10, 11} for c = 0, 1, in the order (b, h, i, a, c).
+ * at or past q_lens[b], has o = 0, lse = -inf and takes no part in any gradient,
+ * whatever it and its d_o hold; so has one whose scores are all -inf.  Nothing at
+ * or past the lengths is used, whatever it holds; keys that the causal mask alone
+ * hides from a query that sees others enter its sums times zero and have to be
+ * finite.  A NaN query, or one that sees a NaN key, has o = lse = NaN.  m is
+ * dropout's 0 or 1 / (share kept); its groups are, for each row (b, h, i), the keys
+ * 16 a + 4 c + {0, 1, 2, 3, 8, 9, 10, 11} for c = 0, 1, in the order (b, h, i, a, c).
+ *
+ * Scores, statistics and sums are fp32.  With bf16 tensors p and the backward's
+ * gradients of the scores are rounded to bf16 as operands of the products that
+ * follow, and the backward takes o as stored: results are off by about 1.3 times
+ * (gradients 1.4 times) what rounding them alone to bf16 would give.
  *
  * Layout: tensors [batch][q_len or kv_len][heads or kv_heads][head_dim] with the
  * given strides, in elements, of the first three dimensions (all three zero:
@@ -437,8 +443,10 @@ petra_status petra_net_backprop_step(petra_net* net, const void* images, const i
  * are refused.
  * Limits: heads a multiple of kv_heads; head_dim a multiple of 8, at most 128;
  * strides not negative and multiples of 16 bytes, those of written tensors such
- * that no elements share memory, a token stride of k and v below 2^22 elements;
- * q_len * heads / kv_heads and kv_len at most 2^30, batch * kv_heads at most
+ * that no elements share memory, a token stride of k and v of head_dim or more and
+ * below 2^22 elements, in the backward 64 token strides and heads / kv_heads head
+ * strides of q and of o together below 2^31 bytes, no tensor from end to end 2^47 bytes
+ * or more; q_len * heads / kv_heads and kv_len at most 2^30, batch * kv_heads at most
  * 65535; scale > 0. */
 typedef struct {
   int32_t batch, q_len, kv_len;

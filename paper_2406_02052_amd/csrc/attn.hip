@@ -216,7 +216,7 @@ __device__ __forceinline__ void in_turn(int t0, int t1, F body) {
 
 // What this workgroup works on: (batch row, key head), split, tile.  Splits and heads run
 // fastest: workgroups go to the 8 XCDs in turn, so that with a multiple of 8 heads each XCD's
-// L2 has the keys of its own (2 x 4096 causal tokens, 16 heads: 165 us, 204 with the tiles
+// L2 has the keys of its own (2 x 4096 causal tokens, 16 heads: 147 us, 227 with the tiles
 // fastest), and the workgroups of a short sequence, which end at once, lie between others';
 // tiles run slowest, from the one with most visible pairs where the mask is causal, so that
 // what is left for the end is short.
@@ -635,8 +635,9 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a) {
 // ---------------------------------------------------------------------------
 
 // Three products a pair, each with one operand in registers (q, do, or what the last two left) and one from
-// LDS; two waves a SIMD.  2 x 4096 causal tokens, 16 heads of 128 over 4: 213 us, 970 TFLOP/s, matrix
-// instructions busy 60 % of the time.
+// LDS; two waves a SIMD (one for the 64-row kernel of 128 channels, whose two waves have 64 KB of LDS between
+// them).  2 x 4096 causal tokens, 16 heads of 128 over 4: 210 us, 980 TFLOP/s, matrix instructions busy 60 % of
+// the time.
 template <typename T, int DP, int WR, int KB, bool DROP>
 __global__ __launch_bounds__(64 * WR, (DP * sizeof(T) > 256 ? 1 : 2)) void attn_dq_kernel(AttnArgs a) {
   using Tl = Tile<T, DP>;
@@ -1120,12 +1121,17 @@ int splits_for(int64_t blocks, int64_t slots, int64_t length, int64_t least) {
 
 }  // namespace
 
-AttnPlan attn_plan(const AttnArgs& a, int) {
+AttnPlan attn_plan(const AttnArgs& a) {
   AttnPlan p{};
   const int64_t rows = static_cast<int64_t>(a.q_len) * a.group, bh = static_cast<int64_t>(a.batch) * a.kv_heads;
   // 128 rows or keys a workgroup share what it brings to LDS; more small workgroups in place of splits
   // are slower (5 x 1000 ragged tokens: dk and dv 72 us by 64 keys, 46 by 128), unless 64 is all there is
   p.row_tile = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  // 256 slots by 64 and 128 rows, where 512 are slower (777 over 1023 fp32 ragged 40 us against 30, 1000 over 4000, 8
+  // heads of 64, 29 against 26, its gradients by 32 channels 75 against 66).  By 32 rows neither is best throughout,
+  // whatever the type and width: single tokens over 4097 keys, 4 key heads, 512 against 256: 8 requests 15 / 14
+  // (128 channels 25 / 21, fp32 79 / 62); 48: 42 / 38 (fp32 99 / 119; 128 channels 84 / 93, fp32 294 / 328); 160: 153 / 129
+  // (fp32 282 / 350; 128 channels 253 / 290, fp32 822 / 941), ragged 73 / 76; 128 ragged 56 / 60.
   p.splits = splits_for(ceil_div(rows, p.row_tile) * bh, p.row_tile == 32 ? 512 : 256, a.kv_len, 128);
   p.dq_tile = rows <= 64 ? 64 : 128;
   p.key_tile = a.kv_len <= 64 ? 64 : 128;

@@ -179,7 +179,10 @@ __global__ __launch_bounds__(Team<TEAM>::THREADS) void couple_forward_kernel(Cou
 // kernel adds those rows, also in a fixed order: results do not depend on timing.
 // Spans hold whole gates (their dgate is written at once) or a part of one gate; with
 // a gate a row, a row's dgate is written with the row.  The next row's tensors are
-// asked for before this one's sums, which wait for the team's waves.
+// asked for before this one's sums, which wait for the team's waves.  All teams of a
+// workgroup are at one gate: gates of fewer rows than it has teams leave some idle (524288 x
+// 64 bf16, 32 teams: 1012 us with 2 rows a gate, 531 with 4, 172 with 16; one gate 100, a
+// gate a row 153).
 // FULL: a layer norm or a beta (the sums that only those need).
 // 4 reads and 3 writes an element: 16384 x 2048 bf16 with dropout in 95 us and 4.8 for the second
 // kernel, 4.7 TB/s; without the next row fetched ahead, and with a barrier more for each sum, 188.
@@ -187,7 +190,9 @@ template <typename T, int TEAM, bool FULL, bool DROP, bool PRE>
 __global__ __launch_bounds__(Team<TEAM>::THREADS) void couple_backward_kernel(CoupleArgs a) {
   using Tm = Team<TEAM>;
   constexpr int TEAMS = Tm::TEAMS, THREADS = Tm::THREADS;
-  // 1024 lanes have 128 registers each: no room for the next row, nor for the parameters
+  // 1024 lanes have 128 registers each: no room for the next row, nor for the parameters.  The sums alone
+  // leave too few: all but the forms without u, layer norm and beta spill, up to 122 registers (4096 x 8192
+  // bf16: rms 174 us, layer 434, memory's share 89; 8192 x 4096, by 512 lanes, 105)
   constexpr bool LEAN = TEAM == 1024;
   // partial sums of the teams, one parameter at a time
   __shared__ float joined[TEAMS > 1 ? THREADS * 8 : 1];

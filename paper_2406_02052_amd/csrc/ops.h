@@ -66,7 +66,7 @@ struct AttnPlan {
   size_t stat_bytes, bwd_bytes;
 };
 
-AttnPlan attn_plan(const AttnArgs& a, int dtype);
+AttnPlan attn_plan(const AttnArgs& a);
 void attn_forward(const AttnArgs& a, const AttnPlan& p, int dtype, void* workspace, hipStream_t s);
 void attn_backward(const AttnArgs& a, const AttnPlan& p, int dtype, void* workspace, hipStream_t s);
 

@@ -264,7 +264,7 @@ struct Attn {
       need_distinct(a.k_stride, nk, a.dim, "dk");
       need_distinct(a.v_stride, nk, a.dim, "dv");
     }
-    plan = petra::attn_plan(a, d->dtype);
+    plan = petra::attn_plan(a);
   }
 
   // The memory of q, k, v, o or what is laid out like it, and of lse.
