@@ -394,7 +394,8 @@ petra_status petra_net_backprop_step(petra_net* net, const void* images, const i
 
 /* ------------------------------------------------------------------------
  * Operators of stages over tokens: attention, the coupling of a residual
- * function to its stream with norms, gate and residual scale, and dropout.
+ * function to its stream with norms, gate and residual scale, dropout, the norms
+ * and rotation of heads, the loss over a vocabulary and the AdamW step.
  *
  * They are stateless: a description, device pointers and a stream a call, no
  * handle.  The conventions above hold (the caller owns all memory, workspaces
@@ -535,6 +536,146 @@ petra_status petra_coupling_backward(const petra_coupling_desc* desc, const void
  * overlap with them. */
 petra_status petra_dropout(int64_t n, int32_t dtype, float p, float alpha, const void* x,
                            const void* residual, const uint64_t* rng, void* y, void* stream);
+
+/* Norms of query and key heads with the rotation by their tokens' positions, between the
+ * product that forms them and the attention.  For each head's channels x of a token:
+ *   z = n(x; norm),  (y_a, y_b) = (z_a cos t - z_b sin t, z_a sin t + z_b cos t)
+ * for its pairs (a, b) of channels, t = freq[i] position[axis[i]] for pair i < pairs; channels in
+ * no pair are not rotated.  n is over the head's channels, as in petra_coupling_desc, with one
+ * gamma (and beta, nullable) [head_dim] for all query heads and one for all key heads; without
+ * (NULL) n(x) = x.  With several axes (time, height and width of images, say) a pair
+ * turns by the position on its own.  Angles are exact to 2^-32 of a turn for every position.
+ *
+ * Layout: q [batch][len][heads][head_dim], k [batch][len][kv_heads][head_dim] with the given
+ * strides as in petra_attn_desc, the results likewise (all three zero: contiguous).  kv_heads = 0:
+ * queries only.  positions: device int32 [axes][batch][len], any values (NULL: a token's index in
+ * its sequence, on every axis).  Limits: head_dim a multiple of 8, at most 128; pairs a multiple of 4,
+ * at most head_dim / 2; batch * len below 2^31; strides not negative and multiples of 16 bytes, those
+ * of written tensors such that no elements share memory. */
+enum { PETRA_HEAD_AXES = 4, PETRA_HEAD_PAIRS = 64 };
+
+typedef enum {
+  PETRA_PAIRS_HALVES = 0,      /* channels (i, i + pairs)   */
+  PETRA_PAIRS_NEIGHBOURS = 1   /* channels (2 i, 2 i + 1)   */
+} petra_pairs;
+
+typedef struct {
+  int32_t batch, len;
+  int32_t heads, kv_heads, head_dim;
+  int32_t dtype;                     /* petra_dtype */
+  int32_t norm;                      /* petra_norm */
+  float eps;                         /* > 0 */
+  int32_t layout;                    /* petra_pairs */
+  int32_t pairs, axes;               /* 1 <= axes <= PETRA_HEAD_AXES */
+  int32_t axis[PETRA_HEAD_PAIRS];    /* of each pair, below axes */
+  double freq[PETRA_HEAD_PAIRS];     /* of each pair, radians a position */
+  int64_t q_stride[3], k_stride[3], yq_stride[3], yk_stride[3];   /* batch, token, head */
+} petra_heads_desc;
+
+/* Workspace of the backward, in bytes. */
+petra_status petra_heads_query(const petra_heads_desc* desc, size_t* backward_bytes);
+/* Writes yq and yk.  yq == q and yk == k with the same strides are allowed; no other overlap. */
+petra_status petra_heads_forward(const petra_heads_desc* desc, const void* q, const void* k,
+                                 const petra_norm_params* q_norm, const petra_norm_params* k_norm,
+                                 const int32_t* positions, void* yq, void* yk, void* stream);
+/* From the forward's inputs and the gradients dyq, dyk (laid out like yq, yk): dq, dk (laid out
+ * like q, k) and the gradients of the norms' parameters, written, not added.  Without a norm the
+ * tensor itself (q, k) is not read.  dq == q, and dq == dyq with the same strides, are allowed
+ * (and for k); no other overlap. */
+petra_status petra_heads_backward(const petra_heads_desc* desc, const void* q, const void* k,
+                                  const petra_norm_params* q_norm,
+                                  const petra_norm_params* k_norm, const int32_t* positions,
+                                  const void* dyq, const void* dyk, void* dq, void* dk,
+                                  const petra_norm_params* dq_norm,
+                                  const petra_norm_params* dk_norm, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/* The loss of a last stage over a large vocabulary: softmax cross entropy of x W^T and its
+ * gradients, without a rows x vocab tensor.  For the rows x_i [width] and their targets t_i:
+ *   s_ij = scale x_i . w_j,  lse_i = log sum_j exp s_ij,  loss_i = lse_i - s_it
+ *   L = sum_i weight_i loss_i,  dx = dL/dx,  dw = dL/dw (written, not added)
+ * A row whose target is not in 0 .. vocab - 1 takes no part, whatever it holds: its loss, lse and
+ * dx are 0.  weight: device fp32 [rows]; NULL: the mean, 1 / (the rows that take part).
+ *
+ * Rows are worked on in pieces (piece_rows at a time; 0: as many as keep a piece's scores within 1 GiB), whose
+ * gradients of w are summed in fp32.  Scores, statistics and sums are fp32.  With bf16 tensors the softmax
+ * and the weighted rows are rounded to bf16 as operands of the gradients' products: these are off by
+ * about 1.3 times what rounding them alone to bf16 would give.
+ * x, dx [rows][width] and w, dw [vocab][width] are contiguous, targets int32 [rows].
+ * Limits: width a multiple of 8, at most 65536; 1 <= vocab <= 2^20; rows at most 2^30; scale > 0. */
+typedef struct {
+  int64_t rows;
+  int64_t piece_rows;
+  int32_t width, vocab;
+  int32_t dtype;          /* petra_dtype */
+  float scale;
+} petra_vocab_desc;
+
+/* Workspace of the two calls, in bytes. */
+petra_status petra_vocab_query(const petra_vocab_desc* desc, size_t* loss_bytes,
+                               size_t* gradient_bytes);
+/* Writes loss and lse (fp32 [rows]) only. */
+petra_status petra_vocab_loss(const petra_vocab_desc* desc, const void* x, const void* w,
+                              const int32_t* targets, float* loss, float* lse, void* workspace,
+                              size_t workspace_bytes, void* stream);
+/* Writes loss, lse, dx and dw: forward and backward in one, three products of the scores' size. */
+petra_status petra_vocab_gradient(const petra_vocab_desc* desc, const void* x, const void* w,
+                                  const int32_t* targets, const float* weight, float* loss,
+                                  float* lse, void* dx, void* dw, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/* AdamW over many tensors at once, the update of stages over tokens:
+ *   g = grad_scale grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   theta -= lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay theta)
+ * for t = steps + 1, all in fp32 (the corrections in fp64).  Gradients are fp32 or bf16; a bf16
+ * copy of theta for the forward is written along where one is given.
+ *
+ * States are fp32, or with PETRA_E4M3 8 bits: blocks of 64 elements of m, and of r = sqrt(v), as
+ * e4m3 numbers (4 exponent and 3 mantissa bits) times the block's scale, the power of two that
+ * brings its largest magnitude into [128, 256).  A value is rounded up or down at random to its
+ * neighbours in the format, such that m and v are kept on average (v's changes by a step are far
+ * smaller than the format's); r of v > 0 stays above 0.  An element's 2 x 16 random bits are Philox's, as
+ * for dropout: groups are of 4 elements, element e takes bits 32 e .. 32 e + 15 for m and the 16 above for r;
+ * a tensor's groups follow those of the tensor before it, its length rounded up to 64.  A step with the same rng
+ * rounds alike; a new step takes a new offset.  An infinite or NaN gradient
+ * leaves NaN in its own element.
+ *
+ * The tensors are laid out once: petra_adamw_layout writes a table, which the caller copies to
+ * device memory (16-byte aligned) and keeps, with the tensors, as long as it steps.
+ * Limits: n >= 0, count at most 2^20, all chunks of 4096 elements below 2^31. */
+enum { PETRA_E4M3 = 2 };   /* state_dtype only */
+
+typedef struct {
+  float* theta;
+  void* grad;
+  void *m, *v;                /* fp32 [n], or bytes [n rounded up to 64] */
+  float *m_scale, *v_scale;   /* 8 bits only: [n / 64 rounded up], 4-byte aligned */
+  void* copy;                 /* bf16 [n], nullable */
+  int64_t n;
+  float weight_decay;
+} petra_adamw_tensor;
+
+typedef struct {
+  double beta1, beta2;        /* in [0, 1) */
+  float eps;                  /* > 0 */
+  int32_t grad_dtype;         /* PETRA_FP32 or PETRA_BF16 */
+  int32_t state_dtype;        /* PETRA_FP32 or PETRA_E4M3 */
+  int32_t zero_grads;         /* gradients are set to 0 as they are read */
+} petra_adamw_desc;
+
+/* Bytes of the table of these tensors, its chunks (both for petra_adamw_step) and the step's workspace. */
+petra_status petra_adamw_query(const petra_adamw_desc* desc, const petra_adamw_tensor* tensors,
+                               int64_t count, size_t* table_bytes, int64_t* chunks,
+                               size_t* workspace_bytes);
+/* Checks the tensors and writes their table to host memory. */
+petra_status petra_adamw_layout(const petra_adamw_desc* desc, const petra_adamw_tensor* tensors,
+                                int64_t count, void* table, size_t table_bytes);
+/* One step of all tensors.  steps (int64: the steps done, advanced by the call), lr, grad_scale
+ * (fp32, nullable: 1) and rng are device memory, so that a captured step may be replayed. */
+petra_status petra_adamw_step(const petra_adamw_desc* desc, const void* table, size_t table_bytes,
+                              int64_t count, int64_t chunks, int64_t* steps, const float* lr,
+                              const float* grad_scale, const uint64_t* rng, void* workspace,
+                              size_t workspace_bytes, void* stream);
 
 /* Measurement support (not part of the method).  petra_stage_profile(st, 1)
  * clears the counters and starts bracketing every kernel launch of the stage

@@ -1,5 +1,6 @@
-"""Operators of stages over tokens in fp64 (numpy): dropout's generator, attention
-and the gated norm coupling with their gradients, each from its formula."""
+"""Operators of stages over tokens in fp64 (numpy): dropout's generator, attention,
+the gated norm coupling, head norms with rotation and the loss over a vocabulary with
+their gradients, and AdamW, each from its formula."""
 import numpy as np
 
 
@@ -144,3 +145,101 @@ def coupling_backward(y, f, dy, gate, post, norm, eps, scale, mask=None, du=None
     out.update(x=(y - g * n) / scale, df=unit_backward(dn * post[0], fn, r, norm),
                dgate=(t * n).reshape(gate.shape[0], -1, w).sum(1), dpost=((dn * fn).sum(0), dn.sum(0)))
     return out
+
+
+# ---- head norms and rotation -------------------------------------------------
+
+def rotate(z, positions, freq, axis, layout):
+    """z [batch, len, heads, dim], positions [axes][batch, len]."""
+    y, n = np.array(z, float), len(freq)
+    for i in range(n):
+        a, b = (i, i + n) if layout == "halves" else (2 * i, 2 * i + 1)
+        # whole turns apart in long double: far positions keep their fraction
+        t = np.asarray(positions[axis[i]], np.longdouble) * np.longdouble(freq[i])
+        t = np.remainder(t, 2 * np.longdouble("3.14159265358979323846264338327950288")).astype(float)[:, :, None]
+        y[..., a] = z[..., a] * np.cos(t) - z[..., b] * np.sin(t)
+        y[..., b] = z[..., a] * np.sin(t) + z[..., b] * np.cos(t)
+    return y
+
+
+def head_norm(x, params, kind, eps, positions, freq, axis, layout, dy=None):
+    """y, or with dy (dx, dgamma, dbeta); params (gamma, beta or None), or None for no norm."""
+    if params is None:
+        return rotate(x, positions, freq, axis, layout) if dy is None else (
+            rotate(dy, positions, [-f for f in freq], axis, layout), None, None)
+    z = x - x.mean(-1, keepdims=True) if kind == "layer" else x
+    r = 1.0 / np.sqrt((z * z).mean(-1, keepdims=True) + eps)
+    z = z * r
+    gamma, beta = params
+    if dy is None:
+        return rotate(z * gamma + (0.0 if beta is None else beta), positions, freq, axis, layout)
+    g = rotate(dy, positions, [-f for f in freq], axis, layout)
+    h = g * gamma
+    dx = h - z * (h * z).mean(-1, keepdims=True)
+    if kind == "layer":
+        dx = dx - h.mean(-1, keepdims=True)
+    return r * dx, (g * z).sum((0, 1, 2)), None if beta is None else g.sum((0, 1, 2))
+
+
+# ---- loss over a vocabulary ---------------------------------------------------
+
+def vocab_loss(x, w, targets, scale=1.0, weight=None):
+    """loss, lse, dx, dw of sum(weight loss); rows whose target is no column take no part."""
+    rows, vocab = len(x), len(w)
+    live = np.array([0 <= t < vocab for t in targets], bool)
+    at = np.flatnonzero(live)
+    loss, lse, dx = np.zeros(rows), np.zeros(rows), np.zeros(x.shape)
+    dw = np.zeros(w.shape)
+    if len(at):
+        t = np.asarray(targets)[at]
+        s = scale * (x[at] @ w.T)
+        top = s.max(1)
+        lse[at] = top + np.log(np.exp(s - top[:, None]).sum(1))
+        loss[at] = lse[at] - s[np.arange(len(at)), t]
+        p = np.exp(s - lse[at, None])
+        p[np.arange(len(at)), t] -= 1.0
+        p *= scale * (np.full(len(at), 1.0 / len(at)) if weight is None else np.asarray(weight)[at])[:, None]
+        dx[at], dw = p @ w, p.T @ x[at]
+    return loss, lse, dx, dw
+
+
+# ---- AdamW --------------------------------------------------------------------
+
+E4M3 = np.array([0.0] + [i / 8 * 2.0 ** -6 for i in range(1, 8)]
+                + [(1 + i / 8) * 2.0 ** e for e in range(-6, 9) for i in range(8)][:119])
+
+
+def adamw(theta, grad, m, v, t, lr, betas, eps, decay, grad_scale=1.0):
+    """theta, m, v after step t (from 1)."""
+    g = grad_scale * grad
+    m = betas[0] * m + (1 - betas[0]) * g
+    v = betas[1] * v + (1 - betas[1]) * g * g
+    step = m / (1 - betas[0] ** t) / (np.sqrt(v / (1 - betas[1] ** t)) + eps)
+    return theta - lr * (step + decay * theta), m, v
+
+
+def hold(x, power, u, scale=None):
+    """|x| by blocks of 64 (padded with zeros) in e4m3 with a power of two as the scale (or the one
+    that is given): (numbers, scales).  u in [0, 1) decides between neighbours such that x^power is
+    kept on average."""
+    n = len(x)
+    a = np.zeros(-(-n // 64) * 64)
+    a[:n] = np.abs(x)
+    blocks = a.reshape(-1, 64)
+    top = blocks.max(1)
+    if scale is None:
+        scale = np.where(top > 0, 2.0 ** (np.floor(np.log2(np.where(top > 0, top, 1.0))) - 7), 0.0)
+    y = blocks / np.where(scale > 0, scale, 1.0)[:, None]
+    lo = np.searchsorted(E4M3, y, side="right") - 1
+    b0, b1 = E4M3[lo] ** power, E4M3[lo + 1] ** power
+    up = np.asarray(u).reshape(y.shape) * (b1 - b0) < y ** power - b0
+    q = E4M3[lo + up]
+    if power == 2:
+        q = np.where(y > 0, np.maximum(q, E4M3[1]), q)
+    return q.reshape(-1), scale
+
+
+def adamw_numbers(rng, first_group, n):
+    """The two random numbers of each of n elements (a multiple of 4) from a group of 4 on."""
+    bits = group_bits(rng, first_group + np.arange(n // 4)).reshape(-1, 2)
+    return bits[:, 0] / 65536.0, bits[:, 1] / 65536.0

@@ -16,4 +16,4 @@ from ._lib import *  # noqa: F401,F403,E402  (the petra_* wrappers, same names a
 _lib.load()
 
 from .stage import Net, Stage, to_host  # noqa: E402,F401
-from .ops import Attention, Coupling, dropout  # noqa: E402,F401
+from .ops import AdamW, Attention, Coupling, HeadNorm, VocabLoss, dropout  # noqa: E402,F401

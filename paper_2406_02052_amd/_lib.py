@@ -92,6 +92,40 @@ class NormParams(ctypes.Structure):
 
 
 PETRA_NORM_RMS, PETRA_NORM_LAYER = 0, 1
+PETRA_PAIRS_HALVES, PETRA_PAIRS_NEIGHBOURS = 0, 1
+PETRA_HEAD_AXES, PETRA_HEAD_PAIRS = 4, 64
+PETRA_E4M3 = 2
+
+
+class HeadsDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("len", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("norm", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("layout", ctypes.c_int32), ("pairs", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("axis", ctypes.c_int32 * PETRA_HEAD_PAIRS),
+                ("freq", ctypes.c_double * PETRA_HEAD_PAIRS), ("q_stride", ctypes.c_int64 * 3),
+                ("k_stride", ctypes.c_int64 * 3), ("yq_stride", ctypes.c_int64 * 3),
+                ("yk_stride", ctypes.c_int64 * 3)]
+
+
+class VocabDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("piece_rows", ctypes.c_int64),
+                ("width", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("weight_decay", ctypes.c_float)]
+
+
+class AdamwDesc(ctypes.Structure):
+    _fields_ = [("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_float),
+                ("grad_dtype", ctypes.c_int32), ("state_dtype", ctypes.c_int32),
+                ("zero_grads", ctypes.c_int32)]
+
 
 # petra_bwd_mode
 BWD_RECONSTRUCT, BWD_INPUT_BUFFER, BWD_PARAM_BUFFER, BWD_DELAYED = 0, 1, 2, 3
@@ -156,6 +190,31 @@ _SIGS = {
                                 [ctypes.POINTER(NormParams)] * 2 + [_VP, ctypes.c_size_t, _VP]),
     "petra_dropout": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_float,
                                      ctypes.c_float, _VP, _VP, _VP, _VP, _VP]),
+    "petra_heads_query": (ctypes.c_int, [ctypes.POINTER(HeadsDesc),
+                                         ctypes.POINTER(ctypes.c_size_t)]),
+    "petra_heads_forward": (ctypes.c_int, [ctypes.POINTER(HeadsDesc), _VP, _VP,
+                                           ctypes.POINTER(NormParams),
+                                           ctypes.POINTER(NormParams), _VP, _VP, _VP, _VP]),
+    "petra_heads_backward": (ctypes.c_int, [ctypes.POINTER(HeadsDesc), _VP, _VP,
+                                            ctypes.POINTER(NormParams),
+                                            ctypes.POINTER(NormParams)] + [_VP] * 5 +
+                             [ctypes.POINTER(NormParams)] * 2 + [_VP, ctypes.c_size_t, _VP]),
+    "petra_vocab_query": (ctypes.c_int, [ctypes.POINTER(VocabDesc),
+                                         ctypes.POINTER(ctypes.c_size_t),
+                                         ctypes.POINTER(ctypes.c_size_t)]),
+    "petra_vocab_loss": (ctypes.c_int, [ctypes.POINTER(VocabDesc)] + [_VP] * 6 +
+                         [ctypes.c_size_t, _VP]),
+    "petra_vocab_gradient": (ctypes.c_int, [ctypes.POINTER(VocabDesc)] + [_VP] * 9 +
+                             [ctypes.c_size_t, _VP]),
+    "petra_adamw_query": (ctypes.c_int, [ctypes.POINTER(AdamwDesc), ctypes.POINTER(AdamwTensor),
+                                         ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t),
+                                         ctypes.POINTER(ctypes.c_int64),
+                                         ctypes.POINTER(ctypes.c_size_t)]),
+    "petra_adamw_layout": (ctypes.c_int, [ctypes.POINTER(AdamwDesc), ctypes.POINTER(AdamwTensor),
+                                          ctypes.c_int64, _VP, ctypes.c_size_t]),
+    "petra_adamw_step": (ctypes.c_int, [ctypes.POINTER(AdamwDesc), _VP, ctypes.c_size_t,
+                                        ctypes.c_int64, ctypes.c_int64] + [_VP] * 5 +
+                         [ctypes.c_size_t, _VP]),
     "petra_stage_forward_noalloc": (ctypes.c_int, [_VP, _VP, _VP, _VP, _VP, _VP]),
     "petra_stage_profile": (ctypes.c_int, [_VP, ctypes.c_int32]),
     "petra_stage_profile_read": (ctypes.c_int, [_VP, ctypes.c_int32,
@@ -516,3 +575,70 @@ def petra_dropout(n: int, dtype: int, p: float, alpha: float, x, residual, rng, 
                   stream=None) -> None:
     _check(load().petra_dropout(n, dtype, p, alpha, _ptr(x), _ptr(residual), _ptr(rng), _ptr(y),
                                 _stream(stream)), "petra_dropout")
+
+
+def petra_heads_query(desc: HeadsDesc) -> int:
+    n = ctypes.c_size_t()
+    _check(load().petra_heads_query(ctypes.byref(desc), ctypes.byref(n)), "petra_heads_query")
+    return n.value
+
+
+def petra_heads_forward(desc: HeadsDesc, q, k, q_norm, k_norm, positions, yq, yk,
+                        stream=None) -> None:
+    """q_norm and k_norm: (gamma, beta or None), or None."""
+    _check(load().petra_heads_forward(ctypes.byref(desc), _ptr(q), _ptr(k), _norm(q_norm),
+                                      _norm(k_norm), _ptr(positions), _ptr(yq), _ptr(yk),
+                                      _stream(stream)), "petra_heads_forward")
+
+
+def petra_heads_backward(desc: HeadsDesc, q, k, q_norm, k_norm, positions, dyq, dyk, dq, dk,
+                         dq_norm, dk_norm, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(load().petra_heads_backward(
+        ctypes.byref(desc), _ptr(q), _ptr(k), _norm(q_norm), _norm(k_norm), _ptr(positions),
+        _ptr(dyq), _ptr(dyk), _ptr(dq), _ptr(dk), _norm(dq_norm), _norm(dk_norm),
+        _ptr(workspace), workspace_bytes, _stream(stream)), "petra_heads_backward")
+
+
+def petra_vocab_query(desc: VocabDesc):
+    """Workspace bytes of (the loss, the loss with its gradients)."""
+    loss, grad = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(load().petra_vocab_query(ctypes.byref(desc), ctypes.byref(loss), ctypes.byref(grad)),
+           "petra_vocab_query")
+    return loss.value, grad.value
+
+
+def petra_vocab_loss(desc: VocabDesc, x, w, targets, loss, lse, workspace, workspace_bytes: int,
+                     stream=None) -> None:
+    _check(load().petra_vocab_loss(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(targets),
+                                   _ptr(loss), _ptr(lse), _ptr(workspace), workspace_bytes,
+                                   _stream(stream)), "petra_vocab_loss")
+
+
+def petra_vocab_gradient(desc: VocabDesc, x, w, targets, weight, loss, lse, dx, dw, workspace,
+                         workspace_bytes: int, stream=None) -> None:
+    _check(load().petra_vocab_gradient(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(targets),
+                                       _ptr(weight), _ptr(loss), _ptr(lse), _ptr(dx), _ptr(dw),
+                                       _ptr(workspace), workspace_bytes, _stream(stream)),
+           "petra_vocab_gradient")
+
+
+def petra_adamw_query(desc: AdamwDesc, tensors, count: int):
+    """(bytes of the table, its chunks, workspace bytes); tensors: an array of AdamwTensor."""
+    table, chunks, ws = ctypes.c_size_t(), ctypes.c_int64(), ctypes.c_size_t()
+    _check(load().petra_adamw_query(ctypes.byref(desc), tensors, count, ctypes.byref(table),
+                                    ctypes.byref(chunks), ctypes.byref(ws)), "petra_adamw_query")
+    return table.value, chunks.value, ws.value
+
+
+def petra_adamw_layout(desc: AdamwDesc, tensors, count: int, table, table_bytes: int) -> None:
+    """Writes the table to host memory."""
+    _check(load().petra_adamw_layout(ctypes.byref(desc), tensors, count, _ptr(table),
+                                     table_bytes), "petra_adamw_layout")
+
+
+def petra_adamw_step(desc: AdamwDesc, table, table_bytes: int, count: int, chunks: int, steps,
+                     lr, grad_scale, rng, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(load().petra_adamw_step(ctypes.byref(desc), _ptr(table), table_bytes, count, chunks,
+                                   _ptr(steps), _ptr(lr), _ptr(grad_scale), _ptr(rng),
+                                   _ptr(workspace), workspace_bytes, _stream(stream)),
+           "petra_adamw_step")

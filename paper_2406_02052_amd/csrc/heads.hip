@@ -1,0 +1,447 @@
+// Norms of query and key heads with the rotation by their tokens' positions, and
+// their backward.
+//
+//   z = n(x) gamma (+ beta),  (y_a, y_b) = (z_a cos t - z_b sin t, z_a sin t + z_b cos t)
+// for the pairs (a, b) of a head's channels, t = freq_i position[axis_i]; n is over
+// the head's channels.  Backward, with g the rotation of dy by -t:
+//   dgamma = sum g x^,  dbeta = sum g,  dx = r (g gamma - x^ mean(g gamma x^) (- mean(g gamma)))
+//
+// Bound by memory: a read and a write an element forward, two and one backward.
+//
+// Angles are held in turns, as 64-bit fractions: position times round(2^64 freq / 2 pi),
+// whose wrap is the wrap of the angle, so that far positions lose nothing (an fp32
+// product would be off by 0.1 at 10^6).  The upper 32 bits give the quarter turn and a rest of at
+// most pi / 4, whose sine and cosine are their Taylor polynomials of degree 9 and 10 (the
+// next terms are 2e-9 and 1e-10).
+#include <type_traits>
+
+#include "common.h"
+#include "ops.h"
+
+namespace petra {
+
+namespace {
+
+constexpr int THREADS = 256;
+
+// cos and sin of u / 2^32 turns.
+__device__ __forceinline__ void turn(uint32_t u, float& c, float& s) {
+  const uint32_t q = (u + 0x20000000u) >> 30;
+  const float x = static_cast<float>(static_cast<int32_t>(u - (q << 30))) * 1.46291807926715968105e-9f;   // 2 pi / 2^32
+  const float x2 = x * x;
+  float sn = fmaf(x2, 2.75573192239858907e-6f, -1.98412698412698413e-4f);
+  sn = fmaf(x2, sn, 8.33333333333333333e-3f);
+  sn = fmaf(x2, sn, -1.66666666666666667e-1f);
+  sn = fmaf(x * x2, sn, x);
+  float cs = fmaf(x2, -2.75573192239858907e-7f, 2.48015873015873016e-5f);
+  cs = fmaf(x2, cs, -1.38888888888888889e-3f);
+  cs = fmaf(x2, cs, 4.16666666666666667e-2f);
+  cs = fmaf(x2, cs, -0.5f);
+  cs = fmaf(x2, cs, 1.f);
+  const bool odd = (q & 1) != 0;
+  const float a = odd ? sn : cs, b = odd ? cs : sn;
+  c = (q == 1 || q == 2) ? -a : a;
+  s = (q & 2) ? -b : b;
+}
+
+// Sum over the LANES lanes (a power of two, at most 16) of a team, in every lane.
+template <int LANES>
+__device__ __forceinline__ float team_sum(float v) {
+  if constexpr (LANES == 16) return sum16(v);
+  auto swapped = [](float x, auto dpp) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(dpp)::value, 0xF, 0xF, false));
+  };
+  if constexpr (LANES >= 2) v += swapped(v, std::integral_constant<int, 0xB1>{});    // [1,0,3,2]
+  if constexpr (LANES >= 4) v += swapped(v, std::integral_constant<int, 0x4E>{});    // [2,3,0,1]
+  if constexpr (LANES >= 8) v += swapped(v, std::integral_constant<int, 0x141>{});   // half mirror
+  return v;
+}
+
+// C consecutive elements (4 or 8) as they lie in memory.
+template <typename T, int C> struct Chunk;
+template <> struct Chunk<bf16_t, 8> {
+  uint4 w;
+  __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float* o) const {
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[2 * i] = __uint_as_float(v[i] << 16), o[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+  }
+  static __device__ __forceinline__ void store(bf16_t* p, const float* o) { Vec8<bf16_t>::store(p, o); }
+};
+template <> struct Chunk<bf16_t, 4> {
+  uint2 w;
+  __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void get(float* o) const {
+    o[0] = __uint_as_float(w.x << 16), o[1] = __uint_as_float(w.x & 0xffff0000u);
+    o[2] = __uint_as_float(w.y << 16), o[3] = __uint_as_float(w.y & 0xffff0000u);
+  }
+  static __device__ __forceinline__ void store(bf16_t* p, const float* o) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+  }
+};
+template <int C> struct Chunk<float, C> {
+  float4 w[C / 4];
+  __device__ __forceinline__ void load(const float* p) {
+#pragma unroll
+    for (int i = 0; i < C / 4; ++i) w[i] = reinterpret_cast<const float4*>(p)[i];
+  }
+  __device__ __forceinline__ void get(float* o) const {
+#pragma unroll
+    for (int i = 0; i < C / 4; ++i) o[4 * i] = w[i].x, o[4 * i + 1] = w[i].y, o[4 * i + 2] = w[i].z, o[4 * i + 3] = w[i].w;
+  }
+  static __device__ __forceinline__ void store(float* p, const float* o) {
+#pragma unroll
+    for (int i = 0; i < C / 4; ++i) reinterpret_cast<float4*>(p)[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+  }
+};
+
+// What a lane of a head's team holds: two chunks of C channels, at a and b.  With halves the channels of a
+// pair are in the two chunks, and a lane past the pairs has two chunks in a row; with neighbours all lanes have.
+template <int C, bool HALVES>
+struct Place {
+  int a, b, pair;            // pair: the first of the lane's C pairs (halves), or a / 2
+  bool in_a, in_b, turn_a, turn_b;
+  __device__ __forceinline__ Place(int lane, int dim, int pairs) {
+    if constexpr (HALVES) {
+      const int n = pairs / C;
+      turn_a = turn_b = lane < n;
+      a = lane < n ? lane * C : 2 * pairs + (lane - n) * 2 * C;
+      b = lane < n ? pairs + lane * C : a + C;
+      pair = lane * C;
+    } else {
+      a = lane * 2 * C;
+      b = a + C;
+      pair = lane * C;
+      turn_a = a < 2 * pairs;
+      turn_b = b < 2 * pairs;
+    }
+    in_a = a < dim;
+    in_b = b < dim;
+  }
+};
+
+// The lane's C angles a token.
+template <int C>
+struct Angles {
+  uint64_t f[C];
+  uint32_t axes;             // 4 bits a pair
+  float c[C], s[C];
+  __device__ __forceinline__ void pairs(const HeadsArgs& a, int first) {
+    axes = 0;
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const int p = first + j < a.pairs ? first + j : 0;
+      f[j] = first + j < a.pairs ? a.freq[p] : 0;
+      axes |= static_cast<uint32_t>(a.axis[p]) << (4 * j);
+    }
+  }
+  __device__ __forceinline__ void at(const HeadsArgs& a, uint32_t token, uint32_t index) {
+    int p[HEADS_AXES];
+#pragma unroll
+    for (int x = 0; x < HEADS_AXES; ++x)
+      p[x] = a.positions == nullptr ? static_cast<int>(index) : x < a.axes ? a.positions[x * a.tokens + token] : 0;
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const uint32_t x = (axes >> (4 * j)) & 15u;
+      const int v = x < 2 ? (x == 0 ? p[0] : p[1]) : (x == 2 ? p[2] : p[3]);
+      const uint32_t lo = static_cast<uint32_t>(f[j]), hi = static_cast<uint32_t>(f[j] >> 32), u = static_cast<uint32_t>(v);
+      turn(__umulhi(u, lo) + u * hi - (v < 0 ? lo : 0u), c[j], s[j]);
+    }
+  }
+};
+
+// Rotates the lane's channels in place, by the angle or (BACK) against it.
+template <int C, bool HALVES, bool BACK>
+__device__ __forceinline__ void rotate(float (&x)[2 * C], const Angles<C>& t, const Place<C, HALVES>& p) {
+#pragma unroll
+  for (int j = 0; j < C; ++j) {
+    const int i = HALVES ? j : 2 * j, k = HALVES ? C + j : 2 * j + 1;
+    const float s = BACK ? -t.s[j] : t.s[j], a = x[i], b = x[k];
+    const float u = fmaf(a, t.c[j], -b * s), v = fmaf(a, s, b * t.c[j]);
+    const bool on = HALVES ? p.turn_a : (j < C / 2 ? p.turn_a : p.turn_b);
+    x[i] = on ? u : a;
+    x[k] = on ? v : b;
+  }
+}
+
+// Normalises the lane's channels of a head in place; returns 1 / the deviation.
+template <int C, int LANES>
+__device__ __forceinline__ float unit(float (&x)[2 * C], bool layer, bool in_a, bool in_b, float inv_dim, float eps) {
+  if (layer) {
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 2 * C; ++e) s += x[e];
+    const float mean = team_sum<LANES>(s) * inv_dim;
+#pragma unroll
+    for (int e = 0; e < 2 * C; ++e) x[e] = (e < C ? in_a : in_b) ? x[e] - mean : 0.f;
+  }
+  float q = 0.f;
+#pragma unroll
+  for (int e = 0; e < 2 * C; ++e) q = fmaf(x[e], x[e], q);
+  const float r = rsqrtf(fmaf(team_sum<LANES>(q), inv_dim, eps));
+#pragma unroll
+  for (int e = 0; e < 2 * C; ++e) x[e] *= r;
+  return r;
+}
+
+// How a workgroup's lanes lie over tokens and heads: a team of LANES lanes a head, 2^head_bits heads and the
+// rest of a wave's teams tokens beside each other.  A wave takes a group of tokens and `rounds` times its heads, so
+// that a token's angles are formed once for them.
+struct Lane {
+  int lane, head;
+  long token, step;          // the first token of this lane, and how far the next is
+};
+template <int LANES>
+__device__ __forceinline__ Lane my_lane(const HeadsPart& p, int block) {
+  const int in_wave = (threadIdx.x & 63) / LANES, wave = threadIdx.x >> 6;
+  const int tokens = (64 / LANES) >> p.head_bits;
+  Lane l;
+  l.lane = threadIdx.x & (LANES - 1);
+  l.head = in_wave & ((1 << p.head_bits) - 1);
+  const int group = block / p.splits, split = block - group * p.splits;
+  l.head += split * (p.rounds << p.head_bits);
+  l.token = (static_cast<long>(group) * (THREADS / 64) + wave) * tokens + (in_wave >> p.head_bits);
+  l.step = static_cast<long>(p.groups) * (THREADS / 64) * tokens;
+  return l;
+}
+
+template <typename T, int C, int LANES, bool HALVES>
+__global__ __launch_bounds__(THREADS) void heads_forward_kernel(HeadsArgs a) {
+  const bool second = static_cast<int>(blockIdx.x) >= a.part[0].blocks;
+  const HeadsPart& p = a.part[second];
+  const Lane l = my_lane<LANES>(p, blockIdx.x - (second ? a.part[0].blocks : 0));
+  const Place<C, HALVES> at(l.lane, a.dim, a.pairs);
+  Angles<C> angles;
+  angles.pairs(a, at.pair);
+  float gamma[2 * C];
+#pragma unroll
+  for (int e = 0; e < 2 * C; ++e) gamma[e] = 1.f;
+  if (p.gamma != nullptr) {
+    Chunk<float, C> t;
+    if (at.in_a) t.load(p.gamma + at.a), t.get(gamma);
+    if (at.in_b) t.load(p.gamma + at.b), t.get(gamma + C);
+  }
+  for (long token = l.token; token < a.tokens; token += l.step) {
+    const uint32_t b = static_cast<uint32_t>(token) / a.len, i = static_cast<uint32_t>(token) - b * a.len;
+    angles.at(a, static_cast<uint32_t>(token), i);
+    const T* const x0 = static_cast<const T*>(p.x) + b * p.x_stride[0] + i * p.x_stride[1];
+    T* const y0 = static_cast<T*>(p.y) + b * p.y_stride[0] + i * p.y_stride[1];
+    for (int n = 0, h = l.head; n < p.rounds; ++n, h += 1 << p.head_bits) {
+      const bool in = h < p.heads;
+      Chunk<T, C> ca{}, cb{};
+      if (in && at.in_a) ca.load(x0 + h * p.x_stride[2] + at.a);
+      if (in && at.in_b) cb.load(x0 + h * p.x_stride[2] + at.b);
+      float x[2 * C];
+      ca.get(x);
+      cb.get(x + C);
+      if (p.gamma != nullptr) {
+        unit<C, LANES>(x, a.layer, at.in_a, at.in_b, a.inv_dim, a.eps);
+#pragma unroll
+        for (int e = 0; e < 2 * C; ++e) x[e] *= gamma[e];
+        if (p.beta != nullptr) {
+          float beta[2 * C] = {};
+          Chunk<float, C> t;
+          if (at.in_a) t.load(p.beta + at.a), t.get(beta);
+          if (at.in_b) t.load(p.beta + at.b), t.get(beta + C);
+#pragma unroll
+          for (int e = 0; e < 2 * C; ++e) x[e] += beta[e];
+        }
+      }
+      rotate<C, HALVES, false>(x, angles, at);
+      if (in && at.in_a) Chunk<T, C>::store(y0 + h * p.y_stride[2] + at.a, x);
+      if (in && at.in_b) Chunk<T, C>::store(y0 + h * p.y_stride[2] + at.b, x + C);
+    }
+  }
+}
+
+// Sums of the parameters' gradients stay in registers over a workgroup's tokens; its teams' are then added in LDS
+// in a fixed order and written as a row of partial sums, which heads_join_kernel adds in a fixed order too.
+template <typename T, int C, int LANES, bool HALVES>
+__global__ __launch_bounds__(THREADS) void heads_backward_kernel(HeadsArgs a) {
+  __shared__ float joined[THREADS * 2 * C];
+  const bool second = static_cast<int>(blockIdx.x) >= a.part[0].blocks;
+  const HeadsPart& p = a.part[second];
+  const int block = blockIdx.x - (second ? a.part[0].blocks : 0);
+  const Lane l = my_lane<LANES>(p, block);
+  const Place<C, HALVES> at(l.lane, a.dim, a.pairs);
+  Angles<C> angles;
+  angles.pairs(a, at.pair);
+  const bool norm = p.gamma != nullptr;
+  float gamma[2 * C], dgamma[2 * C] = {}, dbeta[2 * C] = {};
+#pragma unroll
+  for (int e = 0; e < 2 * C; ++e) gamma[e] = 1.f;
+  if (norm) {
+    Chunk<float, C> t;
+    if (at.in_a) t.load(p.gamma + at.a), t.get(gamma);
+    if (at.in_b) t.load(p.gamma + at.b), t.get(gamma + C);
+  }
+  for (long token = l.token; token < a.tokens; token += l.step) {
+    const uint32_t b = static_cast<uint32_t>(token) / a.len, i = static_cast<uint32_t>(token) - b * a.len;
+    angles.at(a, static_cast<uint32_t>(token), i);
+    const long ox = b * p.x_stride[0] + i * p.x_stride[1], oy = b * p.y_stride[0] + i * p.y_stride[1];
+    for (int n = 0, h = l.head; n < p.rounds; ++n, h += 1 << p.head_bits) {
+      const bool in = h < p.heads;
+      const long px = ox + h * p.x_stride[2], py = oy + h * p.y_stride[2];
+      Chunk<T, C> ca{}, cb{}, xa{}, xb{};
+      if (in && at.in_a) {
+        ca.load(static_cast<const T*>(p.dy) + py + at.a);
+        if (norm) xa.load(static_cast<const T*>(p.x) + px + at.a);
+      }
+      if (in && at.in_b) {
+        cb.load(static_cast<const T*>(p.dy) + py + at.b);
+        if (norm) xb.load(static_cast<const T*>(p.x) + px + at.b);
+      }
+      float g[2 * C];
+      ca.get(g);
+      cb.get(g + C);
+      rotate<C, HALVES, true>(g, angles, at);
+      if (norm) {
+        float x[2 * C], s = 0.f, m = 0.f;
+        xa.get(x);
+        xb.get(x + C);
+        const float r = unit<C, LANES>(x, a.layer, at.in_a, at.in_b, a.inv_dim, a.eps);
+#pragma unroll
+        for (int e = 0; e < 2 * C; ++e) {
+          dgamma[e] = fmaf(g[e], x[e], dgamma[e]);
+          dbeta[e] += g[e];
+          g[e] *= gamma[e];
+          s = fmaf(g[e], x[e], s);
+          m += g[e];
+        }
+        s = team_sum<LANES>(s) * a.inv_dim;
+        m = a.layer ? team_sum<LANES>(m) * a.inv_dim : 0.f;
+#pragma unroll
+        for (int e = 0; e < 2 * C; ++e) g[e] = r * (g[e] - x[e] * s - m);
+      }
+      if (in && at.in_a) Chunk<T, C>::store(static_cast<T*>(p.dx) + px + at.a, g);
+      if (in && at.in_b) Chunk<T, C>::store(static_cast<T*>(p.dx) + px + at.b, g + C);
+    }
+  }
+  if (!norm) return;
+  auto flush = [&](const float (&v)[2 * C], float* to) {
+    __syncthreads();
+    // [team][channel]
+    float* const mine = joined + threadIdx.x / LANES * (LANES * 2 * C);
+#pragma unroll
+    for (int e = 0; e < C; ++e) {
+      if (at.in_a) mine[at.a + e] = v[e];
+      if (at.in_b) mine[at.b + e] = v[C + e];
+    }
+    __syncthreads();
+    if (static_cast<int>(threadIdx.x) < a.dim) {
+      float s = 0.f;
+      for (int t = 0; t < THREADS / LANES; ++t) s += joined[t * (LANES * 2 * C) + threadIdx.x];
+      to[static_cast<long>(block) * a.dim + threadIdx.x] = s;
+    }
+  };
+  flush(dgamma, p.part_gamma);
+  if (p.beta != nullptr) flush(dbeta, p.part_beta);
+}
+
+// Output blockIdx.x (dgamma and dbeta of the queries, then of the keys), channels 16 blockIdx.y ..: the sum over rows of
+// partial sums, in 64 interleaved sums a channel.
+__global__ __launch_bounds__(1024) void heads_join_kernel(HeadsArgs a) {
+  __shared__ float lds[64][17];
+  const HeadsPart& p = a.part[blockIdx.x >> 1];
+  const bool beta = (blockIdx.x & 1) != 0;
+  if (p.heads == 0 || p.gamma == nullptr || (beta && p.beta == nullptr)) return;
+  const float* const from = beta ? p.part_beta : p.part_gamma;
+  float* const to = beta ? p.dbeta : p.dgamma;
+  const int c = blockIdx.y * 16 + (threadIdx.x & 15), lane = threadIdx.x >> 4;
+  float v = 0.f;
+  if (c < a.dim)
+#pragma unroll 8
+    for (int r = lane; r < p.blocks; r += 64) v += from[static_cast<long>(r) * a.dim + c];
+  lds[lane][threadIdx.x & 15] = v;
+  __syncthreads();
+  if (lane == 0 && c < a.dim) {
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 64; ++i) t += lds[i][threadIdx.x & 15];
+    to[c] = t;
+  }
+}
+
+// Channels of a chunk: 8 where the pairs' halves are whole chunks.
+int chunk(const HeadsArgs& a) { return a.halves && a.pairs % 8 != 0 ? 4 : 8; }
+
+int lanes(const HeadsArgs& a) {
+  const int c = chunk(a), rest = a.dim - 2 * a.pairs;
+  const int need = a.halves ? a.pairs / c + (rest + 2 * c - 1) / (2 * c) : (a.dim + 2 * c - 1) / (2 * c);
+  int n = 1;
+  while (n < need) n *= 2;
+  return n;
+}
+
+template <typename T, int C, int LANES>
+void launch(const HeadsArgs& a, bool backward, hipStream_t s) {
+  const unsigned n = static_cast<unsigned>(a.part[0].blocks + a.part[1].blocks);
+  if (n == 0) return;
+  if (a.halves) {
+    if (backward) heads_backward_kernel<T, C, LANES, true><<<n, THREADS, 0, s>>>(a);
+    else heads_forward_kernel<T, C, LANES, true><<<n, THREADS, 0, s>>>(a);
+  } else if constexpr (C == 8) {
+    if (backward) heads_backward_kernel<T, C, LANES, false><<<n, THREADS, 0, s>>>(a);
+    else heads_forward_kernel<T, C, LANES, false><<<n, THREADS, 0, s>>>(a);
+  }
+}
+
+template <typename T>
+void by_shape(const HeadsArgs& a, bool backward, hipStream_t s) {
+  const int n = lanes(a);
+  if (chunk(a) == 8) {
+    switch (n) {
+      case 1: return launch<T, 8, 1>(a, backward, s);
+      case 2: return launch<T, 8, 2>(a, backward, s);
+      case 4: return launch<T, 8, 4>(a, backward, s);
+      default: return launch<T, 8, 8>(a, backward, s);
+    }
+  }
+  switch (n) {
+    case 1: return launch<T, 4, 1>(a, backward, s);
+    case 2: return launch<T, 4, 2>(a, backward, s);
+    case 4: return launch<T, 4, 4>(a, backward, s);
+    case 8: return launch<T, 4, 8>(a, backward, s);
+    default: return launch<T, 4, 16>(a, backward, s);
+  }
+}
+
+}  // namespace
+
+void heads_plan(HeadsArgs& a, bool backward) {
+  const int teams = 64 / lanes(a);
+  // workgroups of both parts together: 8 a CU forward; backward, where each leaves a row of partial sums, 4
+  const long most = backward ? 1024 : 2048;
+  const long work = a.tokens * (a.part[0].heads + a.part[1].heads);
+  for (HeadsPart& p : a.part) {
+    p.blocks = 0;
+    if (p.heads == 0 || a.tokens == 0) continue;
+    p.head_bits = 0;
+    while ((1 << p.head_bits) < p.heads && (2 << p.head_bits) <= teams) ++p.head_bits;
+    const int all = (p.heads + (1 << p.head_bits) - 1) >> p.head_bits;
+    const long tokens = static_cast<long>(teams >> p.head_bits) * (THREADS / 64);
+    const long want = (a.tokens + tokens - 1) / tokens;
+    long share = static_cast<long>(static_cast<double>(most) * a.tokens * p.heads / work);
+    if (share < 1) share = 1;
+    // few tokens: the rounds over heads go to workgroups of their own
+    p.splits = want * all <= share ? all : 1;
+    p.rounds = (all + p.splits - 1) / p.splits;
+    p.groups = static_cast<int>(want < share ? want : share);
+    p.blocks = p.groups * p.splits;
+  }
+}
+
+void heads_forward(const HeadsArgs& a, int dtype, hipStream_t s) {
+  if (dtype == 1) by_shape<bf16_t>(a, false, s);
+  else by_shape<float>(a, false, s);
+}
+
+void heads_backward(const HeadsArgs& a, int dtype, hipStream_t s) {
+  if (dtype == 1) by_shape<bf16_t>(a, true, s);
+  else by_shape<float>(a, true, s);
+  if (a.part[0].gamma != nullptr || a.part[1].gamma != nullptr)
+    heads_join_kernel<<<dim3(4, static_cast<unsigned>((a.dim + 15) / 16)), 1024, 0, s>>>(a);
+}
+
+}  // namespace petra

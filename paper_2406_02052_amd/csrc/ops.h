@@ -70,4 +70,98 @@ AttnPlan attn_plan(const AttnArgs& a);
 void attn_forward(const AttnArgs& a, const AttnPlan& p, int dtype, void* workspace, hipStream_t s);
 void attn_backward(const AttnArgs& a, const AttnPlan& p, int dtype, void* workspace, hipStream_t s);
 
+// --- head norms and rotation ------------------------------------------------
+constexpr int HEADS_AXES = 4, HEADS_PAIRS = 64;
+
+// The queries, or the keys.
+struct HeadsPart {
+  const void *x, *dy;
+  void *y, *dx;
+  const float *gamma, *beta;                 // null gamma: no norm
+  float *dgamma, *dbeta, *part_gamma, *part_beta;
+  int64_t x_stride[3], y_stride[3];          // batch, token, head; dx like x, dy like y
+  int heads;
+  // workgroups: `groups` of tokens times `splits` of heads, each `rounds` of 2^head_bits
+  int blocks, groups, splits, rounds, head_bits;
+};
+struct HeadsArgs {
+  HeadsPart part[2];
+  const int32_t* positions;                  // [axes][tokens]; null: a token's index in its sequence
+  long tokens;                               // batch * len
+  uint32_t len;
+  int dim, pairs, axes, halves, layer;
+  float eps, inv_dim;
+  uint64_t freq[HEADS_PAIRS];                // 2^64 of a turn a position
+  uint8_t axis[HEADS_PAIRS];
+};
+
+// The workgroups of both parts (without tokens none).
+void heads_plan(HeadsArgs& a, bool backward);
+void heads_forward(const HeadsArgs& a, int dtype, hipStream_t s);
+void heads_backward(const HeadsArgs& a, int dtype, hipStream_t s);
+
+// --- loss over a vocabulary -------------------------------------------------
+// A gradient: rows x cols results of the product of a (a_ld between its lines) and b (cols between its lines, b_inner
+// of them) over `inner`, split over `splits` workgroups of per_split.
+struct VocabGrad {
+  const void *a, *b;
+  void* out;
+  const float* factor;                       // [rows], nullable
+  float *part, *acc;                         // the splits' sums; sums over the pieces of rows
+  long rows, cols, inner, a_ld, a_free, b_inner, per_split;   // a_free: rows, or as many as a's lines have
+  int splits, row_tiles, col_tiles, add, last;
+};
+struct VocabArgs {
+  const void *x, *w;
+  const int32_t* targets;
+  const float* weight;                       // nullable: *mean
+  float *loss, *lse;
+  void *dx, *dw;
+  long rows, row0, piece;                    // all rows, and those at work
+  int width, vocab, vocab_padded;            // padded: of e, in which the rest is zeros
+  int row_tiles, col_tiles, row_tile, col_tile;
+  float scale, scale_log2;                   // scale_log2 = scale log2(e)
+  // workspace: each row's reference; of a piece the tiles' sums, the references that differ and which tiles
+  // have them, e, factors and x times them
+  float *ref, *sums, *shift, *mean, *factor, *part, *acc;
+  int* slow;
+  void *scaled, *e;
+};
+struct VocabPlan {
+  long piece;
+  VocabGrad dx, dw;                          // splits and per_split
+  size_t ref, sums, shift, slow, mean, factor, scaled, e, part, acc, bytes;   // offsets in the workspace
+};
+
+// piece_rows: rows at a time (0: by the rule).
+VocabPlan vocab_plan(const VocabArgs& a, int dtype, bool gradients, long piece_rows);
+void vocab_run(VocabArgs a, const VocabPlan& p, int dtype, bool gradients, void* workspace, hipStream_t s);
+
+// --- AdamW ------------------------------------------------------------------
+constexpr int ADAMW_CHUNK = 4096;            // elements a workgroup
+
+// A tensor of the table in device memory, and where it lies among the chunks and the generator's groups of 4 elements.
+struct AdamwEntry {
+  float* theta;
+  void *grad, *m, *v, *copy;
+  float *m_scale, *v_scale;
+  int64_t n, padded, first_chunk, first_group;
+  float decay;
+  int32_t reserved;
+};
+struct AdamwArgs {
+  const AdamwEntry* entries;
+  const int32_t* chunk_of;                   // the tensor of each chunk
+  long chunks;
+  int64_t* steps;
+  const float *lr, *grad_scale;
+  const uint64_t* rng;
+  float* hyper;                              // workspace: corrections of m and of sqrt(v)
+  double log_b1, log_b2;
+  float b1, c1, b2, c2, eps;                 // c = 1 - b
+  int zero_grads;
+};
+
+void adamw_step(const AdamwArgs& a, bool bf16_grads, bool fp8, hipStream_t s);
+
 }  // namespace petra

@@ -1,9 +1,10 @@
-// extern "C" entry points of the token operators (attention, coupling, dropout):
-// argument validation and dispatch.  Nothing here allocates device memory.
+// extern "C" entry points of the token operators (attention, coupling, dropout, head norms
+// with rotation, the loss over a vocabulary, AdamW): argument validation and dispatch.  Nothing here allocates device memory.
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <string>
+#include <vector>
 
 #include "../../include/petra.h"
 #include "ops.h"
@@ -594,6 +595,482 @@ petra_status petra_dropout(int64_t n, int32_t dtype, float p, float alpha, const
     need_apart(sy, sr, true);
     if (n == 0) return false;
     petra::dropout(x, residual, y, n, alpha * inv_keep(cut), cut, rng, dtype, static_cast<hipStream_t>(stream));
+    return true;
+  });
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// head norms and rotation
+// ---------------------------------------------------------------------------
+
+namespace {
+
+static_assert(petra::HEADS_AXES == PETRA_HEAD_AXES && petra::HEADS_PAIRS == PETRA_HEAD_PAIRS, "the header's limits");
+
+struct Heads {
+  petra::HeadsArgs a{};
+  int64_t n[2][3];   // positions of the queries and of the keys
+  size_t esz;
+  bool empty;
+
+  Heads(const petra_heads_desc* d, bool backward) {
+    need(d != nullptr, PETRA_ERR_INVALID_ARG, "null description");
+    need_dtype(d->dtype);
+    esz = size_of(d->dtype);
+    need(d->batch >= 0 && d->len >= 0, PETRA_ERR_SHAPE, "negative size");
+    need(d->heads >= 1 && d->heads <= 65535 && d->kv_heads >= 0 && d->kv_heads <= 65535, PETRA_ERR_SHAPE,
+         "heads must be 1 .. 65535, kv_heads 0 .. 65535");
+    need(d->head_dim >= 8 && d->head_dim <= 128 && d->head_dim % 8 == 0, PETRA_ERR_SHAPE,
+         "head_dim must be a multiple of 8, at most 128");
+    need(d->norm == PETRA_NORM_RMS || d->norm == PETRA_NORM_LAYER, PETRA_ERR_INVALID_ARG, "unknown norm");
+    need(d->eps > 0.f && std::isfinite(d->eps), PETRA_ERR_INVALID_ARG, "eps must be positive and finite");
+    need(d->layout == PETRA_PAIRS_HALVES || d->layout == PETRA_PAIRS_NEIGHBOURS, PETRA_ERR_INVALID_ARG, "unknown layout of pairs");
+    need(d->pairs >= 0 && d->pairs % 4 == 0 && 2 * d->pairs <= d->head_dim, PETRA_ERR_SHAPE,
+         "pairs must be a multiple of 4, at most head_dim / 2");
+    need(d->axes >= 1 && d->axes <= PETRA_HEAD_AXES, PETRA_ERR_SHAPE, "axes must be 1 .. 4");
+    const int64_t tokens = static_cast<int64_t>(d->batch) * d->len;
+    need(tokens < (int64_t{1} << 31), PETRA_ERR_SHAPE, "batch * len of 2^31 or more");
+    a.tokens = tokens;
+    a.len = static_cast<uint32_t>(d->len);
+    a.dim = d->head_dim;
+    a.pairs = d->pairs;
+    a.axes = d->axes;
+    a.halves = d->layout == PETRA_PAIRS_HALVES;
+    a.layer = d->norm == PETRA_NORM_LAYER;
+    a.eps = d->eps;
+    a.inv_dim = 1.f / static_cast<float>(d->head_dim);
+    empty = tokens == 0;
+    for (int i = 0; i < d->pairs; ++i) {
+      need(d->axis[i] >= 0 && d->axis[i] < d->axes, PETRA_ERR_INVALID_ARG, "a pair's axis is none of the axes");
+      need(std::isfinite(d->freq[i]), PETRA_ERR_INVALID_ARG, "frequencies must be finite");
+      a.axis[i] = static_cast<uint8_t>(d->axis[i]);
+      // the fraction of a turn in 64 bits; a whole one wraps
+      long double f = static_cast<long double>(d->freq[i]) / 6.283185307179586476925286766559005768L;
+      f = roundl((f - floorl(f)) * 18446744073709551616.0L);
+      a.freq[i] = f >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(f);
+    }
+    for (int i = 0; i < 2; ++i) {
+      petra::HeadsPart& p = a.part[i];
+      p.heads = i == 0 ? d->heads : d->kv_heads;
+      n[i][0] = d->batch, n[i][1] = d->len, n[i][2] = p.heads;
+      const char *x = i == 0 ? "q" : "k", *y = i == 0 ? "yq" : "yk";
+      strides(i == 0 ? d->q_stride : d->k_stride, p.x_stride, d->len, p.heads, a.dim, esz, x);
+      strides(i == 0 ? d->yq_stride : d->yk_stride, p.y_stride, d->len, p.heads, a.dim, esz, y);
+      need_reach(p.x_stride, n[i], a.dim, esz, x);
+      need_reach(p.y_stride, n[i], a.dim, esz, y);
+      if (backward) need_distinct(p.x_stride, n[i], a.dim, i == 0 ? "dq" : "dk");
+      else need_distinct(p.y_stride, n[i], a.dim, y);
+    }
+    petra::heads_plan(a, backward);
+  }
+
+  bool none(int i) const { return empty || a.part[i].heads == 0; }
+  Runs x(const void* p, int i, const char* name) const { return {none(i) ? nullptr : p, a.part[i].x_stride, n[i], a.dim, esz, name}; }
+  Runs y(const void* p, int i, const char* name) const { return {none(i) ? nullptr : p, a.part[i].y_stride, n[i], a.dim, esz, name}; }
+  bool same_strides(int i) const {
+    for (int d = 0; d < 3; ++d)
+      if (n[i][d] > 1 && a.part[i].x_stride[d] != a.part[i].y_stride[d]) return false;
+    return true;
+  }
+  Span positions(const int32_t* p) const {
+    return {empty ? nullptr : p, static_cast<size_t>(a.axes) * static_cast<size_t>(a.tokens) * 4, "positions"};
+  }
+  Span param(const float* p, const char* name) const { return {p, static_cast<size_t>(a.dim) * 4, name}; }
+  // gamma and beta of both norms, or of their gradients
+  int params(const petra_norm_params* q, const petra_norm_params* k, Span out[4], const char* const names[4]) const {
+    int count = 0;
+    for (int i = 0; i < 2; ++i) {
+      const petra_norm_params* const p = i == 0 ? q : k;
+      if (p == nullptr) continue;
+      out[count++] = param(p->gamma, names[2 * i]);
+      if (p->beta != nullptr) out[count++] = param(p->beta, names[2 * i + 1]);
+    }
+    return count;
+  }
+  size_t part_bytes(int i) const { return static_cast<size_t>(a.part[i].blocks) * a.dim * 4; }
+  size_t backward_bytes() const { return 2 * (part_bytes(0) + part_bytes(1)); }
+};
+
+const char* const HEAD_PARAMS[4] = {"q_norm.gamma", "q_norm.beta", "k_norm.gamma", "k_norm.beta"};
+const char* const HEAD_GRADS[4] = {"dq_norm.gamma", "dq_norm.beta", "dk_norm.gamma", "dk_norm.beta"};
+
+}  // namespace
+
+extern "C" {
+
+petra_status petra_heads_query(const petra_heads_desc* desc, size_t* backward_bytes) {
+  return entry("petra_heads_query", [&]() -> bool {
+    const Heads t(desc, true);
+    if (backward_bytes != nullptr) *backward_bytes = t.backward_bytes();
+    return false;
+  });
+}
+
+petra_status petra_heads_forward(const petra_heads_desc* desc, const void* q, const void* k,
+                                 const petra_norm_params* q_norm, const petra_norm_params* k_norm,
+                                 const int32_t* positions, void* yq, void* yk, void* stream) {
+  return entry("petra_heads_forward", [&]() -> bool {
+    Heads t(desc, false);
+    const void* const in[2] = {q, k};
+    void* const out[2] = {yq, yk};
+    const petra_norm_params* const norm[2] = {q_norm, k_norm};
+    const char* const names[6] = {"q", "k", "yq", "yk", "q_norm", "k_norm"};
+    for (int i = 0; i < 2; ++i) {
+      need_ptr(in[i], names[i], t.none(i));
+      need_ptr(out[i], names[2 + i], t.none(i));
+      if (norm[i] != nullptr) need_norm(norm[i], names[4 + i]);
+    }
+    need(desc->kv_heads > 0 || (k == nullptr && yk == nullptr && k_norm == nullptr), PETRA_ERR_INVALID_ARG,
+         "k, yk and k_norm without key heads");
+    need_int_ptr(positions, "positions", 4);
+    Span small[5];
+    int count = t.params(q_norm, k_norm, small, HEAD_PARAMS);
+    small[count++] = t.positions(positions);
+    for (int i = 0; i < 2; ++i) {
+      const Runs y = t.y(out[i], i, names[2 + i]);
+      for (int j = 0; j < 2; ++j)
+        if (!(i == j && out[i] == in[j] && t.same_strides(i))) need_apart(y, t.x(in[j], j, names[j]));
+      for (int j = 0; j < count; ++j) need_apart(y, small[j]);
+    }
+    need_apart(t.y(yq, 0, "yq"), t.y(yk, 1, "yk"));
+    if (t.empty) return false;
+    t.a.positions = positions;
+    for (int i = 0; i < 2; ++i) {
+      t.a.part[i].x = in[i];
+      t.a.part[i].y = out[i];
+      t.a.part[i].gamma = norm[i] != nullptr ? norm[i]->gamma : nullptr;
+      t.a.part[i].beta = norm[i] != nullptr ? norm[i]->beta : nullptr;
+    }
+    petra::heads_forward(t.a, desc->dtype, static_cast<hipStream_t>(stream));
+    return true;
+  });
+}
+
+petra_status petra_heads_backward(const petra_heads_desc* desc, const void* q, const void* k,
+                                  const petra_norm_params* q_norm, const petra_norm_params* k_norm,
+                                  const int32_t* positions, const void* dyq, const void* dyk, void* dq, void* dk,
+                                  const petra_norm_params* dq_norm, const petra_norm_params* dk_norm, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  return entry("petra_heads_backward", [&]() -> bool {
+    Heads t(desc, true);
+    const void *const x[2] = {q, k}, *const dy[2] = {dyq, dyk};
+    void* const dx[2] = {dq, dk};
+    const petra_norm_params *const norm[2] = {q_norm, k_norm}, *const dnorm[2] = {dq_norm, dk_norm};
+    const char* const names[10] = {"q", "k", "dyq", "dyk", "dq", "dk", "q_norm", "k_norm", "dq_norm", "dk_norm"};
+    need(desc->kv_heads > 0 || (k == nullptr && dyk == nullptr && dk == nullptr && k_norm == nullptr && dk_norm == nullptr),
+         PETRA_ERR_INVALID_ARG, "k, dyk, dk, k_norm and dk_norm without key heads");
+    for (int i = 0; i < 2; ++i) {
+      need_ptr(x[i], names[i], t.none(i) || norm[i] == nullptr);
+      need_ptr(dy[i], names[2 + i], t.none(i));
+      need_ptr(dx[i], names[4 + i], t.none(i));
+      if (norm[i] != nullptr) {
+        need_norm(norm[i], names[6 + i]);
+        need_norm(dnorm[i], names[8 + i]);
+        need((norm[i]->beta != nullptr) == (dnorm[i]->beta != nullptr), PETRA_ERR_INVALID_ARG,
+             "a norm and its gradient differ in beta");
+      } else {
+        need(dnorm[i] == nullptr, PETRA_ERR_INVALID_ARG, "a norm's gradient without the norm");
+      }
+    }
+    need_int_ptr(positions, "positions", 4);
+    Span in[5], out[4];
+    int ins = t.params(q_norm, k_norm, in, HEAD_PARAMS);
+    in[ins++] = t.positions(positions);
+    const int outs = t.params(dq_norm, dk_norm, out, HEAD_GRADS);
+    for (int i = 0; i < 2; ++i) {
+      const Runs d = t.x(dx[i], i, names[4 + i]);
+      for (int j = 0; j < 2; ++j) {
+        if (norm[j] != nullptr && !(i == j && dx[i] == x[j])) need_apart(d, t.x(x[j], j, names[j]));
+        if (!(i == j && dx[i] == dy[j] && t.same_strides(i))) need_apart(d, t.y(dy[j], j, names[2 + j]));
+      }
+      for (int j = 0; j < ins; ++j) need_apart(d, in[j]);
+      for (int j = 0; j < outs; ++j) {
+        need_apart(d, out[j]);
+        if (norm[i] != nullptr) need_apart(t.x(x[i], i, names[i]), out[j]);
+        need_apart(t.y(dy[i], i, names[2 + i]), out[j]);
+      }
+    }
+    need_apart(t.x(dq, 0, "dq"), t.x(dk, 1, "dk"));
+    for (int i = 0; i < outs; ++i) {
+      for (int j = 0; j < ins; ++j) need_apart(out[i], in[j]);
+      for (int j = 0; j < i; ++j) need_apart(out[i], out[j]);
+    }
+    const bool sums = q_norm != nullptr || k_norm != nullptr;
+    need_workspace(workspace, workspace_bytes, sums ? t.backward_bytes() : 0);
+    if (t.empty && !sums) return false;
+    t.a.positions = positions;
+    float* ws = static_cast<float*>(workspace);
+    for (int i = 0; i < 2; ++i) {
+      petra::HeadsPart& p = t.a.part[i];
+      p.x = x[i];
+      p.dy = dy[i];
+      p.dx = dx[i];
+      if (norm[i] != nullptr) {
+        p.gamma = norm[i]->gamma;
+        p.beta = norm[i]->beta;
+        p.dgamma = dnorm[i]->gamma;
+        p.dbeta = dnorm[i]->beta;
+      }
+      p.part_gamma = ws;
+      p.part_beta = ws + t.part_bytes(i) / 4;
+      ws += t.part_bytes(i) / 2;
+    }
+    petra::heads_backward(t.a, desc->dtype, static_cast<hipStream_t>(stream));
+    return true;
+  });
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// loss over a vocabulary
+// ---------------------------------------------------------------------------
+
+namespace {
+
+struct Vocab {
+  petra::VocabArgs a{};
+  size_t x_bytes, w_bytes, row_bytes;
+  int dtype;
+  long piece_rows;
+
+  explicit Vocab(const petra_vocab_desc* d) {
+    need(d != nullptr, PETRA_ERR_INVALID_ARG, "null description");
+    need_dtype(d->dtype);
+    need(d->rows >= 0 && d->rows <= (int64_t{1} << 30) && d->piece_rows >= 0, PETRA_ERR_SHAPE, "negative size or too many rows");
+    need(d->width >= 8 && d->width <= 65536 && d->width % 8 == 0, PETRA_ERR_SHAPE,
+         "width must be a multiple of 8, at most 65536");
+    need(d->vocab >= 1 && d->vocab <= (1 << 20), PETRA_ERR_SHAPE, "vocab must be 1 .. 2^20");
+    need(d->scale > 0.f && std::isfinite(d->scale), PETRA_ERR_INVALID_ARG, "scale must be positive and finite");
+    a.rows = d->rows;
+    a.width = d->width;
+    a.vocab = d->vocab;
+    a.vocab_padded = (d->vocab + 63) / 64 * 64;
+    a.scale = d->scale;
+    a.scale_log2 = d->scale * 1.44269504088896340736f;
+    dtype = d->dtype;
+    piece_rows = d->piece_rows;
+    x_bytes = static_cast<size_t>(a.rows) * a.width * size_of(dtype);
+    w_bytes = static_cast<size_t>(a.vocab) * a.width * size_of(dtype);
+    row_bytes = static_cast<size_t>(a.rows) * 4;
+  }
+
+  petra::VocabPlan plan(bool gradients) const { return petra::vocab_plan(a, dtype, gradients, piece_rows); }
+};
+
+petra_status vocab_call(const char* name, const petra_vocab_desc* desc, const void* x, const void* w, const int32_t* targets,
+                        const float* weight, float* loss, float* lse, void* dx, void* dw, bool gradients, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  return entry(name, [&]() -> bool {
+    Vocab t(desc);
+    const bool empty = t.a.rows == 0;
+    need_ptr(x, "x", empty);
+    need_ptr(w, "w");
+    need_ptr(loss, "loss", empty);
+    need_ptr(lse, "lse", empty);
+    if (!empty && targets == nullptr) throw Refused{PETRA_ERR_INVALID_ARG, "null pointer: targets"};
+    need_int_ptr(targets, "targets", 4);
+    need_int_ptr(weight, "weight", 4);
+    if (gradients) {
+      need_ptr(dx, "dx", empty);
+      need_ptr(dw, "dw");
+    }
+    const Span in[4] = {{x, t.x_bytes, "x"}, {w, t.w_bytes, "w"}, {targets, t.row_bytes, "targets"}, {weight, t.row_bytes, "weight"}};
+    const Span out[4] = {{loss, t.row_bytes, "loss"}, {lse, t.row_bytes, "lse"}, {dx, t.x_bytes, "dx"}, {dw, t.w_bytes, "dw"}};
+    for (int i = 0; i < (gradients ? 4 : 2); ++i) {
+      for (const Span& s : in) need_apart(out[i], s);
+      for (int j = 0; j < i; ++j) need_apart(out[i], out[j]);
+    }
+    const petra::VocabPlan plan = t.plan(gradients);
+    need_workspace(workspace, workspace_bytes, plan.bytes);
+    if (empty && !gradients) return false;
+    t.a.x = x;
+    t.a.w = w;
+    t.a.targets = targets;
+    t.a.weight = weight;
+    t.a.loss = loss;
+    t.a.lse = lse;
+    t.a.dx = dx;
+    t.a.dw = dw;
+    petra::vocab_run(t.a, plan, t.dtype, gradients, workspace, static_cast<hipStream_t>(stream));
+    return true;
+  });
+}
+
+}  // namespace
+
+extern "C" {
+
+petra_status petra_vocab_query(const petra_vocab_desc* desc, size_t* loss_bytes, size_t* gradient_bytes) {
+  return entry("petra_vocab_query", [&]() -> bool {
+    const Vocab t(desc);
+    if (loss_bytes != nullptr) *loss_bytes = t.plan(false).bytes;
+    if (gradient_bytes != nullptr) *gradient_bytes = t.plan(true).bytes;
+    return false;
+  });
+}
+
+petra_status petra_vocab_loss(const petra_vocab_desc* desc, const void* x, const void* w, const int32_t* targets, float* loss,
+                              float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  return vocab_call("petra_vocab_loss", desc, x, w, targets, nullptr, loss, lse, nullptr, nullptr, false, workspace,
+                    workspace_bytes, stream);
+}
+
+petra_status petra_vocab_gradient(const petra_vocab_desc* desc, const void* x, const void* w, const int32_t* targets,
+                                  const float* weight, float* loss, float* lse, void* dx, void* dw, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  return vocab_call("petra_vocab_gradient", desc, x, w, targets, weight, loss, lse, dx, dw, true, workspace, workspace_bytes,
+                    stream);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// AdamW
+// ---------------------------------------------------------------------------
+
+namespace {
+
+constexpr size_t ADAMW_WORKSPACE = 16;
+
+struct AdamwTable {
+  int64_t chunks = 0;
+  size_t bytes = 0;
+};
+
+size_t adamw_bytes(int64_t count, int64_t chunks) {
+  return (static_cast<size_t>(count) * sizeof(petra::AdamwEntry) + static_cast<size_t>(chunks) * 4 + 15) / 16 * 16;
+}
+
+void need_adamw(const petra_adamw_desc* d) {
+  need(d != nullptr, PETRA_ERR_INVALID_ARG, "null description");
+  need(d->beta1 >= 0. && d->beta1 < 1. && d->beta2 >= 0. && d->beta2 < 1., PETRA_ERR_INVALID_ARG, "betas outside [0, 1)");
+  need(d->eps > 0.f && std::isfinite(d->eps), PETRA_ERR_INVALID_ARG, "eps must be positive and finite");
+  need_dtype(d->grad_dtype);
+  need(d->state_dtype == PETRA_FP32 || d->state_dtype == PETRA_E4M3, PETRA_ERR_DTYPE, "states must be fp32 or e4m3");
+}
+
+AdamwTable adamw_table(const petra_adamw_desc* d, const petra_adamw_tensor* tensors, int64_t count) {
+  need_adamw(d);
+  need(count >= 0 && count <= (int64_t{1} << 20), PETRA_ERR_SHAPE, "negative or too large count");
+  need(count == 0 || tensors != nullptr, PETRA_ERR_INVALID_ARG, "null pointer: tensors");
+  AdamwTable t;
+  for (int64_t i = 0; i < count; ++i) {
+    need(tensors[i].n >= 0 && tensors[i].n <= (int64_t{1} << 42), PETRA_ERR_SHAPE, "negative or too large tensor");
+    t.chunks += (tensors[i].n + petra::ADAMW_CHUNK - 1) / petra::ADAMW_CHUNK;
+    need(t.chunks < (int64_t{1} << 31), PETRA_ERR_SHAPE, "too many elements");
+  }
+  t.bytes = adamw_bytes(count, t.chunks);
+  return t;
+}
+
+}  // namespace
+
+extern "C" {
+
+petra_status petra_adamw_query(const petra_adamw_desc* desc, const petra_adamw_tensor* tensors, int64_t count,
+                               size_t* table_bytes, int64_t* chunks, size_t* workspace_bytes) {
+  return entry("petra_adamw_query", [&]() -> bool {
+    const AdamwTable t = adamw_table(desc, tensors, count);
+    if (table_bytes != nullptr) *table_bytes = t.bytes;
+    if (chunks != nullptr) *chunks = t.chunks;
+    if (workspace_bytes != nullptr) *workspace_bytes = ADAMW_WORKSPACE;
+    return false;
+  });
+}
+
+petra_status petra_adamw_layout(const petra_adamw_desc* desc, const petra_adamw_tensor* tensors, int64_t count, void* table,
+                                size_t table_bytes) {
+  return entry("petra_adamw_layout", [&]() -> bool {
+    const AdamwTable t = adamw_table(desc, tensors, count);
+    need(t.bytes == 0 || (table != nullptr && table_bytes >= t.bytes), PETRA_ERR_WORKSPACE, "table missing or too small");
+    const bool fp8 = desc->state_dtype == PETRA_E4M3;
+    const size_t gsz = size_of(desc->grad_dtype);
+    // each range of memory once: a step works on all tensors at the same time
+    std::vector<Span> all;
+    for (int64_t i = 0; i < count; ++i) {
+      const petra_adamw_tensor& x = tensors[i];
+      const bool empty = x.n == 0;
+      need(std::isfinite(x.weight_decay), PETRA_ERR_INVALID_ARG, "weight_decay must be finite");
+      need_ptr(x.theta, "theta", empty);
+      need_ptr(x.grad, "grad", empty);
+      need_ptr(x.m, "m", empty);
+      need_ptr(x.v, "v", empty);
+      need_ptr(x.copy, "copy", empty || x.copy == nullptr);
+      for (float* const scale : {x.m_scale, x.v_scale}) {
+        if (!fp8 || empty) continue;
+        need(scale != nullptr, PETRA_ERR_INVALID_ARG, "null pointer: m_scale or v_scale");
+        need_int_ptr(scale, "m_scale or v_scale", 4);
+      }
+      if (empty) continue;
+      const size_t n = static_cast<size_t>(x.n), blocks = (n + 63) / 64, state = fp8 ? 64 * blocks : 4 * n;
+      all.push_back({x.theta, 4 * n, "theta"});
+      all.push_back({x.grad, gsz * n, "grad"});
+      all.push_back({x.m, state, "m"});
+      all.push_back({x.v, state, "v"});
+      if (x.copy != nullptr) all.push_back({x.copy, 2 * n, "copy"});
+      if (fp8) {
+        all.push_back({x.m_scale, 4 * blocks, "m_scale"});
+        all.push_back({x.v_scale, 4 * blocks, "v_scale"});
+      }
+    }
+    std::sort(all.begin(), all.end(), [](const Span& a, const Span& b) {
+      return reinterpret_cast<uintptr_t>(a.p) < reinterpret_cast<uintptr_t>(b.p);
+    });
+    for (size_t i = 1; i < all.size(); ++i) need_apart(all[i - 1], all[i]);
+    auto* const entries = static_cast<petra::AdamwEntry*>(table);
+    auto* const chunk_of = reinterpret_cast<int32_t*>(entries + count);
+    int64_t chunk = 0, group = 0;
+    for (int64_t i = 0; i < count; ++i) {
+      const petra_adamw_tensor& x = tensors[i];
+      const int64_t padded = (x.n + 63) / 64 * 64;
+      entries[i] = {x.theta, x.grad, x.m, x.v, x.copy, x.m_scale, x.v_scale, x.n, padded, chunk, group, x.weight_decay, 0};
+      group += padded / 4;
+      for (int64_t c = 0; c < x.n; c += petra::ADAMW_CHUNK) chunk_of[chunk++] = static_cast<int32_t>(i);
+    }
+    return false;
+  });
+}
+
+petra_status petra_adamw_step(const petra_adamw_desc* desc, const void* table, size_t table_bytes, int64_t count,
+                              int64_t chunks, int64_t* steps, const float* lr, const float* grad_scale, const uint64_t* rng,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  return entry("petra_adamw_step", [&]() -> bool {
+    need_adamw(desc);
+    need(count >= 0 && count <= (int64_t{1} << 20) && chunks >= 0 && chunks < (int64_t{1} << 31), PETRA_ERR_SHAPE,
+         "negative or too large count");
+    need(chunks == 0 || table != nullptr, PETRA_ERR_INVALID_ARG, "null pointer: table");
+    need(table_bytes >= adamw_bytes(count, chunks), PETRA_ERR_WORKSPACE, "table too small for its tensors and chunks");
+    need_ptr(table, "table", table == nullptr);
+    if (steps == nullptr) throw Refused{PETRA_ERR_INVALID_ARG, "null pointer: steps"};
+    if (lr == nullptr) throw Refused{PETRA_ERR_INVALID_ARG, "null pointer: lr"};
+    need_int_ptr(steps, "steps", 8);
+    need_int_ptr(lr, "lr", 4);
+    need_int_ptr(grad_scale, "grad_scale", 4);
+    need_int_ptr(rng, "rng", 8);
+    const bool fp8 = desc->state_dtype == PETRA_E4M3;
+    need(!fp8 || rng != nullptr, PETRA_ERR_INVALID_ARG, "states in 8 bits without rng");
+    need_workspace(workspace, workspace_bytes, ADAMW_WORKSPACE);
+    petra::AdamwArgs a{};
+    a.entries = static_cast<const petra::AdamwEntry*>(table);
+    a.chunk_of = reinterpret_cast<const int32_t*>(a.entries + count);
+    a.chunks = chunks;
+    a.steps = steps;
+    a.lr = lr;
+    a.grad_scale = grad_scale;
+    a.rng = rng;
+    a.hyper = static_cast<float*>(workspace);
+    a.log_b1 = std::log(desc->beta1);
+    a.log_b2 = std::log(desc->beta2);
+    a.b1 = static_cast<float>(desc->beta1);
+    a.c1 = static_cast<float>(1. - desc->beta1);
+    a.b2 = static_cast<float>(desc->beta2);
+    a.c2 = static_cast<float>(1. - desc->beta2);
+    a.eps = desc->eps;
+    a.zero_grads = desc->zero_grads != 0;
+    petra::adamw_step(a, desc->grad_dtype == PETRA_BF16, fp8, static_cast<hipStream_t>(stream));
     return true;
   });
 }

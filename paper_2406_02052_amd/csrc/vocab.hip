@@ -1,0 +1,673 @@
+// The loss over a large vocabulary and its gradients, without a rows x vocabulary tensor.
+//
+//   s_ij = scale x_i . w_j,  lse_i = log sum_j exp s_ij,  loss_i = lse_i - s_it  (t: the row's target)
+//   dx_i = scale weight_i sum_j (p_ij - [j = t]) w_j,  dw_j = scale sum_i weight_i (p_ij - [j = t]) x_i
+//
+// Three products of 2 rows width vocabulary operations each; bound by them for all but a few rows.
+// The rows go in pieces, of which one at a time is held as e_ij = exp(s_ij - s_it) in the storage type: the
+// target's score is known before the product and a softmax may take any reference, so that
+// Z_i = sum_j e_ij = exp(loss_i), and both gradients are products of e as it lies:
+//   f_i = scale weight_i / Z_i,  e'_it = e_it - Z_i,  dx_i = f_i sum_j e'_ij w_j,  dw_j = sum_i e'_ij (f_i x_i)
+// where a maximum as the reference would have e rescaled, or the first product made twice.  bf16
+// has the exponents of fp32; a tile with scores of more than 2^86 times the target's takes its own largest as the
+// reference, and the row's e are brought to one when all are known.
+//
+// Scores, sums, statistics and accumulators are fp32.  With bf16 tensors e and f x are rounded to bf16 as
+// operands of the products (the matrix unit takes bf16), 2^-9 of each term at most.
+#include "common.h"
+#include "ops.h"
+
+namespace petra {
+
+namespace {
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
+
+constexpr float LN2 = 0.69314718055994530942f;
+constexpr float MOST = 86.f;                  // log2 of the largest e; sums of 2^31 of them fit fp32
+constexpr float INF = __builtin_huge_valf();
+
+__device__ __forceinline__ f32x16_t mfma32(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16_t mfma32(const Frag<float>& a, const Frag<float>& b, f32x16_t c) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], c, 0, 0, 0);
+  return c;
+}
+
+// ---------------------------------------------------------------------------
+// tiles of a product's operands in LDS
+// ---------------------------------------------------------------------------
+
+// FREE free indices by 128 bytes of the inner index, as they lie in memory: lines of the inner index (ALONG), or lines of
+// the free one.  Chunks of 16 bytes are moved within a line by an exclusive or with a key of the line, so that the 16
+// lanes of a straight read (16 lines at one chunk) and the 32 of a transposing one (4 lines at 4 chunks) meet different banks.
+template <typename T, int FREE, bool ALONG, int THREADS>
+struct Panel {
+  static constexpr int INNER = 128 / static_cast<int>(sizeof(T));
+  static constexpr int LINES = ALONG ? FREE : INNER, CHUNKS = ALONG ? 8 : FREE * static_cast<int>(sizeof(T)) / 16;
+  static constexpr int BYTES = FREE * 128, N = BYTES / 16 / THREADS, PER = 16 / static_cast<int>(sizeof(T));
+  static_assert(BYTES % (16 * THREADS) == 0, "whole chunks a thread");
+  uint32_t off[N];
+  const T* base;
+  int64_t ld, step;
+  int64_t left;              // elements of the tensor from `base` on
+
+  static __device__ __forceinline__ int key(int line) {
+    if constexpr (ALONG) return (line >> 1) & 7;
+    else if constexpr (sizeof(T) == 2) return ((line & 3) << 2) & (CHUNKS - 1);
+    else return line & 8;
+  }
+  static __device__ __forceinline__ int at(int line, int chunk) { return (line * CHUNKS + (chunk ^ key(line))) << 4; }
+  static __device__ __forceinline__ int line(int i) { return (i * THREADS + static_cast<int>(threadIdx.x)) / CHUNKS; }
+  static __device__ __forceinline__ int chunk(int i) {
+    const int place = i * THREADS + static_cast<int>(threadIdx.x), l = place / CHUNKS;
+    return (place - l * CHUNKS) ^ key(l);
+  }
+
+  // Free indices first .. of `free` and inner ones from k0 of a matrix at p, `inner` wide, lines ld apart.
+  __device__ __forceinline__ void begin(const T* p, int64_t ld_, long first, long free, long k0, long inner) {
+    ld = ld_;
+    if constexpr (ALONG) {
+      base = p + first * ld + k0;
+      left = (free - first - 1) * ld + inner - k0;
+      step = INNER;
+    } else {
+      base = p + k0 * ld + first;
+      left = (inner - k0 - 1) * ld + free - first;
+      step = INNER * ld;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t o = (static_cast<uint32_t>(line(i)) * static_cast<uint32_t>(ld) + chunk(i) * PER) * static_cast<uint32_t>(sizeof(T));
+      // (past the last line: past `left`)
+      off[i] = !ALONG && first + chunk(i) * PER >= free ? BUF_OOB : o;
+    }
+  }
+  // Asks for the next tile, of which `inner` inner indices exist, and goes on.  The loads are written out: the compiler would
+  // let every later transposing LDS read wait for them.  They write no register; arrived() waits for them.
+  __device__ __forceinline__ void load(char* lds, long inner) {
+    const uint64_t from = reinterpret_cast<uint64_t>(base);
+    const int64_t bytes = left * static_cast<int64_t>(sizeof(T));
+    const uint32_t most = inner <= 0 || bytes <= 0 ? 0u : bytes < 0x7fffffff ? static_cast<uint32_t>(bytes) : 0x7fffffffu;
+    const u32x4_t r = {static_cast<uint32_t>(from), static_cast<uint32_t>(from >> 32) & 0xffffu, most, 0x00020000u};
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t to = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds)) + wave * 1024;
+    const bool part = ALONG && inner < INNER;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t o = part && chunk(i) * PER >= inner ? BUF_OOB : off[i];
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   ::"s"(to + i * THREADS * 16), "v"(o), "s"(r) : "memory");
+    }
+    base += step;
+    left -= step;
+  }
+  // This lane's operand: free index free0 + (lane & 31), inner ones 16 k + 8 (lane >> 5) .. + 7.
+  static __device__ __forceinline__ Frag<T> get(char* lds, int free0, int k, int lane) {
+    Frag<T> f;
+    const int h = lane >> 5;
+    if constexpr (ALONG) {
+      const int l = free0 + (lane & 31);
+      if constexpr (sizeof(T) == 2) {
+        f.v = *reinterpret_cast<const bf16x8_t*>(lds + at(l, 2 * k + h));
+      } else {
+        const float4 a = *reinterpret_cast<const float4*>(lds + at(l, 4 * k + 2 * h));
+        const float4 b = *reinterpret_cast<const float4*>(lds + at(l, 4 * k + 2 * h + 1));
+        f.v[0] = a.x; f.v[1] = a.y; f.v[2] = a.z; f.v[3] = a.w;
+        f.v[4] = b.x; f.v[5] = b.y; f.v[6] = b.z; f.v[7] = b.w;
+      }
+    } else if constexpr (sizeof(T) == 2) {
+      const int l = 16 * k + 8 * h + ((lane & 15) >> 2), col = free0 + (lane & 16) + 4 * (lane & 3);
+      const int in = (col & 7) * 2;
+      const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lds + at(l, col >> 3) + in));
+      const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lds + at(l + 4, col >> 3) + in));
+      f.v = __builtin_bit_cast(bf16x8_t, s16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    } else {
+      const int col = free0 + (lane & 31);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        f.v[j] = *reinterpret_cast<const float*>(lds + at(16 * k + 8 * h + j, col >> 2) + 4 * (col & 3));
+    }
+    return f;
+  }
+};
+
+template <int N> struct Const { static constexpr int value = N; };
+
+// All but the newest LOADS of this wave's loads to LDS have arrived, this wave has read what it asked LDS for, and every wave
+// is here.
+template <int LOADS>
+__device__ __forceinline__ void arrived() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+}
+
+// A tile of a product: BM x BN results of A's and B's free indices, by WM x WN waves, in BUFS buffers.  A wave has (BM / WM) x
+// (BN / WN) results as blocks of 32 x 32, a row (A's free index) a lane and in lane half h the columns 8 g + 4 h + {0..3}: what a
+// row needs, its sums or its factor, is then a lane's.
+template <typename T, int BM_, int BN_, int WM_, int WN_, int BUFS_, bool A_ALONG, bool B_ALONG>
+struct Product {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BUFS = BUFS_, THREADS = 64 * WM * WN;
+  static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;
+  using A = Panel<T, BM, A_ALONG, THREADS>;
+  using B = Panel<T, BN, B_ALONG, THREADS>;
+  static constexpr int BUF = A::BYTES + B::BYTES, LDS = BUFS * BUF, INNER = A::INNER, LOADS = A::N + B::N;
+
+  // acc += the inner indices k0 .. k1 (k0 a multiple of INNER); a.begin() and b.begin() have been called at k0.
+  static __device__ __forceinline__ void run(A& a, B& b, long k0, long k1, char* lds, f32x16_t (&acc)[MB][NB]) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m0 = wave / WN * (BM / WM), n0 = wave % WN * (BN / WN);
+    const int steps = static_cast<int>((k1 - k0 + INNER - 1) / INNER);
+    auto fetch = [&](int s, char* to) {
+      const long inner = k1 - k0 - static_cast<long>(s) * INNER;
+      a.load(to, inner);
+      b.load(to + A::BYTES, inner);
+    };
+#pragma unroll
+    for (int s = 0; s < BUFS - 1; ++s) fetch(s, lds + s * BUF);
+    auto body = [&](int s, auto buf) {
+      constexpr int I = decltype(buf)::value;
+      char* const at = lds + I * BUF;
+      arrived<(BUFS - 2) * LOADS>();
+      fetch(s + BUFS - 1, lds + (I + BUFS - 1) % BUFS * BUF);   // (past the end: nothing)
+#pragma unroll
+      for (int k = 0; k < INNER / 16; ++k) {
+        Frag<T> fa[MB], fb[NB];
+#pragma unroll
+        for (int i = 0; i < MB; ++i) fa[i] = A::get(at, m0 + 32 * i, k, lane);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) fb[j] = B::get(at + A::BYTES, n0 + 32 * j, k, lane);
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+          for (int j = 0; j < NB; ++j) acc[i][j] = mfma32(fb[j], fa[i], acc[i][j]);
+      }
+    };
+    for (int s = 0; s < steps; s += BUFS) {
+      body(s, Const<0>{});
+      if constexpr (BUFS > 1) if (s + 1 < steps) body(s + 1, Const<1 % BUFS>{});
+      if constexpr (BUFS > 2) if (s + 2 < steps) body(s + 2, Const<2 % BUFS>{});
+      if constexpr (BUFS > 3) if (s + 3 < steps) body(s + 3, Const<3 % BUFS>{});
+    }
+    arrived<0>();   // LDS is free
+  }
+  static __device__ __forceinline__ void zero(f32x16_t (&acc)[MB][NB]) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  }
+};
+
+// The tile of workgroup `id` of ms x ns: each of the 8 XCDs, which take workgroups in turn, has a run of tiles, in groups of 8 along
+// m with m fastest, so that the 32 workgroups of an XCD share 8 + 4 panels through its L2.
+__device__ __forceinline__ void tile_of(int id, int ms, int ns, int& m, int& n) {
+  const int all = ms * ns, per = all / 8, more = all % 8;
+  const int x = id & 7;
+  const int t = x * per + (x < more ? x : more) + (id >> 3);
+  const int group = t / (8 * ns), in = t - group * 8 * ns;
+  const int size = ms - group * 8 < 8 ? ms - group * 8 : 8;
+  n = in / size;
+  m = group * 8 + in - n * size;
+}
+
+// ---------------------------------------------------------------------------
+// rows
+// ---------------------------------------------------------------------------
+
+// Whether a row takes part: its target is a column.
+__device__ __forceinline__ bool takes_part(const VocabArgs& a, long row) {
+  return static_cast<uint32_t>(a.targets[row]) < static_cast<uint32_t>(a.vocab);
+}
+
+__device__ __forceinline__ float wave_sum(float v) { return sum_halves(sum_quarters(sum16(v))); }
+__device__ __forceinline__ float max16f(float v) {
+  auto over = [](float x, auto dpp) {
+    return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(dpp)::value, 0xF, 0xF, false)));
+  };
+  v = over(v, Const<0xB1>{});
+  v = over(v, Const<0x4E>{});
+  v = over(v, Const<0x141>{});
+  return over(v, Const<0x140>{});
+}
+
+// A row's reference, its target's score in binary logarithms, a wave a row.
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_target_kernel(VocabArgs a) {
+  const long row = static_cast<long>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (row >= a.rows) return;
+  const int lane = threadIdx.x & 63;
+  if (!takes_part(a, row)) return;
+  const int t = a.targets[row];
+  const T* const x = static_cast<const T*>(a.x) + row * a.width;
+  const T* const w = static_cast<const T*>(a.w) + static_cast<long>(t) * a.width;
+  float s = 0.f;
+  for (int c = lane * 8; c < a.width; c += 512) {
+    float p[8], q[8];
+    Vec8<T>::load(x + c, p);
+    Vec8<T>::load(w + c, q);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fmaf(p[e], q[e], s);
+  }
+  s = wave_sum(s);
+  if (lane == 0) a.ref[row] = s * a.scale_log2;
+}
+
+// 1 / (the rows that take part).
+__global__ __launch_bounds__(1024) void vocab_mean_kernel(VocabArgs a) {
+  __shared__ int counts[16];
+  int n = 0;
+  for (long r = threadIdx.x; r < a.rows; r += 1024) n += takes_part(a, r);
+  for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d, 64);
+  if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int all = 0;
+    for (int i = 0; i < 16; ++i) all += counts[i];
+    *a.mean = 1.f / static_cast<float>(all > 1 ? all : 1);
+  }
+}
+
+// e of a tile and each row's sum of it.  One of (KEEP) e kept, or the sums alone.
+template <typename T, typename P, bool KEEP>
+__global__ __launch_bounds__(P::THREADS, 2) void vocab_scores_kernel(VocabArgs a) {
+  __shared__ __attribute__((aligned(16))) char lds[P::LDS];
+  int mt, nt;
+  tile_of(blockIdx.x, a.row_tiles, a.col_tiles, mt, nt);
+  const long m0 = static_cast<long>(mt) * P::BM, n0 = static_cast<long>(nt) * P::BN;
+  f32x16_t acc[P::MB][P::NB];
+  P::zero(acc);
+  {
+    typename P::A pa;
+    typename P::B pb;
+    pa.begin(static_cast<const T*>(a.x) + a.row0 * a.width, a.width, m0, a.piece, 0, a.width);
+    pb.begin(static_cast<const T*>(a.w), a.width, n0, a.vocab, 0, a.width);
+    P::run(pa, pb, 0, a.width, lds, acc);
+  }
+  const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / P::WN * (P::BM / P::WM) + (lane & 31), wn = wave % P::WN * (P::BN / P::WN) + 4 * h;
+  float* const shared = reinterpret_cast<float*>(lds);   // [wave column][row of the tile]
+  const bool edge = n0 + P::BN > a.vocab;
+  bool live[P::MB], over = false;
+  // binary logarithms of e; those past the vocabulary -inf
+#pragma unroll
+  for (int i = 0; i < P::MB; ++i) {
+    const long row = m0 + wm + 32 * i;
+    live[i] = row < a.piece && takes_part(a, a.row0 + row);
+    const float c = live[i] ? -a.ref[a.row0 + row] : 0.f;
+    float top = -INF;
+#pragma unroll
+    for (int j = 0; j < P::NB; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int n = wn + 32 * j + 8 * (e >> 2) + (e & 3);
+        float v = fmaf(acc[i][j][e], a.scale_log2, c);
+        if (edge && n0 + n >= a.vocab) v = -INF;
+        acc[i][j][e] = v;
+        top = fmaxf(top, v);
+      }
+    over |= top > MOST && live[i];
+  }
+  // rows that need another reference are rare: their whole tile takes the slow way
+  float shift[P::MB] = {};
+  const bool slow = __syncthreads_or(over);
+  if (slow) {
+#pragma unroll
+    for (int i = 0; i < P::MB; ++i) {
+      float top = -INF;
+#pragma unroll
+      for (int j = 0; j < P::NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[i][j][e]);
+      top = max_halves(top);
+      if (h == 0) shared[(wave % P::WN) * P::BM + wm + 32 * i] = top;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < P::MB; ++i) {
+      float top = -INF;
+#pragma unroll
+      for (int w = 0; w < P::WN; ++w) top = fmaxf(top, shared[w * P::BM + wm + 32 * i]);
+      shift[i] = top > MOST ? top : 0.f;
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < P::MB; ++i) {
+    const long row = m0 + wm + 32 * i;
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < P::NB; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = !live[i] ? 0.f : __builtin_amdgcn_exp2f(acc[i][j][4 * g + e] - shift[i]);
+          sum += v[e];
+        }
+        const long n = n0 + wn + 32 * j + 8 * g;
+        if (KEEP && row < a.piece && n < a.vocab_padded) {
+          T* const to = static_cast<T*>(a.e) + row * a.vocab_padded + n;
+          if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+          else *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
+        }
+      }
+    sum = sum_halves(sum);
+    if (h == 0) shared[(wave % P::WN) * P::BM + wm + 32 * i] = sum;
+    if (slow && h == 0 && wave % P::WN == 0 && row < a.piece) a.shift[row * a.col_tiles + nt] = shift[i];
+  }
+  __syncthreads();
+  for (int r = threadIdx.x; r < P::BM; r += P::THREADS) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < P::WN; ++w) s += shared[w * P::BM + r];
+    if (m0 + r < a.piece) a.sums[(m0 + r) * a.col_tiles + nt] = s;
+  }
+  if (threadIdx.x == 0) a.slow[static_cast<long>(mt) * a.col_tiles + nt] = slow;
+}
+
+// A row's Z, loss and lse from its tiles' sums; with gradients also its factor, f x, the target's e' and what had another
+// reference.  A workgroup a row.
+template <typename T, bool KEEP>
+__global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a) {
+  __shared__ float lds[8];
+  const long row = blockIdx.x, all = a.row0 + row;
+  const float* const sums = a.sums + row * a.col_tiles;
+  const float* const shifts = a.shift + row * a.col_tiles;
+  const int* const slow = a.slow + row / a.row_tile * a.col_tiles;
+  T* const scaled = KEEP ? static_cast<T*>(a.scaled) + row * a.width : nullptr;
+  if (!takes_part(a, all)) {
+    if (threadIdx.x == 0) {
+      a.loss[all] = 0.f;
+      a.lse[all] = 0.f;
+      if (KEEP) a.factor[row] = 0.f;
+    }
+    if (KEEP) {
+      const float none[8] = {};
+      for (int c = threadIdx.x * 8; c < a.width; c += 2048) Vec8<T>::store(scaled + c, none);
+    }
+    return;
+  }
+  const float ref = a.ref[all];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  float s = 0.f, top = 0.f;
+  for (int t = threadIdx.x; t < a.col_tiles; t += 256)
+    if (slow[t]) top = fmaxf(top, shifts[t]);
+  top = max_halves(max16f(fmaxf(top, __shfl_xor(top, 16, 64))));
+  if (lane == 0) lds[wave] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+  for (int t = threadIdx.x; t < a.col_tiles; t += 256)
+    s += top > 0.f ? sums[t] * __builtin_amdgcn_exp2f((slow[t] ? shifts[t] : 0.f) - top) : sums[t];
+  s = wave_sum(s);
+  if (lane == 0) lds[4 + wave] = s;
+  __syncthreads();
+  const float z = lds[4] + lds[5] + lds[6] + lds[7];
+  const float loss = LN2 * (top + log2f(z));
+  if (threadIdx.x == 0) {
+    a.loss[all] = loss;
+    a.lse[all] = fmaf(LN2, ref, loss);
+  }
+  if constexpr (KEEP) {
+    const float f = a.scale * (a.weight != nullptr ? a.weight[all] : *a.mean) / z;
+    if (threadIdx.x == 0) a.factor[row] = f;
+    T* const e = static_cast<T*>(a.e) + row * a.vocab_padded;
+    if (top > 0.f) {
+      for (int t = 0; t < a.col_tiles; ++t) {
+        const float d = (slow[t] ? shifts[t] : 0.f) - top;
+        if (d == 0.f) continue;
+        const float by = __builtin_amdgcn_exp2f(d);
+        for (int c = threadIdx.x; c < a.col_tile && t * a.col_tile + c < a.vocab; c += 256) {
+          T* const p = e + static_cast<long>(t) * a.col_tile + c;
+          store1(p, load1(p) * by);
+        }
+      }
+      __syncthreads();   // before the target's
+    }
+    if (threadIdx.x == 0) {
+      T* const p = e + a.targets[all];
+      store1(p, load1(p) - z);
+    }
+    const T* const x = static_cast<const T*>(a.x) + all * a.width;
+    for (int c = threadIdx.x * 8; c < a.width; c += 2048) {
+      float v[8];
+      Vec8<T>::load(x + c, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= f;
+      Vec8<T>::store(scaled + c, v);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// gradients
+// ---------------------------------------------------------------------------
+
+// Where a gradient's sums go: times the row's factor, added to what earlier pieces gave, and on to the tensor or to the sums
+// for the next piece.
+template <typename T>
+__device__ __forceinline__ void finish(const VocabGrad& g, long row, long col, float (&v)[4]) {
+  const long at = row * g.cols + col;
+  if (g.factor != nullptr) {
+    const float f = g.factor[row];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] *= f;
+  }
+  if (g.add) {
+    const float4 o = *reinterpret_cast<const float4*>(g.acc + at);
+    v[0] += o.x, v[1] += o.y, v[2] += o.z, v[3] += o.w;
+  }
+  if (!g.last) {
+    *reinterpret_cast<float4*>(g.acc + at) = make_float4(v[0], v[1], v[2], v[3]);
+  } else if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint2*>(static_cast<T*>(g.out) + at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  } else {
+    *reinterpret_cast<float4*>(static_cast<T*>(g.out) + at) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+}
+
+// rows x cols results, inner indices split over g.splits workgroups, whose sums then go to g.part.
+template <typename T, typename P>
+__global__ __launch_bounds__(P::THREADS, 2) void vocab_grad_kernel(VocabGrad g) {
+  __shared__ __attribute__((aligned(16))) char lds[P::LDS];
+  const int id = blockIdx.x / g.splits, split = blockIdx.x - id * g.splits;
+  int mt, nt;
+  tile_of(id, g.row_tiles, g.col_tiles, mt, nt);
+  const long m0 = static_cast<long>(mt) * P::BM, n0 = static_cast<long>(nt) * P::BN;
+  const long k0 = split * g.per_split, k1 = k0 + g.per_split < g.inner ? k0 + g.per_split : g.inner;
+  f32x16_t acc[P::MB][P::NB];
+  P::zero(acc);
+  {
+    typename P::A pa;
+    typename P::B pb;
+    pa.begin(static_cast<const T*>(g.a), g.a_ld, m0, g.a_free, k0, g.inner);
+    pb.begin(static_cast<const T*>(g.b), g.cols, n0, g.cols, k0, g.b_inner);
+    P::run(pa, pb, k0, k1, lds, acc);
+  }
+  const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+  for (int i = 0; i < P::MB; ++i) {
+    const long row = m0 + wave / P::WN * (P::BM / P::WM) + 32 * i + (lane & 31);
+    if (row >= g.rows) continue;
+#pragma unroll
+    for (int j = 0; j < P::NB; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const long col = n0 + wave % P::WN * (P::BN / P::WN) + 32 * j + 8 * q + 4 * h;
+        if (col >= g.cols) continue;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
+        if (g.splits > 1)
+          *reinterpret_cast<float4*>(g.part + (split * g.rows + row) * g.cols + col) = make_float4(v[0], v[1], v[2], v[3]);
+        else
+          finish<T>(g, row, col, v);
+      }
+  }
+}
+
+// Adds the splits' sums, 4 columns a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_add_kernel(VocabGrad g) {
+  const long all = g.rows * g.cols;
+  for (long at = (static_cast<long>(blockIdx.x) * 256 + threadIdx.x) * 4; at < all; at += static_cast<long>(gridDim.x) * 1024) {
+    float v[4] = {};
+    for (int s = 0; s < g.splits; ++s) {
+      const float4 o = *reinterpret_cast<const float4*>(g.part + s * all + at);
+      v[0] += o.x, v[1] += o.y, v[2] += o.z, v[3] += o.w;
+    }
+    const long row = at / g.cols;
+    finish<T>(g, row, at - row * g.cols, v);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+
+constexpr int TILE = 256;
+template <typename T, bool A, bool B> using Large = Product<T, 256, 256, 2, 4, 2, A, B>;
+
+long up(long x, long y) { return (x + y - 1) / y; }
+
+template <typename T>
+void scores(const VocabArgs& a, bool keep, hipStream_t s) {
+  using P = Large<T, true, true>;
+  const unsigned n = static_cast<unsigned>(a.row_tiles * a.col_tiles);
+  if (keep) vocab_scores_kernel<T, P, true><<<n, P::THREADS, 0, s>>>(a);
+  else vocab_scores_kernel<T, P, false><<<n, P::THREADS, 0, s>>>(a);
+}
+
+template <typename T>
+void add(const VocabGrad& g, hipStream_t s) {
+  const long n = up(g.rows * g.cols, 1024);
+  vocab_add_kernel<T><<<static_cast<unsigned>(n < 4096 ? n : 4096), 256, 0, s>>>(g);
+}
+
+template <typename T, typename P>
+void grad(VocabGrad& g, hipStream_t s) {
+  g.row_tiles = static_cast<int>(up(g.rows, P::BM));
+  g.col_tiles = static_cast<int>(up(g.cols, P::BN));
+  vocab_grad_kernel<T, P><<<static_cast<unsigned>(g.row_tiles * g.col_tiles * g.splits), P::THREADS, 0, s>>>(g);
+  if (g.splits > 1) add<T>(g, s);
+}
+
+// Splits of a product's inner index: as many as fill the 256 CUs, each of 8 tiles of it at least.
+void split(VocabGrad& g, long inner_tile) {
+  const long tiles = up(g.rows, TILE) * up(g.cols, TILE), steps = up(g.inner, inner_tile);
+  long n = tiles >= 192 ? 1 : 256 / tiles;
+  if (n > steps / 8) n = steps / 8;
+  if (n < 1) n = 1;
+  g.per_split = up(steps, n) * inner_tile;
+  g.splits = static_cast<int>(up(g.inner, g.per_split));
+}
+
+template <typename T>
+void run(const VocabArgs& all, const VocabPlan& p, bool gradients, hipStream_t s) {
+  VocabArgs a = all;
+  if (a.rows == 0) {   // nothing but the zeros of dw
+    VocabGrad none{};
+    none.rows = a.vocab, none.cols = a.width, none.out = a.dw, none.last = 1;
+    if (gradients) add<T>(none, s);
+    return;
+  }
+  vocab_target_kernel<T><<<static_cast<unsigned>(up(a.rows, 4)), 256, 0, s>>>(a);
+  if (gradients && a.weight == nullptr) vocab_mean_kernel<<<1, 1024, 0, s>>>(a);
+  a.col_tiles = static_cast<int>(up(a.vocab, TILE));
+  a.row_tile = a.col_tile = TILE;
+  for (a.row0 = 0; a.row0 < a.rows; a.row0 += p.piece) {
+    a.piece = a.rows - a.row0 < p.piece ? a.rows - a.row0 : p.piece;
+    a.row_tiles = static_cast<int>(up(a.piece, TILE));
+    scores<T>(a, gradients, s);
+    const unsigned n = static_cast<unsigned>(a.piece);
+    if (!gradients) {
+      vocab_join_kernel<T, false><<<n, 256, 0, s>>>(a);
+      continue;
+    }
+    vocab_join_kernel<T, true><<<n, 256, 0, s>>>(a);
+    VocabGrad x = p.dx, w = p.dw;
+    x.a = a.e, x.b = a.w, x.a_ld = a.vocab_padded, x.a_free = a.piece, x.b_inner = a.vocab, x.rows = a.piece, x.cols = a.width, x.inner = a.vocab_padded;
+    x.out = static_cast<T*>(a.dx) + a.row0 * a.width, x.factor = a.factor, x.part = a.part, x.last = 1;
+    grad<T, Large<T, true, false>>(x, s);
+    w.a = a.e, w.b = a.scaled, w.a_ld = w.a_free = a.vocab_padded, w.b_inner = a.piece, w.rows = a.vocab, w.cols = a.width, w.inner = a.piece;
+    w.out = a.dw, w.part = a.part, w.acc = a.acc, w.add = a.row0 > 0, w.last = a.row0 + a.piece == a.rows;
+    if (w.per_split >= w.inner) w.splits = 1;   // a last, smaller piece
+    else w.splits = static_cast<int>(up(w.inner, w.per_split));
+    grad<T, Large<T, false, false>>(w, s);
+  }
+}
+
+}  // namespace
+
+VocabPlan vocab_plan(const VocabArgs& a, int dtype, bool gradients, long piece_rows) {
+  const size_t esz = dtype == 1 ? 2 : 4;
+  const long inner_tile = 128 / static_cast<long>(esz);
+  VocabPlan p{};
+  // 2^30 bytes of e at a time, in whole tiles; of the sums 2^31
+  long most = gradients ? (1L << 30) / (a.vocab_padded * static_cast<long>(esz)) : (1L << 31) / (8 * up(a.vocab, TILE));
+  most = most / TILE * TILE;
+  if (most < TILE) most = TILE;
+  if (piece_rows > 0 && piece_rows < most) most = piece_rows;
+  const long rows = a.rows > 0 ? a.rows : 1;
+  p.piece = rows < most ? rows : most;
+  if (piece_rows <= 0) {   // pieces of one size
+    const long even = up(up(rows, up(rows, p.piece)), TILE) * TILE;
+    if (even < p.piece) p.piece = even;
+  }
+  const long tiles = up(a.vocab, TILE);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += (bytes + 255) / 256 * 256;
+    return here;
+  };
+  p.ref = take(static_cast<size_t>(a.rows) * 4);
+  p.sums = take(static_cast<size_t>(p.piece) * tiles * 4);
+  p.shift = take(static_cast<size_t>(p.piece) * tiles * 4);
+  p.slow = take(static_cast<size_t>(up(p.piece, TILE)) * tiles * 4);
+  if (gradients) {
+    p.mean = take(4);
+    p.factor = take(static_cast<size_t>(p.piece) * 4);
+    p.scaled = take(static_cast<size_t>(p.piece) * a.width * esz);
+    p.e = take(static_cast<size_t>(p.piece) * a.vocab_padded * esz);
+    p.dx.rows = p.piece, p.dx.cols = a.width, p.dx.inner = a.vocab_padded;
+    p.dw.rows = a.vocab, p.dw.cols = a.width, p.dw.inner = p.piece;
+    size_t part = 0;
+    for (VocabGrad* g : {&p.dx, &p.dw}) {
+      split(*g, inner_tile);
+      const size_t bytes = g->splits > 1 ? static_cast<size_t>(g->splits) * g->rows * g->cols * 4 : 0;
+      if (bytes > part) part = bytes;
+    }
+    p.part = take(part);
+    // sums over pieces; fp32 has them in dw itself
+    p.acc = take(esz == 2 && p.piece < a.rows ? static_cast<size_t>(a.vocab) * a.width * 4 : 0);
+  }
+  p.bytes = at;
+  return p;
+}
+
+void vocab_run(VocabArgs a, const VocabPlan& p, int dtype, bool gradients, void* workspace, hipStream_t s) {
+  char* const ws = static_cast<char*>(workspace);
+  a.ref = reinterpret_cast<float*>(ws + p.ref);
+  a.sums = reinterpret_cast<float*>(ws + p.sums);
+  a.shift = reinterpret_cast<float*>(ws + p.shift);
+  a.slow = reinterpret_cast<int*>(ws + p.slow);
+  if (gradients) {
+    a.mean = reinterpret_cast<float*>(ws + p.mean);
+    a.factor = reinterpret_cast<float*>(ws + p.factor);
+    a.scaled = ws + p.scaled;
+    a.e = ws + p.e;
+    a.part = reinterpret_cast<float*>(ws + p.part);
+    a.acc = dtype == 1 ? reinterpret_cast<float*>(ws + p.acc) : static_cast<float*>(a.dw);
+  }
+  if (dtype == 1) run<bf16_t>(a, p, gradients, s);
+  else run<float>(a, p, gradients, s);
+}
+
+}  // namespace petra

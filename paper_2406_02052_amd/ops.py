@@ -1,5 +1,6 @@
 """Owners of the workspaces of the token operators around the C ABI: attention,
-the coupling of a residual function to its stream, and dropout.
+the coupling of a residual function to its stream, dropout, the norms and rotation
+of heads, the loss over a vocabulary and AdamW.
 
 Marshalling only, as in stage.py.  Tensors are the caller's; their types, shapes
 and strides are checked here, everything else by the library.  A workspace holds
@@ -194,3 +195,240 @@ def dropout(x, y, p: float, rng, residual=None, alpha: float = 1.0, stream=None)
         _need_rng(rng)
     L.petra_dropout(x.numel(), L.PETRA_BF16 if x.dtype is torch.bfloat16 else L.PETRA_FP32, p,
                     alpha, x, residual, rng, y, stream)
+
+
+class HeadNorm(_Owner):
+    """Norms of query and key heads with the rotation by their tokens' positions, over
+    [batch, length, heads, head_dim] and [batch, length, kv_heads, head_dim] tensors (any strides
+    of the first three dimensions; channels contiguous).
+
+    freq: radians a position of each pair of channels, by default 10000^(-i / (head_dim / 2)) for
+    i < head_dim / 2, () for no rotation; axis: the axis of positions of each pair (default 0).
+    layout: the pairs are channels (i, i + pairs), 'halves', or (2 i, 2 i + 1), 'neighbours'.
+    kv_heads = 0: queries only."""
+
+    def __init__(self, batch: int, length: int, heads: int, kv_heads: int, head_dim: int,
+                 dtype: str = "bf16", norm: str | None = "rms", eps: float = 1e-6,
+                 layout: str = "halves", freq=None, axis=None, device: str = "cuda"):
+        import torch
+        code, self.tdtype = _types(dtype)
+        if norm not in ("rms", "layer", None):
+            raise ValueError(f"norm must be 'rms', 'layer' or None, got {norm!r}")
+        if layout not in ("halves", "neighbours"):
+            raise ValueError(f"layout must be 'halves' or 'neighbours', got {layout!r}")
+        if freq is None:
+            freq = [10000.0 ** (-2.0 * i / head_dim) for i in range(head_dim // 2)]
+        freq = [float(f) for f in freq]
+        axis = [0] * len(freq) if axis is None else [int(a) for a in axis]
+        if len(freq) > L.PETRA_HEAD_PAIRS or len(axis) != len(freq):
+            raise ValueError(f"need an axis for each of at most {L.PETRA_HEAD_PAIRS} frequencies, "
+                             f"got {len(axis)} and {len(freq)}")
+        self.norm = norm
+        self.axes = max(axis, default=0) + 1
+        self.shapes = ((batch, length, heads, head_dim), (batch, length, kv_heads, head_dim))
+        self.param_shape, self.positions_shape = (head_dim,), (self.axes, batch, length)
+        self.itype, self.ftype = torch.int32, torch.float32
+        self.desc = L.HeadsDesc(batch, length, heads, kv_heads, head_dim, code,
+                                L.PETRA_NORM_LAYER if norm == "layer" else L.PETRA_NORM_RMS, eps,
+                                L.PETRA_PAIRS_HALVES if layout == "halves" else
+                                L.PETRA_PAIRS_NEIGHBOURS, len(freq), self.axes)
+        for i, (f, a) in enumerate(zip(freq, axis)):
+            self.desc.freq[i], self.desc.axis[i] = f, a
+        self.form = None
+        self._own(L.petra_heads_query(self.desc), device)
+
+    def _lay(self, x, y, norms, positions) -> None:
+        """x: (name, tensor) of q and k or their gradients, y likewise of the results; None for
+        the keys where there are none.  Puts their strides into the description; what was checked
+        last (types, shapes and strides) is not checked again."""
+        form = tuple((n, t.shape, t.stride(), t.dtype, t.is_cuda) if t is not None else None
+                     for n, t in x + y)
+        if form != self.form:
+            self.form = None
+            for fields, pair in ((("q_stride", "k_stride"), x), (("yq_stride", "yk_stride"), y)):
+                for (name, t), field, shape in zip(pair, fields, self.shapes):
+                    if shape[2] == 0 and t is None:
+                        continue
+                    _need(t, name, self.tdtype, shape, dense=False)
+                    setattr(self.desc, field, self._strides(t, name))
+            self.form = form
+        for name, p in norms:
+            if p is None:
+                continue
+            if self.norm is None:
+                raise ValueError(f"{name}: this owner has no norm")
+            _need(p[0], name, self.ftype, self.param_shape)
+            if p[1] is not None:
+                _need(p[1], name, self.ftype, self.param_shape)
+        if positions is not None:
+            _need(positions, "positions", self.itype, self.positions_shape)
+
+    @staticmethod
+    def _strides(t, name: str):
+        st = t.stride()
+        if st[3] != 1 and t.shape[3] > 1:
+            raise ValueError(f"{name}: channels must be contiguous, got strides {st}")
+        st = tuple(s if n > 1 else 0 for s, n in zip(st[:3], t.shape[:3]))
+        # (three zeros are a contiguous tensor's in the description)
+        if st == (0, 0, 0) and math.prod(t.shape[:3]) > 1:
+            raise ValueError(f"{name}: all positions share one vector")
+        return (L.ctypes.c_int64 * 3)(*st)
+
+    def forward(self, q, k, yq, yk, q_norm=None, k_norm=None, positions=None, stream=None) -> None:
+        """Writes yq and yk.  q_norm and k_norm: (gamma, beta or None), fp32; positions: int32
+        [axes, batch, length] (None: a token's index)."""
+        self._need_norms(q_norm, k_norm)
+        self._lay((("q", q), ("k", k)), (("yq", yq), ("yk", yk)),
+                  (("q_norm", q_norm), ("k_norm", k_norm)), positions)
+        L.petra_heads_forward(self.desc, q, k, q_norm, k_norm, positions, yq, yk, stream)
+
+    def backward(self, q, k, dyq, dyk, dq, dk, q_norm=None, k_norm=None, dq_norm=None,
+                 dk_norm=None, positions=None, stream=None) -> None:
+        """Writes dq, dk (strides of q and k) and the norms' parameters' gradients.  Without a
+        norm q and k may be None."""
+        self._need_norms(q_norm, k_norm)
+        self._lay((("dq", dq), ("dk", dk)), (("dyq", dyq), ("dyk", dyk)),
+                  (("q_norm", q_norm), ("k_norm", k_norm), ("dq_norm", dq_norm),
+                   ("dk_norm", dk_norm)), positions)
+        for t, name, like in ((q, "q", dq), (k, "k", dk)):
+            if t is None:
+                continue
+            _need(t, name, self.tdtype, like.shape, dense=False)
+            st, want = t.stride(), like.stride()
+            if st != want and any(x != y for x, y, n in zip(st, want, t.shape) if n > 1):
+                raise ValueError(f"{name}: need the strides of its gradient {want}, got {st}")
+        L.petra_heads_backward(self.desc, q, k, q_norm, k_norm, positions, dyq, dyk, dq, dk,
+                               dq_norm, dk_norm, self.workspace, self.ws_bytes, self._on(stream))
+
+    def _need_norms(self, q_norm, k_norm) -> None:
+        if self.norm is not None and (q_norm is None or (k_norm is None and self.shapes[1][2])):
+            raise ValueError(f"q_norm, k_norm: a {self.norm} norm needs its parameters")
+
+
+class VocabLoss(_Owner):
+    """Softmax cross entropy of scale x w^T over a vocabulary, without its logits: x [rows, width],
+    w [vocab, width], targets int32 [rows] (any that is no column takes its row out).
+
+    piece_rows: rows whose scores are held at a time, for less memory (0: within 1 GiB).
+    gradients=False: a workspace for the loss alone."""
+
+    def __init__(self, rows: int, width: int, vocab: int, dtype: str = "bf16", scale: float = 1.0,
+                 piece_rows: int = 0, gradients: bool = True, device: str = "cuda"):
+        import torch
+        code, self.tdtype = _types(dtype)
+        self.x_shape, self.w_shape, self.row_shape = (rows, width), (vocab, width), (rows,)
+        self.itype, self.ftype = torch.int32, torch.float32
+        self.desc = L.VocabDesc(rows, piece_rows, width, vocab, code, scale)
+        self.loss_bytes, self.gradient_bytes = L.petra_vocab_query(self.desc)
+        self._own(max(self.loss_bytes, self.gradient_bytes) if gradients else self.loss_bytes,
+                  device)
+
+    def _check(self, x, w, targets, loss, lse) -> None:
+        _need(x, "x", self.tdtype, self.x_shape)
+        _need(w, "w", self.tdtype, self.w_shape)
+        _need(targets, "targets", self.itype, self.row_shape)
+        _need(loss, "loss", self.ftype, self.row_shape)
+        _need(lse, "lse", self.ftype, self.row_shape)
+
+    def forward(self, x, w, targets, loss, lse, stream=None) -> None:
+        """Writes loss and lse, fp32 [rows]."""
+        self._check(x, w, targets, loss, lse)
+        L.petra_vocab_loss(self.desc, x, w, targets, loss, lse, self.workspace, self.ws_bytes,
+                           self._on(stream))
+
+    def gradient(self, x, w, targets, loss, lse, dx, dw, weight=None, stream=None) -> None:
+        """Writes loss, lse and the gradients of sum(weight * loss); weight: fp32 [rows] (None:
+        1 / the rows that take part)."""
+        self._check(x, w, targets, loss, lse)
+        _need(dx, "dx", self.tdtype, self.x_shape)
+        _need(dw, "dw", self.tdtype, self.w_shape)
+        if weight is not None:
+            _need(weight, "weight", self.ftype, self.row_shape)
+        L.petra_vocab_gradient(self.desc, x, w, targets, weight, loss, lse, dx, dw,
+                               self.workspace, self.ws_bytes, self._on(stream))
+
+
+class AdamW(_Owner):
+    """An AdamW step over many tensors: params (fp32) and their grads (fp32 or bf16, all of one
+    type), which the owner keeps and whose memory stays theirs.
+
+    states: 'fp32', or 'fp8' for 8 bits an element.  m and v (fp8: r = sqrt(v), as
+    float8_e4m3fn, with m_scale and v_scale for each 64 elements) are one tensor each for all, each
+    parameter's from a multiple of 64 on: m[starts[i]:starts[i] + n].  lr (fp32) and steps
+    (int64) are device tensors of one element, for the caller to set.  weight_decay: one for all, or
+    one for each.  copies: bf16 tensors that follow their parameters (None: none).  zero_grads: each
+    step sets the gradients to 0."""
+
+    def __init__(self, params, grads, states: str = "fp32", lr: float = 1e-3,
+                 betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01, copies=None,
+                 zero_grads: bool = False):
+        import torch
+        if states not in ("fp32", "fp8"):
+            raise ValueError(f"states must be 'fp32' or 'fp8', got {states!r}")
+        self.params, self.grads = list(params), list(grads)
+        self.copies = [None] * len(self.params) if copies is None else list(copies)
+        try:
+            decay = [float(d) for d in weight_decay]
+        except TypeError:
+            decay = [float(weight_decay)] * len(self.params)
+        if not self.params:
+            raise ValueError("params: need at least one tensor")
+        if not len(self.params) == len(self.grads) == len(self.copies) == len(decay):
+            raise ValueError(f"need as many of each: {len(self.params)} params, {len(self.grads)} "
+                             f"grads, {len(self.copies)} copies, {len(decay)} weight decays")
+        device, gtype = self.params[0].device, self.grads[0].dtype
+        if gtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"grads: need float32 or bfloat16, got {gtype}")
+        for i, (p, g, c) in enumerate(zip(self.params, self.grads, self.copies)):
+            _need(p, f"params[{i}]", torch.float32, p.shape)
+            _need(g, f"grads[{i}]", gtype, p.shape)
+            if c is not None:
+                _need(c, f"copies[{i}]", torch.bfloat16, p.shape)
+            if any(t is not None and t.device != device for t in (p, g, c)):
+                raise ValueError(f"params[{i}]: need all tensors on {device}")
+        fp8, at = states == "fp8", 0
+        self.starts = []
+        for p in self.params:
+            self.starts.append(at)
+            at += -(-p.numel() // 64) * 64
+        # (zeros of a type with no fill of its own)
+        self.m, self.v = (torch.zeros(at, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+                          if fp8 else torch.zeros(at, device=device) for _ in range(2))
+        self.m_scale, self.v_scale = ((torch.zeros(at // 64, device=device) for _ in range(2))
+                                      if fp8 else (None, None))
+        self.lr = torch.full((1,), lr, device=device)
+        self.steps = torch.zeros(1, dtype=torch.int64, device=device)
+        self.fp8, self.ftype = fp8, torch.float32
+        self.desc = L.AdamwDesc(betas[0], betas[1], eps,
+                                L.PETRA_BF16 if gtype is torch.bfloat16 else L.PETRA_FP32,
+                                L.PETRA_E4M3 if fp8 else L.PETRA_FP32, int(zero_grads))
+        self.count = len(self.params)
+        tensors = (L.AdamwTensor * self.count)()
+        size = 1 if fp8 else 4
+        # scales of a tensor begin at any multiple of 4 bytes in theirs: blocks of 64
+        for t, p, g, c, d, start in zip(tensors, self.params, self.grads, self.copies, decay,
+                                        self.starts):
+            t.theta, t.grad, t.n, t.weight_decay = p.data_ptr(), g.data_ptr(), p.numel(), d
+            t.m, t.v = self.m.data_ptr() + size * start, self.v.data_ptr() + size * start
+            if fp8:
+                t.m_scale = self.m_scale.data_ptr() + start // 64 * 4
+                t.v_scale = self.v_scale.data_ptr() + start // 64 * 4
+            t.copy = None if c is None else c.data_ptr()
+        self.table_bytes, self.chunks, ws_bytes = L.petra_adamw_query(self.desc, tensors,
+                                                                      self.count)
+        table = torch.empty(max(self.table_bytes, 1), dtype=torch.uint8)
+        L.petra_adamw_layout(self.desc, tensors, self.count, table, self.table_bytes)
+        self.table = table.to(device)
+        self._own(ws_bytes, device)
+
+    def step(self, rng=None, grad_scale=None, stream=None) -> None:
+        """Updates params, copies and states; rng (device int64 [seed, offset], for fp8): another
+        offset each step; grad_scale: a device fp32 factor of all gradients."""
+        if rng is not None:
+            _need_rng(rng)
+        if grad_scale is not None:
+            _need(grad_scale, "grad_scale", self.ftype, (1,))
+        _need(self.lr, "lr", self.ftype, (1,))
+        L.petra_adamw_step(self.desc, self.table, self.table_bytes, self.count, self.chunks,
+                           self.steps, self.lr, grad_scale, rng, self.workspace, self.ws_bytes,
+                           self._on(stream))
