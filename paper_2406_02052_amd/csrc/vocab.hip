@@ -26,7 +26,8 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr float LN2 = 0.69314718055994530942f;
-constexpr float MOST = 86.f;                  // log2 of the largest e; sums of 2^31 of them fit fp32
+// How large a tile's sum of a row may be (sums of all tiles fit fp32), and log2 of the least largest e that makes a reference of its own.
+constexpr float MOST = 0x1p86f, REACH = 70.f;
 constexpr float INF = __builtin_huge_valf();
 
 __device__ __forceinline__ f32x16_t mfma32(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x16_t c) {
@@ -87,50 +88,77 @@ struct Panel {
       off[i] = !ALONG && first + chunk(i) * PER >= free ? BUF_OOB : o;
     }
   }
-  // Asks for the next tile, of which `inner` inner indices exist, and goes on.  The loads are written out: the compiler would
-  // let every later transposing LDS read wait for them.  They write no register; arrived() waits for them.
-  __device__ __forceinline__ void load(char* lds, long inner) {
-    const uint64_t from = reinterpret_cast<uint64_t>(base);
+  // The next tile, of which `inner` inner indices exist: a resource that ends with the tensor, and the buffer it goes to.
+  struct Next {
+    u32x4_t from;
+    uint32_t to;
+    long inner;
+  };
+  __device__ __forceinline__ Next next(char* lds, long inner) {
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
     const int64_t bytes = left * static_cast<int64_t>(sizeof(T));
     const uint32_t most = inner <= 0 || bytes <= 0 ? 0u : bytes < 0x7fffffff ? static_cast<uint32_t>(bytes) : 0x7fffffffu;
-    const u32x4_t r = {static_cast<uint32_t>(from), static_cast<uint32_t>(from >> 32) & 0xffffu, most, 0x00020000u};
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t to = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds)) + wave * 1024;
-    const bool part = ALONG && inner < INNER;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const uint32_t o = part && chunk(i) * PER >= inner ? BUF_OOB : off[i];
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                   ::"s"(to + i * THREADS * 16), "v"(o), "s"(r) : "memory");
-    }
     base += step;
     left -= step;
+    return {{static_cast<uint32_t>(at), static_cast<uint32_t>(at >> 32) & 0xffffu, most, 0x00020000u},
+            static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds)) + wave * 1024, inner};
   }
-  // This lane's operand: free index free0 + (lane & 31), inner ones 16 k + 8 (lane >> 5) .. + 7.
-  static __device__ __forceinline__ Frag<T> get(char* lds, int free0, int k, int lane) {
-    Frag<T> f;
+  // Asks for this thread's chunk i of it (CUT: a last, partial tile).  The loads are written out: the compiler would let every
+  // later transposing LDS read wait for them.  They write no register, and a buffer that is not read before the next arrived(),
+  // which waits for them.
+  template <bool CUT>
+  __device__ __forceinline__ void load(const Next& n, int i) const {
+    const uint32_t o = CUT && ALONG && chunk(i) * PER >= n.inner ? BUF_OOB : off[i];
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(n.to + i * THREADS * 16), "v"(o), "s"(n.from));
+  }
+};
+
+// Where in a panel a lane finds its operands: free index free0 + 32 i + (lane & 31) for i < BLOCKS, inner ones 16 k + 8 (lane >> 5) .. + 7.
+// The keys leave few places that differ by lane; the rest are constants.
+template <typename T, typename P, bool ALONG, int BLOCKS>
+struct Reader {
+  static constexpr int LINE = P::CHUNKS * 16;
+  int at[ALONG ? 4 : BLOCKS];
+
+  __device__ __forceinline__ Reader(int free0, int lane) {
     const int h = lane >> 5;
     if constexpr (ALONG) {
-      const int l = free0 + (lane & 31);
-      if constexpr (sizeof(T) == 2) {
-        f.v = *reinterpret_cast<const bf16x8_t*>(lds + at(l, 2 * k + h));
-      } else {
-        const float4 a = *reinterpret_cast<const float4*>(lds + at(l, 4 * k + 2 * h));
-        const float4 b = *reinterpret_cast<const float4*>(lds + at(l, 4 * k + 2 * h + 1));
-        f.v[0] = a.x; f.v[1] = a.y; f.v[2] = a.z; f.v[3] = a.w;
-        f.v[4] = b.x; f.v[5] = b.y; f.v[6] = b.z; f.v[7] = b.w;
-      }
+      const int l = free0 + (lane & 31);   // (its key does not go by 32 i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) at[q] = P::at(l, sizeof(T) == 2 ? 2 * q + h : 4 * (q >> 1) + 2 * h + (q & 1));
     } else if constexpr (sizeof(T) == 2) {
-      const int l = 16 * k + 8 * h + ((lane & 15) >> 2), col = free0 + (lane & 16) + 4 * (lane & 3);
-      const int in = (col & 7) * 2;
-      const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lds + at(l, col >> 3) + in));
-      const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lds + at(l + 4, col >> 3) + in));
+      const int l = 8 * h + ((lane & 15) >> 2);   // (nor by 16 k or 4)
+#pragma unroll
+      for (int i = 0; i < BLOCKS; ++i) {
+        const int col = free0 + 32 * i + (lane & 16) + 4 * (lane & 3);
+        at[i] = P::at(l, col >> 3) + (col & 7) * 2;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < BLOCKS; ++i) {
+        const int col = free0 + 32 * i + (lane & 31);
+        at[i] = P::at(8 * h, col >> 2) + (col & 3) * 4;
+      }
+    }
+  }
+  __device__ __forceinline__ Frag<T> get(char* lds, int i, int k) const {
+    Frag<T> f;
+    if constexpr (ALONG && sizeof(T) == 2) {
+      f.v = *reinterpret_cast<const bf16x8_t*>(lds + at[k] + i * 32 * LINE);
+    } else if constexpr (ALONG) {
+      const float4 a = *reinterpret_cast<const float4*>(lds + at[2 * k] + i * 32 * LINE);
+      const float4 b = *reinterpret_cast<const float4*>(lds + at[2 * k + 1] + i * 32 * LINE);
+      f.v[0] = a.x; f.v[1] = a.y; f.v[2] = a.z; f.v[3] = a.w;
+      f.v[4] = b.x; f.v[5] = b.y; f.v[6] = b.z; f.v[7] = b.w;
+    } else if constexpr (sizeof(T) == 2) {
+      char* const p = lds + at[i] + k * 16 * LINE;
+      const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)p);
+      const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p + 4 * LINE));
       f.v = __builtin_bit_cast(bf16x8_t, s16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
     } else {
-      const int col = free0 + (lane & 31);
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        f.v[j] = *reinterpret_cast<const float*>(lds + at(16 * k + 8 * h + j, col >> 2) + 4 * (col & 3));
+      for (int j = 0; j < 8; ++j) f.v[j] = *reinterpret_cast<const float*>(lds + at[i] + (16 * k + j) * LINE);
     }
     return f;
   }
@@ -138,61 +166,115 @@ struct Panel {
 
 template <int N> struct Const { static constexpr int value = N; };
 
-// All but the newest LOADS of this wave's loads to LDS have arrived, this wave has read what it asked LDS for, and every wave
-// is here.
+// This wave's loads to LDS have arrived but for the newest LOADS, it has read what it asked LDS for, and every wave is here.
 template <int LOADS>
 __device__ __forceinline__ void arrived() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
 }
 
-// A tile of a product: BM x BN results of A's and B's free indices, by WM x WN waves, in BUFS buffers.  A wave has (BM / WM) x
+// A tile of a product: BM x BN results of A's and B's free indices, by WM x WN waves, in two buffers.  A wave has (BM / WM) x
 // (BN / WN) results as blocks of 32 x 32, a row (A's free index) a lane and in lane half h the columns 8 g + 4 h + {0..3}: what a
 // row needs, its sums or its factor, is then a lane's.
-template <typename T, int BM_, int BN_, int WM_, int WN_, int BUFS_, bool A_ALONG, bool B_ALONG>
+template <typename T, int BM_, int BN_, int WM_, int WN_, bool A_ALONG, bool B_ALONG>
 struct Product {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BUFS = BUFS_, THREADS = 64 * WM * WN;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, THREADS = 64 * WM * WN;
   static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;
   using A = Panel<T, BM, A_ALONG, THREADS>;
   using B = Panel<T, BN, B_ALONG, THREADS>;
-  static constexpr int BUF = A::BYTES + B::BYTES, LDS = BUFS * BUF, INNER = A::INNER, LOADS = A::N + B::N;
+  static constexpr bool CUT = A_ALONG && B_ALONG;   // (e is padded to whole tiles)
+  static constexpr int BUF = A::BYTES + B::BYTES, LDS = 2 * BUF, INNER = A::INNER, LOADS = A::N + B::N;
 
-  // acc += the inner indices k0 .. k1 (k0 a multiple of INNER); a.begin() and b.begin() have been called at k0.
+  // acc += the inner indices k0 .. k1 (k0 a multiple of INNER); a.begin() and b.begin() have been called at k0.  A tile is taken 16
+  // inner indices at a time, and the operands of the next 16 are read while the matrix unit has these: at the tile's last 16 all
+  // reads of its buffer are done, so that the next tile is waited for there, its first operands read, and the buffer given to
+  // the tile after it.  Reads and loads go one by one between the matrix instructions, in the order written.
   static __device__ __forceinline__ void run(A& a, B& b, long k0, long k1, char* lds, f32x16_t (&acc)[MB][NB]) {
+    constexpr int PARTS = INNER / 16, M = MB * NB, R = MB + NB;
+    static_assert(PARTS % 2 == 0, "operands in turn");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m0 = wave / WN * (BM / WM), n0 = wave % WN * (BN / WN);
-    const int steps = static_cast<int>((k1 - k0 + INNER - 1) / INNER);
-    auto fetch = [&](int s, char* to) {
-      const long inner = k1 - k0 - static_cast<long>(s) * INNER;
-      a.load(to, inner);
-      b.load(to + A::BYTES, inner);
+    // a last part of lines of the inner index goes after the whole tiles; of lines of free ones those past the end are zeros
+    const int steps = static_cast<int>((k1 - k0 + (CUT ? 0 : INNER - 1)) / INNER);
+    const Reader<T, A, A_ALONG, MB> ra(m0, lane);
+    const Reader<T, B, B_ALONG, NB> rb(n0, lane);
+    Frag<T> fa[2][MB], fb[2][NB];
+    auto read = [&](char* from, int k, int r, Frag<T> (&x)[MB], Frag<T> (&y)[NB]) {
+      if (r < NB) y[r < NB ? r : 0] = rb.get(from + A::BYTES, r, k);
+      else x[r < NB ? 0 : r - NB] = ra.get(from, r - NB, k);
     };
+    auto fetch = [&](int s, char* to) {   // (past the end: nothing)
+      const long inner = s < steps ? INNER : 0;
+      const typename A::Next na = a.next(to, inner);
+      const typename B::Next nb = b.next(to + A::BYTES, inner);
 #pragma unroll
-    for (int s = 0; s < BUFS - 1; ++s) fetch(s, lds + s * BUF);
+      for (int i = 0; i < A::N; ++i) a.template load<false>(na, i);
+#pragma unroll
+      for (int i = 0; i < B::N; ++i) b.template load<false>(nb, i);
+    };
+    fetch(0, lds);
+    fetch(1, lds + BUF);
+    arrived<LOADS>();
+#pragma unroll
+    for (int r = 0; r < R; ++r) read(lds, 0, r, fa[0], fb[0]);
     auto body = [&](int s, auto buf) {
       constexpr int I = decltype(buf)::value;
-      char* const at = lds + I * BUF;
-      arrived<(BUFS - 2) * LOADS>();
-      fetch(s + BUFS - 1, lds + (I + BUFS - 1) % BUFS * BUF);   // (past the end: nothing)
+      char *const at = lds + I * BUF, *const other = lds + (1 - I) * BUF;
 #pragma unroll
-      for (int k = 0; k < INNER / 16; ++k) {
-        Frag<T> fa[MB], fb[NB];
+      for (int k = 0; k < PARTS; ++k) {
+        const bool last = k + 1 == PARTS;
+        const int now = k & 1, then = 1 - now;
+        typename A::Next na{};
+        typename B::Next nb{};
+        if (last) {
+          const long inner = s + 2 < steps ? INNER : 0;
+          na = a.next(at, inner);
+          nb = b.next(at + A::BYTES, inner);
+          arrived<0>();
+        }
 #pragma unroll
-        for (int i = 0; i < MB; ++i) fa[i] = A::get(at, m0 + 32 * i, k, lane);
+        for (int m = 0; m < M; ++m) {
 #pragma unroll
-        for (int j = 0; j < NB; ++j) fb[j] = B::get(at + A::BYTES, n0 + 32 * j, k, lane);
+          for (int r = 0; r < R; ++r)
+            if (r * M / R == m) read(last ? other : at, last ? 0 : k + 1, r, fa[then], fb[then]);
+          if (last) {
 #pragma unroll
-        for (int i = 0; i < MB; ++i)
+            for (int i = 0; i < A::N; ++i)
+              if (i * M / LOADS == m) a.template load<false>(na, i);
 #pragma unroll
-          for (int j = 0; j < NB; ++j) acc[i][j] = mfma32(fb[j], fa[i], acc[i][j]);
+            for (int i = 0; i < B::N; ++i)
+              if ((A::N + i) * M / LOADS == m) b.template load<false>(nb, i);
+          }
+          acc[m / NB][m % NB] = mfma32(fb[now][m % NB], fa[now][m / NB], acc[m / NB][m % NB]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     };
-    for (int s = 0; s < steps; s += BUFS) {
+    for (int s = 0; s < steps; s += 2) {
       body(s, Const<0>{});
-      if constexpr (BUFS > 1) if (s + 1 < steps) body(s + 1, Const<1 % BUFS>{});
-      if constexpr (BUFS > 2) if (s + 2 < steps) body(s + 2, Const<2 % BUFS>{});
-      if constexpr (BUFS > 3) if (s + 3 < steps) body(s + 3, Const<3 % BUFS>{});
+      if (s + 1 < steps) body(s + 1, Const<1>{});
     }
     arrived<0>();   // LDS is free
+    if constexpr (CUT) {
+      const long inner = k1 - k0 - static_cast<long>(steps) * INNER;
+      if (inner > 0) {
+        a.base -= 2 * a.step, a.left += 2 * a.step, b.base -= 2 * b.step, b.left += 2 * b.step;   // (asked for nothing twice)
+        const typename A::Next na = a.next(lds, inner);
+        const typename B::Next nb = b.next(lds + A::BYTES, inner);
+#pragma unroll
+        for (int i = 0; i < A::N; ++i) a.template load<true>(na, i);
+#pragma unroll
+        for (int i = 0; i < B::N; ++i) b.template load<true>(nb, i);
+        arrived<0>();
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+#pragma unroll
+          for (int r = 0; r < R; ++r) read(lds, k, r, fa[0], fb[0]);
+#pragma unroll
+          for (int m = 0; m < M; ++m) acc[m / NB][m % NB] = mfma32(fb[0][m % NB], fa[0][m / NB], acc[m / NB][m % NB]);
+        }
+        arrived<0>();
+      }
+    }
   }
   static __device__ __forceinline__ void zero(f32x16_t (&acc)[MB][NB]) {
 #pragma unroll
@@ -273,14 +355,16 @@ __global__ __launch_bounds__(1024) void vocab_mean_kernel(VocabArgs a) {
   }
 }
 
-// e of a tile and each row's sum of it.  One of (KEEP) e kept, or the sums alone.
+// e of a tile (KEEP: kept; a bf16 tile goes through LDS, so that whole lines are written) and each row's sum of it.
 template <typename T, typename P, bool KEEP>
 __global__ __launch_bounds__(P::THREADS, 2) void vocab_scores_kernel(VocabArgs a) {
-  __shared__ __attribute__((aligned(16))) char lds[P::LDS];
+  constexpr int MB = P::MB, NB = P::NB, CHUNKS = P::BN / 8;   // chunks of 16 bytes of a line of e, moved by the line's number
+  __shared__ __attribute__((aligned(16))) char lds[P::LDS + P::WN * P::BM * 4];
+  float* const shared = reinterpret_cast<float*>(lds + P::LDS);   // [wave column][row of the tile]
   int mt, nt;
   tile_of(blockIdx.x, a.row_tiles, a.col_tiles, mt, nt);
   const long m0 = static_cast<long>(mt) * P::BM, n0 = static_cast<long>(nt) * P::BN;
-  f32x16_t acc[P::MB][P::NB];
+  f32x16_t acc[MB][NB];
   P::zero(acc);
   {
     typename P::A pa;
@@ -290,79 +374,86 @@ __global__ __launch_bounds__(P::THREADS, 2) void vocab_scores_kernel(VocabArgs a
     P::run(pa, pb, 0, a.width, lds, acc);
   }
   const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave / P::WN * (P::BM / P::WM) + (lane & 31), wn = wave % P::WN * (P::BN / P::WN) + 4 * h;
-  float* const shared = reinterpret_cast<float*>(lds);   // [wave column][row of the tile]
-  const bool edge = n0 + P::BN > a.vocab;
-  bool live[P::MB], over = false;
-  // binary logarithms of e; those past the vocabulary -inf
+  const int wm = wave / P::WN * (P::BM / P::WM) + (lane & 31), wn = wave % P::WN * (P::BN / P::WN);
+  if (n0 + P::BN > a.vocab) {
 #pragma unroll
-  for (int i = 0; i < P::MB; ++i) {
-    const long row = m0 + wm + 32 * i;
-    live[i] = row < a.piece && takes_part(a, a.row0 + row);
-    const float c = live[i] ? -a.ref[a.row0 + row] : 0.f;
-    float top = -INF;
+    for (int j = 0; j < NB; ++j)
 #pragma unroll
-    for (int j = 0; j < P::NB; ++j)
+      for (int e = 0; e < 16; ++e)
+        if (n0 + wn + 32 * j + 8 * (e >> 2) + 4 * h + (e & 3) >= a.vocab)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int n = wn + 32 * j + 8 * (e >> 2) + (e & 3);
-        float v = fmaf(acc[i][j][e], a.scale_log2, c);
-        if (edge && n0 + n >= a.vocab) v = -INF;
-        acc[i][j][e] = v;
-        top = fmaxf(top, v);
-      }
-    over |= top > MOST && live[i];
+          for (int i = 0; i < MB; ++i) acc[i][j][e] = -INF;
   }
-  // rows that need another reference are rare: their whole tile takes the slow way
-  float shift[P::MB] = {};
-  const bool slow = __syncthreads_or(over);
+  float c[MB];
+  uint32_t live[MB];   // all ones for a row that takes part
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    const long row = m0 + wm + 32 * i;
+    const bool in = row < a.piece && takes_part(a, a.row0 + row);
+    live[i] = in ? ~0u : 0u;
+    c[i] = in ? -a.ref[a.row0 + row] : 0.f;
+  }
+  // e and its sums; whether a row's passed MOST
+  auto exponentials = [&]() {
+    bool over = false;
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+      const long row = m0 + wm + 32 * i;
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[e] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][4 * g + e], a.scale_log2, c[i]));
+            sum += v[e];
+          }
+          const int n = wn + 32 * j + 8 * g;
+          if constexpr (KEEP && sizeof(T) == 2) {
+            *reinterpret_cast<uint2*>(lds + (wm + 32 * i) * (CHUNKS * 16) + (((n >> 3) ^ (lane & 31 & (CHUNKS - 1))) << 4) + 8 * h) =
+                make_uint2(pack_bf16x2(v[0], v[1]) & live[i], pack_bf16x2(v[2], v[3]) & live[i]);
+          } else if constexpr (KEEP) {
+            if (row < a.piece && n0 + n < a.vocab_padded)
+              *reinterpret_cast<float4*>(static_cast<T*>(a.e) + row * a.vocab_padded + n0 + n + 4 * h) =
+                  live[i] ? make_float4(v[0], v[1], v[2], v[3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+        }
+      sum = sum_halves(sum);
+      over |= live[i] && sum > MOST;
+      if (h == 0) shared[(wave % P::WN) * P::BM + wm + 32 * i] = sum;
+    }
+    return over;
+  };
+  // rows that need another reference are rare: their whole tile is done again, with their largest as the reference
+  const bool slow = __syncthreads_or(exponentials());
   if (slow) {
+    float top[MB];
 #pragma unroll
-    for (int i = 0; i < P::MB; ++i) {
-      float top = -INF;
+    for (int i = 0; i < MB; ++i) {
+      top[i] = -INF;
 #pragma unroll
-      for (int j = 0; j < P::NB; ++j)
+      for (int j = 0; j < NB; ++j)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[i][j][e]);
-      top = max_halves(top);
-      if (h == 0) shared[(wave % P::WN) * P::BM + wm + 32 * i] = top;
+        for (int e = 0; e < 16; ++e) top[i] = fmaxf(top[i], fmaf(acc[i][j][e], a.scale_log2, c[i]));
+      top[i] = max_halves(top[i]);
+      if (h == 0) shared[(wave % P::WN) * P::BM + wm + 32 * i] = top[i];
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < P::MB; ++i) {
-      float top = -INF;
+    for (int i = 0; i < MB; ++i) {
 #pragma unroll
-      for (int w = 0; w < P::WN; ++w) top = fmaxf(top, shared[w * P::BM + wm + 32 * i]);
-      shift[i] = top > MOST ? top : 0.f;
+      for (int w = 0; w < P::WN; ++w) top[i] = fmaxf(top[i], shared[w * P::BM + wm + 32 * i]);
+      const long row = m0 + wm + 32 * i;
+      const float shift = top[i] > REACH ? top[i] : 0.f;
+      c[i] -= shift;
+      if (h == 0 && wave % P::WN == 0 && row < a.piece) a.shift[row * a.col_tiles + nt] = shift;
     }
     __syncthreads();
+    exponentials();
+    __syncthreads();
   }
-#pragma unroll
-  for (int i = 0; i < P::MB; ++i) {
-    const long row = m0 + wm + 32 * i;
-    float sum = 0.f;
-#pragma unroll
-    for (int j = 0; j < P::NB; ++j)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = !live[i] ? 0.f : __builtin_amdgcn_exp2f(acc[i][j][4 * g + e] - shift[i]);
-          sum += v[e];
-        }
-        const long n = n0 + wn + 32 * j + 8 * g;
-        if (KEEP && row < a.piece && n < a.vocab_padded) {
-          T* const to = static_cast<T*>(a.e) + row * a.vocab_padded + n;
-          if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-          else *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
-        }
-      }
-    sum = sum_halves(sum);
-    if (h == 0) shared[(wave % P::WN) * P::BM + wm + 32 * i] = sum;
-    if (slow && h == 0 && wave % P::WN == 0 && row < a.piece) a.shift[row * a.col_tiles + nt] = shift[i];
-  }
-  __syncthreads();
   for (int r = threadIdx.x; r < P::BM; r += P::THREADS) {
     float s = 0.f;
 #pragma unroll
@@ -370,6 +461,14 @@ __global__ __launch_bounds__(P::THREADS, 2) void vocab_scores_kernel(VocabArgs a
     if (m0 + r < a.piece) a.sums[(m0 + r) * a.col_tiles + nt] = s;
   }
   if (threadIdx.x == 0) a.slow[static_cast<long>(mt) * a.col_tiles + nt] = slow;
+  if constexpr (KEEP && sizeof(T) == 2) {
+    const int chunk = threadIdx.x % CHUNKS;
+    const long col = n0 + chunk * 8;
+    for (int r = threadIdx.x / CHUNKS; r < P::BM; r += P::THREADS / CHUNKS)
+      if (m0 + r < a.piece && col < a.vocab_padded)
+        *reinterpret_cast<uint4*>(static_cast<T*>(a.e) + (m0 + r) * a.vocab_padded + col) =
+            *reinterpret_cast<const uint4*>(lds + r * (CHUNKS * 16) + ((chunk ^ (r & 31 & (CHUNKS - 1))) << 4));
+  }
 }
 
 // A row's Z, loss and lse from its tiles' sums; with gradients also its factor, f x, the target's e' and what had another
@@ -490,25 +589,35 @@ __global__ __launch_bounds__(P::THREADS, 2) void vocab_grad_kernel(VocabGrad g) 
     pb.begin(static_cast<const T*>(g.b), g.cols, n0, g.cols, k0, g.b_inner);
     P::run(pa, pb, k0, k1, lds, acc);
   }
+  // through LDS, half of each wave's rows at a time, so that whole lines are written: a lane's results are 4 columns here and there
+  constexpr int CHUNKS = P::BN / 4, HALF = P::BM / P::WM / 2, ROWS = P::BM / 2, MB = P::MB / 2;
+  static_assert(ROWS * P::BN * 4 <= P::LDS, "half a tile in fp32");
   const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int chunk = threadIdx.x % CHUNKS;
+  const long col = n0 + chunk * 4;
 #pragma unroll
-  for (int i = 0; i < P::MB; ++i) {
-    const long row = m0 + wave / P::WN * (P::BM / P::WM) + 32 * i + (lane & 31);
-    if (row >= g.rows) continue;
+  for (int p = 0; p < 2; ++p) {
+    if (p > 0) __syncthreads();
 #pragma unroll
-    for (int j = 0; j < P::NB; ++j)
+    for (int i = 0; i < MB; ++i)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const long col = n0 + wave % P::WN * (P::BN / P::WN) + 32 * j + 8 * q + 4 * h;
-        if (col >= g.cols) continue;
-        float v[4];
+      for (int j = 0; j < P::NB; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
-        if (g.splits > 1)
-          *reinterpret_cast<float4*>(g.part + (split * g.rows + row) * g.cols + col) = make_float4(v[0], v[1], v[2], v[3]);
-        else
-          finish<T>(g, row, col, v);
-      }
+        for (int q = 0; q < 4; ++q) {
+          const int r = wave / P::WN * HALF + 32 * i + (lane & 31), c = (wave % P::WN * (P::BN / P::WN) + 32 * j + 8 * q) / 4 + h;
+          const f32x16_t& v = acc[p * MB + i][j];
+          *reinterpret_cast<float4*>(lds + r * (CHUNKS * 16) + ((c ^ (lane & 31 & (CHUNKS - 1))) << 4)) =
+              make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        }
+    __syncthreads();
+    for (int r = threadIdx.x / CHUNKS; r < ROWS; r += P::THREADS / CHUNKS) {
+      const long row = m0 + r / HALF * (2 * HALF) + p * HALF + r % HALF;
+      if (row >= g.rows || col >= g.cols) continue;
+      const float4 x = *reinterpret_cast<const float4*>(lds + r * (CHUNKS * 16) + ((chunk ^ (r & 31 & (CHUNKS - 1))) << 4));
+      float v[4] = {x.x, x.y, x.z, x.w};
+      if (g.splits > 1) *reinterpret_cast<float4*>(g.part + (split * g.rows + row) * g.cols + col) = x;
+      else finish<T>(g, row, col, v);
+    }
   }
 }
 
@@ -532,7 +641,7 @@ __global__ __launch_bounds__(256) void vocab_add_kernel(VocabGrad g) {
 // ---------------------------------------------------------------------------
 
 constexpr int TILE = 256;
-template <typename T, bool A, bool B> using Large = Product<T, 256, 256, 2, 4, 2, A, B>;
+template <typename T, bool A, bool B> using Large = Product<T, 256, 256, 2, 4, A, B>;
 
 long up(long x, long y) { return (x + y - 1) / y; }
 
