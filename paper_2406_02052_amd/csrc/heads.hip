@@ -57,6 +57,19 @@ __device__ __forceinline__ float team_sum(float v) {
   return v;
 }
 
+// Sum over a wave's teams, of the lanes at one place in theirs: rows of 16 lanes turned by multiples of a team, then the rows.
+template <int LANES>
+__device__ __forceinline__ float over_teams(float v) {
+  auto turned = [](float x, auto dpp) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(dpp)::value, 0xF, 0xF, false));
+  };
+  if constexpr (LANES <= 8) v += turned(v, std::integral_constant<int, 0x128>{});
+  if constexpr (LANES <= 4) v += turned(v, std::integral_constant<int, 0x124>{});
+  if constexpr (LANES <= 2) v += turned(v, std::integral_constant<int, 0x122>{});
+  if constexpr (LANES <= 1) v += turned(v, std::integral_constant<int, 0x121>{});
+  return sum_halves(sum_quarters(v));
+}
+
 // C consecutive elements (4 or 8) as they lie in memory.
 template <typename T, int C> struct Chunk;
 template <> struct Chunk<bf16_t, 8> {
@@ -100,7 +113,7 @@ template <int C> struct Chunk<float, C> {
 // pair are in the two chunks, and a lane past the pairs has two chunks in a row; with neighbours all lanes have.
 template <int C, bool HALVES>
 struct Place {
-  int a, b, pair;            // pair: the first of the lane's C pairs (halves), or a / 2
+  int a, b;                  // (the lane's C pairs begin at C lane in either layout)
   bool in_a, in_b, turn_a, turn_b;
   __device__ __forceinline__ Place(int lane, int dim, int pairs) {
     if constexpr (HALVES) {
@@ -108,11 +121,9 @@ struct Place {
       turn_a = turn_b = lane < n;
       a = lane < n ? lane * C : 2 * pairs + (lane - n) * 2 * C;
       b = lane < n ? pairs + lane * C : a + C;
-      pair = lane * C;
     } else {
       a = lane * 2 * C;
       b = a + C;
-      pair = lane * C;
       turn_a = a < 2 * pairs;
       turn_b = b < 2 * pairs;
     }
@@ -127,13 +138,19 @@ struct Angles {
   uint64_t f[C];
   uint32_t axes;             // 4 bits a pair
   float c[C], s[C];
-  __device__ __forceinline__ void pairs(const HeadsArgs& a, int first) {
+  // Those of the lane's pairs.  The table is read by constant indexes, into scalar registers: a lane's own index would read the
+  // arguments' memory again (8 x 1 tokens: 4.5 us in place of 3).
+  template <int LANES>
+  __device__ __forceinline__ void pairs(const HeadsArgs& a, int lane) {
     axes = 0;
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-      const int p = first + j < a.pairs ? first + j : 0;
-      f[j] = first + j < a.pairs ? a.freq[p] : 0;
-      axes |= static_cast<uint32_t>(a.axis[p]) << (4 * j);
+    for (int j = 0; j < C; ++j) f[j] = 0;
+#pragma unroll
+    for (int t = 0; t < LANES && t * C < HEADS_PAIRS; ++t) {
+      if (t * C >= a.pairs) break;
+#pragma unroll
+      for (int j = 0; j < C; ++j) f[j] = lane == t ? a.freq[t * C + j] : f[j];   // (0 past the pairs)
+      axes = lane == t ? a.axes4[t * C / 8] >> (t * C % 8 * 4) : axes;
     }
   }
   __device__ __forceinline__ void at(const HeadsArgs& a, uint32_t token, uint32_t index) {
@@ -213,7 +230,7 @@ __global__ __launch_bounds__(THREADS) void heads_forward_kernel(HeadsArgs a) {
   const Lane l = my_lane<LANES>(p, blockIdx.x - (second ? a.part[0].blocks : 0));
   const Place<C, HALVES> at(l.lane, a.dim, a.pairs);
   Angles<C> angles;
-  angles.pairs(a, at.pair);
+  angles.template pairs<LANES>(a, l.lane);
   float gamma[2 * C];
 #pragma unroll
   for (int e = 0; e < 2 * C; ++e) gamma[e] = 1.f;
@@ -222,51 +239,71 @@ __global__ __launch_bounds__(THREADS) void heads_forward_kernel(HeadsArgs a) {
     if (at.in_a) t.load(p.gamma + at.a), t.get(gamma);
     if (at.in_b) t.load(p.gamma + at.b), t.get(gamma + C);
   }
-  for (long token = l.token; token < a.tokens; token += l.step) {
-    const uint32_t b = static_cast<uint32_t>(token) / a.len, i = static_cast<uint32_t>(token) - b * a.len;
-    angles.at(a, static_cast<uint32_t>(token), i);
-    const T* const x0 = static_cast<const T*>(p.x) + b * p.x_stride[0] + i * p.x_stride[1];
-    T* const y0 = static_cast<T*>(p.y) + b * p.y_stride[0] + i * p.y_stride[1];
-    for (int n = 0, h = l.head; n < p.rounds; ++n, h += 1 << p.head_bits) {
-      const bool in = h < p.heads;
-      Chunk<T, C> ca{}, cb{};
-      if (in && at.in_a) ca.load(x0 + h * p.x_stride[2] + at.a);
-      if (in && at.in_b) cb.load(x0 + h * p.x_stride[2] + at.b);
-      float x[2 * C];
-      ca.get(x);
-      cb.get(x + C);
-      if (p.gamma != nullptr) {
-        unit<C, LANES>(x, a.layer, at.in_a, at.in_b, a.inv_dim, a.eps);
-#pragma unroll
-        for (int e = 0; e < 2 * C; ++e) x[e] *= gamma[e];
-        if (p.beta != nullptr) {
-          float beta[2 * C] = {};
-          Chunk<float, C> t;
-          if (at.in_a) t.load(p.beta + at.a), t.get(beta);
-          if (at.in_b) t.load(p.beta + at.b), t.get(beta + C);
-#pragma unroll
-          for (int e = 0; e < 2 * C; ++e) x[e] += beta[e];
-        }
-      }
-      rotate<C, HALVES, false>(x, angles, at);
-      if (in && at.in_a) Chunk<T, C>::store(y0 + h * p.y_stride[2] + at.a, x);
-      if (in && at.in_b) Chunk<T, C>::store(y0 + h * p.y_stride[2] + at.b, x + C);
+  // the next head's channels are asked for before these are worked on
+  struct Item {
+    Chunk<T, C> a, b;
+    uint32_t row, index;     // batch row, token of it
+    long token;
+    int round;
+  } next{};
+  auto fetch = [&](long token, int round) {
+    if (round == 0 && token < a.tokens) {
+      next.row = static_cast<uint32_t>(token) / a.len;
+      next.index = static_cast<uint32_t>(token) - next.row * a.len;
     }
+    next.token = token;
+    next.round = round;
+    const int h = l.head + (round << p.head_bits);
+    const T* const x = static_cast<const T*>(p.x) + next.row * p.x_stride[0] + next.index * p.x_stride[1] + h * p.x_stride[2];
+    next.a = next.b = Chunk<T, C>{};
+    const bool in = token < a.tokens && h < p.heads;
+    if (in && at.in_a) next.a.load(x + at.a);
+    if (in && at.in_b) next.b.load(x + at.b);
+  };
+  fetch(l.token, 0);
+  while (next.token < a.tokens) {
+    const Item now = next;
+    if (now.round == 0) angles.at(a, static_cast<uint32_t>(now.token), now.index);
+    const bool more = now.round + 1 < p.rounds;
+    fetch(more ? now.token : now.token + l.step, more ? now.round + 1 : 0);
+    float x[2 * C];
+    now.a.get(x);
+    now.b.get(x + C);
+    if (p.gamma != nullptr) {
+      unit<C, LANES>(x, a.layer, at.in_a, at.in_b, a.inv_dim, a.eps);
+#pragma unroll
+      for (int e = 0; e < 2 * C; ++e) x[e] *= gamma[e];
+      if (p.beta != nullptr) {
+        float beta[2 * C] = {};
+        Chunk<float, C> t;
+        if (at.in_a) t.load(p.beta + at.a), t.get(beta);
+        if (at.in_b) t.load(p.beta + at.b), t.get(beta + C);
+#pragma unroll
+        for (int e = 0; e < 2 * C; ++e) x[e] += beta[e];
+      }
+    }
+    rotate<C, HALVES, false>(x, angles, at);
+    const int h = l.head + (now.round << p.head_bits);
+    if (h >= p.heads) continue;
+    T* const y = static_cast<T*>(p.y) + now.row * p.y_stride[0] + now.index * p.y_stride[1] + h * p.y_stride[2];
+    if (at.in_a) Chunk<T, C>::store(y + at.a, x);
+    if (at.in_b) Chunk<T, C>::store(y + at.b, x + C);
   }
 }
 
-// Sums of the parameters' gradients stay in registers over a workgroup's tokens; its teams' are then added in LDS
+// Sums of the parameters' gradients stay in registers over a workgroup's tokens; its teams' are then added
 // in a fixed order and written as a row of partial sums, which heads_join_kernel adds in a fixed order too.
-template <typename T, int C, int LANES, bool HALVES>
+// BETA: a norm has one.
+template <typename T, int C, int LANES, bool HALVES, bool BETA>
 __global__ __launch_bounds__(THREADS) void heads_backward_kernel(HeadsArgs a) {
-  __shared__ float joined[THREADS * 2 * C];
+  __shared__ float joined[THREADS / 64][128];
   const bool second = static_cast<int>(blockIdx.x) >= a.part[0].blocks;
   const HeadsPart& p = a.part[second];
   const int block = blockIdx.x - (second ? a.part[0].blocks : 0);
   const Lane l = my_lane<LANES>(p, block);
   const Place<C, HALVES> at(l.lane, a.dim, a.pairs);
   Angles<C> angles;
-  angles.pairs(a, at.pair);
+  angles.template pairs<LANES>(a, l.lane);
   const bool norm = p.gamma != nullptr;
   float gamma[2 * C], dgamma[2 * C] = {}, dbeta[2 * C] = {};
 #pragma unroll
@@ -276,67 +313,86 @@ __global__ __launch_bounds__(THREADS) void heads_backward_kernel(HeadsArgs a) {
     if (at.in_a) t.load(p.gamma + at.a), t.get(gamma);
     if (at.in_b) t.load(p.gamma + at.b), t.get(gamma + C);
   }
-  for (long token = l.token; token < a.tokens; token += l.step) {
-    const uint32_t b = static_cast<uint32_t>(token) / a.len, i = static_cast<uint32_t>(token) - b * a.len;
-    angles.at(a, static_cast<uint32_t>(token), i);
-    const long ox = b * p.x_stride[0] + i * p.x_stride[1], oy = b * p.y_stride[0] + i * p.y_stride[1];
-    for (int n = 0, h = l.head; n < p.rounds; ++n, h += 1 << p.head_bits) {
-      const bool in = h < p.heads;
-      const long px = ox + h * p.x_stride[2], py = oy + h * p.y_stride[2];
-      Chunk<T, C> ca{}, cb{}, xa{}, xb{};
-      if (in && at.in_a) {
-        ca.load(static_cast<const T*>(p.dy) + py + at.a);
-        if (norm) xa.load(static_cast<const T*>(p.x) + px + at.a);
-      }
-      if (in && at.in_b) {
-        cb.load(static_cast<const T*>(p.dy) + py + at.b);
-        if (norm) xb.load(static_cast<const T*>(p.x) + px + at.b);
-      }
-      float g[2 * C];
-      ca.get(g);
-      cb.get(g + C);
-      rotate<C, HALVES, true>(g, angles, at);
-      if (norm) {
-        float x[2 * C], s = 0.f, m = 0.f;
-        xa.get(x);
-        xb.get(x + C);
-        const float r = unit<C, LANES>(x, a.layer, at.in_a, at.in_b, a.inv_dim, a.eps);
-#pragma unroll
-        for (int e = 0; e < 2 * C; ++e) {
-          dgamma[e] = fmaf(g[e], x[e], dgamma[e]);
-          dbeta[e] += g[e];
-          g[e] *= gamma[e];
-          s = fmaf(g[e], x[e], s);
-          m += g[e];
-        }
-        s = team_sum<LANES>(s) * a.inv_dim;
-        m = a.layer ? team_sum<LANES>(m) * a.inv_dim : 0.f;
-#pragma unroll
-        for (int e = 0; e < 2 * C; ++e) g[e] = r * (g[e] - x[e] * s - m);
-      }
-      if (in && at.in_a) Chunk<T, C>::store(static_cast<T*>(p.dx) + px + at.a, g);
-      if (in && at.in_b) Chunk<T, C>::store(static_cast<T*>(p.dx) + px + at.b, g + C);
+  struct Item {
+    Chunk<T, C> ga, gb, xa, xb;
+    uint32_t row, index;     // batch row, token of it
+    long token;
+    int round;
+  } next{};
+  auto fetch = [&](long token, int round) {
+    if (round == 0 && token < a.tokens) {
+      next.row = static_cast<uint32_t>(token) / a.len;
+      next.index = static_cast<uint32_t>(token) - next.row * a.len;
     }
+    next.token = token;
+    next.round = round;
+    const int h = l.head + (round << p.head_bits);
+    const T* const dy = static_cast<const T*>(p.dy) + next.row * p.y_stride[0] + next.index * p.y_stride[1] + h * p.y_stride[2];
+    const T* const x = static_cast<const T*>(p.x) + next.row * p.x_stride[0] + next.index * p.x_stride[1] + h * p.x_stride[2];
+    next.ga = next.gb = next.xa = next.xb = Chunk<T, C>{};
+    const bool in = token < a.tokens && h < p.heads;
+    if (in && at.in_a) {
+      next.ga.load(dy + at.a);
+      if (norm) next.xa.load(x + at.a);
+    }
+    if (in && at.in_b) {
+      next.gb.load(dy + at.b);
+      if (norm) next.xb.load(x + at.b);
+    }
+  };
+  fetch(l.token, 0);
+  while (next.token < a.tokens) {
+    const Item now = next;
+    if (now.round == 0) angles.at(a, static_cast<uint32_t>(now.token), now.index);
+    const bool more = now.round + 1 < p.rounds;
+    fetch(more ? now.token : now.token + l.step, more ? now.round + 1 : 0);
+    float g[2 * C];
+    now.ga.get(g);
+    now.gb.get(g + C);
+    rotate<C, HALVES, true>(g, angles, at);
+    if (norm) {
+      float x[2 * C], s = 0.f, m = 0.f;
+      now.xa.get(x);
+      now.xb.get(x + C);
+      const float r = unit<C, LANES>(x, a.layer, at.in_a, at.in_b, a.inv_dim, a.eps);
+#pragma unroll
+      for (int e = 0; e < 2 * C; ++e) {
+        dgamma[e] = fmaf(g[e], x[e], dgamma[e]);
+        if (BETA) dbeta[e] += g[e];
+        g[e] *= gamma[e];
+        s = fmaf(g[e], x[e], s);
+        m += g[e];
+      }
+      s = team_sum<LANES>(s) * a.inv_dim;
+      m = a.layer ? team_sum<LANES>(m) * a.inv_dim : 0.f;
+#pragma unroll
+      for (int e = 0; e < 2 * C; ++e) g[e] = r * (g[e] - x[e] * s - m);
+    }
+    const int h = l.head + (now.round << p.head_bits);
+    if (h >= p.heads) continue;
+    T* const dx = static_cast<T*>(p.dx) + now.row * p.x_stride[0] + now.index * p.x_stride[1] + h * p.x_stride[2];
+    if (at.in_a) Chunk<T, C>::store(dx + at.a, g);
+    if (at.in_b) Chunk<T, C>::store(dx + at.b, g + C);
   }
   if (!norm) return;
   auto flush = [&](const float (&v)[2 * C], float* to) {
     __syncthreads();
-    // [team][channel]
-    float* const mine = joined + threadIdx.x / LANES * (LANES * 2 * C);
+    float* const mine = joined[threadIdx.x >> 6];
 #pragma unroll
-    for (int e = 0; e < C; ++e) {
-      if (at.in_a) mine[at.a + e] = v[e];
-      if (at.in_b) mine[at.b + e] = v[C + e];
+    for (int e = 0; e < 2 * C; ++e) {
+      const float t = over_teams<LANES>(v[e]);
+      if ((threadIdx.x & 63) < LANES && (e < C ? at.in_a : at.in_b)) mine[e < C ? at.a + e : at.b + e - C] = t;
     }
     __syncthreads();
     if (static_cast<int>(threadIdx.x) < a.dim) {
       float s = 0.f;
-      for (int t = 0; t < THREADS / LANES; ++t) s += joined[t * (LANES * 2 * C) + threadIdx.x];
+#pragma unroll
+      for (int w = 0; w < THREADS / 64; ++w) s += joined[w][threadIdx.x];
       to[static_cast<long>(block) * a.dim + threadIdx.x] = s;
     }
   };
   flush(dgamma, p.part_gamma);
-  if (p.beta != nullptr) flush(dbeta, p.part_beta);
+  if (BETA && p.beta != nullptr) flush(dbeta, p.part_beta);
 }
 
 // Output blockIdx.x (dgamma and dbeta of the queries, then of the keys), channels 16 blockIdx.y ..: the sum over rows of
@@ -378,13 +434,14 @@ template <typename T, int C, int LANES>
 void launch(const HeadsArgs& a, bool backward, hipStream_t s) {
   const unsigned n = static_cast<unsigned>(a.part[0].blocks + a.part[1].blocks);
   if (n == 0) return;
-  if (a.halves) {
-    if (backward) heads_backward_kernel<T, C, LANES, true><<<n, THREADS, 0, s>>>(a);
-    else heads_forward_kernel<T, C, LANES, true><<<n, THREADS, 0, s>>>(a);
-  } else if constexpr (C == 8) {
-    if (backward) heads_backward_kernel<T, C, LANES, false><<<n, THREADS, 0, s>>>(a);
-    else heads_forward_kernel<T, C, LANES, false><<<n, THREADS, 0, s>>>(a);
-  }
+  auto by_layout = [&](auto halves) {
+    constexpr bool HALVES = decltype(halves)::value;
+    if (!backward) heads_forward_kernel<T, C, LANES, HALVES><<<n, THREADS, 0, s>>>(a);
+    else if (a.part[0].beta != nullptr || a.part[1].beta != nullptr) heads_backward_kernel<T, C, LANES, HALVES, true><<<n, THREADS, 0, s>>>(a);
+    else heads_backward_kernel<T, C, LANES, HALVES, false><<<n, THREADS, 0, s>>>(a);
+  };
+  if (a.halves) by_layout(std::true_type{});
+  else if constexpr (C == 8) by_layout(std::false_type{});
 }
 
 template <typename T>

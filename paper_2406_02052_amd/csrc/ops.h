@@ -91,8 +91,8 @@ struct HeadsArgs {
   uint32_t len;
   int dim, pairs, axes, halves, layer;
   float eps, inv_dim;
-  uint64_t freq[HEADS_PAIRS];                // 2^64 of a turn a position
-  uint8_t axis[HEADS_PAIRS];
+  uint64_t freq[HEADS_PAIRS];                // 2^64 of a turn a position; 0 past the pairs
+  uint32_t axes4[HEADS_PAIRS / 8];           // axes of the pairs, 4 bits each
 };
 
 // The workgroups of both parts (without tokens none).
@@ -109,7 +109,7 @@ struct VocabGrad {
   const float* factor;                       // [rows], nullable
   float *part, *acc;                         // the splits' sums; sums over the pieces of rows
   long rows, cols, inner, a_ld, a_free, b_inner, per_split;   // a_free: rows, or as many as a's lines have
-  int splits, row_tiles, col_tiles, add, last;
+  int splits, tile, row_tiles, col_tiles, add, last;
 };
 struct VocabArgs {
   const void *x, *w;
@@ -129,7 +129,8 @@ struct VocabArgs {
 };
 struct VocabPlan {
   long piece;
-  VocabGrad dx, dw;                          // splits and per_split
+  int row_tile, col_tile;                    // of the scores
+  VocabGrad dx, dw;                          // tile, splits and per_split
   size_t ref, sums, shift, slow, mean, factor, scaled, e, part, acc, bytes;   // offsets in the workspace
 };
 

@@ -645,7 +645,7 @@ struct Heads {
     for (int i = 0; i < d->pairs; ++i) {
       need(d->axis[i] >= 0 && d->axis[i] < d->axes, PETRA_ERR_INVALID_ARG, "a pair's axis is none of the axes");
       need(std::isfinite(d->freq[i]), PETRA_ERR_INVALID_ARG, "frequencies must be finite");
-      a.axis[i] = static_cast<uint8_t>(d->axis[i]);
+      a.axes4[i / 8] |= static_cast<uint32_t>(d->axis[i]) << (i % 8 * 4);
       // the fraction of a turn in 64 bits; a whole one wraps
       long double f = static_cast<long double>(d->freq[i]) / 6.283185307179586476925286766559005768L;
       f = roundl((f - floorl(f)) * 18446744073709551616.0L);

@@ -589,14 +589,16 @@ __global__ __launch_bounds__(P::THREADS, 2) void vocab_grad_kernel(VocabGrad g) 
     pb.begin(static_cast<const T*>(g.b), g.cols, n0, g.cols, k0, g.b_inner);
     P::run(pa, pb, k0, k1, lds, acc);
   }
-  // through LDS, half of each wave's rows at a time, so that whole lines are written: a lane's results are 4 columns here and there
-  constexpr int CHUNKS = P::BN / 4, HALF = P::BM / P::WM / 2, ROWS = P::BM / 2, MB = P::MB / 2;
-  static_assert(ROWS * P::BN * 4 <= P::LDS, "half a tile in fp32");
+  // through LDS, as many of each wave's rows at a time as fit, so that whole lines are written: a lane's results are 4 columns here
+  // and there
+  constexpr int PASSES = P::BM * P::BN * 4 <= P::LDS ? 1 : 2;
+  constexpr int CHUNKS = P::BN / 4, PART = P::BM / P::WM / PASSES, ROWS = P::BM / PASSES, MB = P::MB / PASSES;
+  static_assert(ROWS * P::BN * 4 <= P::LDS && MB > 0, "a pass's rows in fp32");
   const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int chunk = threadIdx.x % CHUNKS;
   const long col = n0 + chunk * 4;
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {
+  for (int p = 0; p < PASSES; ++p) {
     if (p > 0) __syncthreads();
 #pragma unroll
     for (int i = 0; i < MB; ++i)
@@ -604,14 +606,14 @@ __global__ __launch_bounds__(P::THREADS, 2) void vocab_grad_kernel(VocabGrad g) 
       for (int j = 0; j < P::NB; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int r = wave / P::WN * HALF + 32 * i + (lane & 31), c = (wave % P::WN * (P::BN / P::WN) + 32 * j + 8 * q) / 4 + h;
+          const int r = wave / P::WN * PART + 32 * i + (lane & 31), c = (wave % P::WN * (P::BN / P::WN) + 32 * j + 8 * q) / 4 + h;
           const f32x16_t& v = acc[p * MB + i][j];
           *reinterpret_cast<float4*>(lds + r * (CHUNKS * 16) + ((c ^ (lane & 31 & (CHUNKS - 1))) << 4)) =
               make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
         }
     __syncthreads();
     for (int r = threadIdx.x / CHUNKS; r < ROWS; r += P::THREADS / CHUNKS) {
-      const long row = m0 + r / HALF * (2 * HALF) + p * HALF + r % HALF;
+      const long row = m0 + r / PART * (PASSES * PART) + p * PART + r % PART;
       if (row >= g.rows || col >= g.cols) continue;
       const float4 x = *reinterpret_cast<const float4*>(lds + r * (CHUNKS * 16) + ((chunk ^ (r & 31 & (CHUNKS - 1))) << 4));
       float v[4] = {x.x, x.y, x.z, x.w};
@@ -640,17 +642,41 @@ __global__ __launch_bounds__(256) void vocab_add_kernel(VocabGrad g) {
 // launches
 // ---------------------------------------------------------------------------
 
-constexpr int TILE = 256;
+// Tiles of a product.  Large ones feed the matrix unit best, a workgroup a CU; smaller ones, two and four a CU, leave less of the
+// chip and of their own edges idle where there are few; and few rows are bound by reading w, which needs many workgroups.
 template <typename T, bool A, bool B> using Large = Product<T, 256, 256, 2, 4, A, B>;
+template <typename T, bool A, bool B> using Small = Product<T, 128, 128, 2, 2, A, B>;
+template <typename T, bool A, bool B> using Tiny = Product<T, 64, 64, 2, 2, A, B>;
+template <typename T> using Few = Product<T, 32, 64, 1, 2, true, true>;
 
 long up(long x, long y) { return (x + y - 1) / y; }
 
+// How long rows x cols results over `steps` tiles of the inner index take by one kind of tile, in microseconds: the tiles of
+// the fullest CU, as many at a time as it holds, each 3 steps longer than its inner index.  A step of a tile measured, with a CU
+// full of them: 256 x 256 1.6 (bf16) and 6.9 (fp32), 128 x 128 0.5 and 1.7, 64 x 64 0.25 and 0.43; none is shorter than loads take
+// to arrive.  Split sums are written and read again, at 4 TB/s.
+double cost(int tile, int dtype, long rows, long cols, long steps, long splits) {
+  const double step = dtype == 1 ? (tile == 256 ? 1.6 : tile == 128 ? 0.5 : 0.25) : (tile == 256 ? 6.9 : tile == 128 ? 1.7 : 0.43);
+  const long held = tile == 256 ? 1 : tile == 128 ? 2 : 4;
+  const long a_cu = up(up(rows, tile) * up(cols, tile) * splits, 256), rest = a_cu % held;
+  const double latency = 0.9, full = held * step > latency ? held * step : latency;
+  const double last = rest == 0 ? 0. : rest * step > latency ? rest * step : latency;
+  const double sums = splits > 1 ? 4. + static_cast<double>(rows) * cols * 8 * splits / 4e6 : 0.;
+  return (a_cu / held * full + last) * (up(steps, splits) + 3) + sums;
+}
+
 template <typename T>
 void scores(const VocabArgs& a, bool keep, hipStream_t s) {
-  using P = Large<T, true, true>;
   const unsigned n = static_cast<unsigned>(a.row_tiles * a.col_tiles);
-  if (keep) vocab_scores_kernel<T, P, true><<<n, P::THREADS, 0, s>>>(a);
-  else vocab_scores_kernel<T, P, false><<<n, P::THREADS, 0, s>>>(a);
+  auto launch = [&](auto p) {
+    using P = decltype(p);
+    if (keep) vocab_scores_kernel<T, P, true><<<n, P::THREADS, 0, s>>>(a);
+    else vocab_scores_kernel<T, P, false><<<n, P::THREADS, 0, s>>>(a);
+  };
+  if (a.row_tile == 32) launch(Few<T>{});
+  else if (a.row_tile == 64) launch(Tiny<T, true, true>{});
+  else if (a.row_tile == 128) launch(Small<T, true, true>{});
+  else launch(Large<T, true, true>{});
 }
 
 template <typename T>
@@ -659,21 +685,31 @@ void add(const VocabGrad& g, hipStream_t s) {
   vocab_add_kernel<T><<<static_cast<unsigned>(n < 4096 ? n : 4096), 256, 0, s>>>(g);
 }
 
-template <typename T, typename P>
+template <typename T, bool A, bool B>
 void grad(VocabGrad& g, hipStream_t s) {
-  g.row_tiles = static_cast<int>(up(g.rows, P::BM));
-  g.col_tiles = static_cast<int>(up(g.cols, P::BN));
-  vocab_grad_kernel<T, P><<<static_cast<unsigned>(g.row_tiles * g.col_tiles * g.splits), P::THREADS, 0, s>>>(g);
+  auto launch = [&](auto p) {
+    using P = decltype(p);
+    g.row_tiles = static_cast<int>(up(g.rows, P::BM));
+    g.col_tiles = static_cast<int>(up(g.cols, P::BN));
+    vocab_grad_kernel<T, P><<<static_cast<unsigned>(g.row_tiles * g.col_tiles * g.splits), P::THREADS, 0, s>>>(g);
+  };
+  if (g.tile == 64) launch(Tiny<T, A, B>{});
+  else if (g.tile == 128) launch(Small<T, A, B>{});
+  else launch(Large<T, A, B>{});
   if (g.splits > 1) add<T>(g, s);
 }
 
-// Splits of a product's inner index: as many as fill the 256 CUs, each of 8 tiles of it at least.
-void split(VocabGrad& g, long inner_tile) {
-  const long tiles = up(g.rows, TILE) * up(g.cols, TILE), steps = up(g.inner, inner_tile);
-  long n = tiles >= 192 ? 1 : 256 / tiles;
-  if (n > steps / 8) n = steps / 8;
-  if (n < 1) n = 1;
-  g.per_split = up(steps, n) * inner_tile;
+// Tiles and splits of a gradient's product: the cheapest.
+void split(VocabGrad& g, int dtype, long inner_tile) {
+  const long steps = up(g.inner, inner_tile);
+  double best = 0.;
+  long splits = 1;
+  for (int tile : {256, 128, 64})
+    for (long n = 1; n <= 64 && (n == 1 || n <= steps / 4); n = n < 4 ? n + 1 : n + n / 4) {
+      const double c = cost(tile, dtype, g.rows, g.cols, steps, n);
+      if (best == 0. || c < best) best = c, splits = n, g.tile = tile;
+    }
+  g.per_split = up(steps, splits) * inner_tile;
   g.splits = static_cast<int>(up(g.inner, g.per_split));
 }
 
@@ -688,11 +724,12 @@ void run(const VocabArgs& all, const VocabPlan& p, bool gradients, hipStream_t s
   }
   vocab_target_kernel<T><<<static_cast<unsigned>(up(a.rows, 4)), 256, 0, s>>>(a);
   if (gradients && a.weight == nullptr) vocab_mean_kernel<<<1, 1024, 0, s>>>(a);
-  a.col_tiles = static_cast<int>(up(a.vocab, TILE));
-  a.row_tile = a.col_tile = TILE;
+  a.row_tile = p.row_tile;
+  a.col_tile = p.col_tile;
+  a.col_tiles = static_cast<int>(up(a.vocab, a.col_tile));
   for (a.row0 = 0; a.row0 < a.rows; a.row0 += p.piece) {
     a.piece = a.rows - a.row0 < p.piece ? a.rows - a.row0 : p.piece;
-    a.row_tiles = static_cast<int>(up(a.piece, TILE));
+    a.row_tiles = static_cast<int>(up(a.piece, a.row_tile));
     scores<T>(a, gradients, s);
     const unsigned n = static_cast<unsigned>(a.piece);
     if (!gradients) {
@@ -703,12 +740,12 @@ void run(const VocabArgs& all, const VocabPlan& p, bool gradients, hipStream_t s
     VocabGrad x = p.dx, w = p.dw;
     x.a = a.e, x.b = a.w, x.a_ld = a.vocab_padded, x.a_free = a.piece, x.b_inner = a.vocab, x.rows = a.piece, x.cols = a.width, x.inner = a.vocab_padded;
     x.out = static_cast<T*>(a.dx) + a.row0 * a.width, x.factor = a.factor, x.part = a.part, x.last = 1;
-    grad<T, Large<T, true, false>>(x, s);
+    grad<T, true, false>(x, s);
     w.a = a.e, w.b = a.scaled, w.a_ld = w.a_free = a.vocab_padded, w.b_inner = a.piece, w.rows = a.vocab, w.cols = a.width, w.inner = a.piece;
     w.out = a.dw, w.part = a.part, w.acc = a.acc, w.add = a.row0 > 0, w.last = a.row0 + a.piece == a.rows;
     if (w.per_split >= w.inner) w.splits = 1;   // a last, smaller piece
     else w.splits = static_cast<int>(up(w.inner, w.per_split));
-    grad<T, Large<T, false, false>>(w, s);
+    grad<T, false, false>(w, s);
   }
 }
 
@@ -718,18 +755,22 @@ VocabPlan vocab_plan(const VocabArgs& a, int dtype, bool gradients, long piece_r
   const size_t esz = dtype == 1 ? 2 : 4;
   const long inner_tile = 128 / static_cast<long>(esz);
   VocabPlan p{};
-  // 2^30 bytes of e at a time, in whole tiles; of the sums 2^31
-  long most = gradients ? (1L << 30) / (a.vocab_padded * static_cast<long>(esz)) : (1L << 31) / (8 * up(a.vocab, TILE));
-  most = most / TILE * TILE;
-  if (most < TILE) most = TILE;
+  // 2^30 bytes of e at a time, in whole tiles; without it 2^30 of sums
+  long most = gradients ? (1L << 30) / (a.vocab_padded * static_cast<long>(esz)) : (1L << 30) / (8 * up(a.vocab, 64));
+  most = most < 256 ? 256 : most / 256 * 256;
   if (piece_rows > 0 && piece_rows < most) most = piece_rows;
   const long rows = a.rows > 0 ? a.rows : 1;
   p.piece = rows < most ? rows : most;
   if (piece_rows <= 0) {   // pieces of one size
-    const long even = up(up(rows, up(rows, p.piece)), TILE) * TILE;
+    const long even = up(up(rows, up(rows, p.piece)), 256) * 256;
     if (even < p.piece) p.piece = even;
   }
-  const long tiles = up(a.vocab, TILE);
+  const long steps = up(a.width, inner_tile);
+  p.row_tile = p.col_tile = 256;
+  for (int tile : {128, 64})
+    if (cost(tile, dtype, p.piece, a.vocab, steps, 1) < cost(p.row_tile, dtype, p.piece, a.vocab, steps, 1)) p.row_tile = p.col_tile = tile;
+  if (p.piece <= 32) p.row_tile = 32, p.col_tile = 64;
+  const long tiles = up(a.vocab, p.col_tile);
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -739,7 +780,7 @@ VocabPlan vocab_plan(const VocabArgs& a, int dtype, bool gradients, long piece_r
   p.ref = take(static_cast<size_t>(a.rows) * 4);
   p.sums = take(static_cast<size_t>(p.piece) * tiles * 4);
   p.shift = take(static_cast<size_t>(p.piece) * tiles * 4);
-  p.slow = take(static_cast<size_t>(up(p.piece, TILE)) * tiles * 4);
+  p.slow = take(static_cast<size_t>(up(p.piece, p.row_tile)) * tiles * 4);
   if (gradients) {
     p.mean = take(4);
     p.factor = take(static_cast<size_t>(p.piece) * 4);
@@ -749,7 +790,7 @@ VocabPlan vocab_plan(const VocabArgs& a, int dtype, bool gradients, long piece_r
     p.dw.rows = a.vocab, p.dw.cols = a.width, p.dw.inner = p.piece;
     size_t part = 0;
     for (VocabGrad* g : {&p.dx, &p.dw}) {
-      split(*g, inner_tile);
+      split(*g, dtype, inner_tile);
       const size_t bytes = g->splits > 1 ? static_cast<size_t>(g->splits) * g->rows * g->cols * 4 : 0;
       if (bytes > part) part = bytes;
     }

@@ -56,9 +56,14 @@ class _Owner:
         handle = L._stream(stream)
         if handle not in self.streams and not isinstance(stream, int):
             import torch
-            self.workspace.record_stream(torch.cuda.current_stream() if stream is None else stream)
+            for t in self._owned():
+                t.record_stream(torch.cuda.current_stream() if stream is None else stream)
             self.streams.add(handle)
         return handle
+
+    def _owned(self):
+        """The owner's memory that its calls use."""
+        return (self.workspace,)
 
 
 class Attention(_Owner):
@@ -197,6 +202,9 @@ def dropout(x, y, p: float, rng, residual=None, alpha: float = 1.0, stream=None)
                     alpha, x, residual, rng, y, stream)
 
 
+_NONE = (None, None)
+
+
 class HeadNorm(_Owner):
     """Norms of query and key heads with the rotation by their tokens' positions, over
     [batch, length, heads, head_dim] and [batch, length, kv_heads, head_dim] tensors (any strides
@@ -237,31 +245,42 @@ class HeadNorm(_Owner):
         self.form = None
         self._own(L.petra_heads_query(self.desc), device)
 
-    def _lay(self, x, y, norms, positions) -> None:
-        """x: (name, tensor) of q and k or their gradients, y likewise of the results; None for
-        the keys where there are none.  Puts their strides into the description; what was checked
-        last (types, shapes and strides) is not checked again."""
-        form = tuple((n, t.shape, t.stride(), t.dtype, t.is_cuda) if t is not None else None
-                     for n, t in x + y)
-        if form != self.form:
-            self.form = None
-            for fields, pair in ((("q_stride", "k_stride"), x), (("yq_stride", "yk_stride"), y)):
-                for (name, t), field, shape in zip(pair, fields, self.shapes):
-                    if shape[2] == 0 and t is None:
-                        continue
-                    _need(t, name, self.tdtype, shape, dense=False)
-                    setattr(self.desc, field, self._strides(t, name))
-            self.form = form
-        for name, p in norms:
-            if p is None:
-                continue
-            if self.norm is None:
-                raise ValueError(f"{name}: this owner has no norm")
-            _need(p[0], name, self.ftype, self.param_shape)
-            if p[1] is not None:
-                _need(p[1], name, self.ftype, self.param_shape)
+    @staticmethod
+    def _form(tensors):
+        return [(t.shape, t.stride(), t.dtype, t.is_cuda) if t is not None else None
+                for t in tensors]
+
+    def _lay(self, back, acts, params, positions) -> None:
+        """Checks the tensors and puts their strides into the description.  acts: q and k (back:
+        their gradients too, at the end) and what is laid out like the results; params: the
+        norms' and (back) their gradients'.  What was checked last (types, shapes and strides) is
+        not checked again."""
+        form = self._form(acts + params + (positions,))
+        if self.form == (back, form):
+            return
+        self.form = None
+        names = ("dq", "dk", "dyq", "dyk", "q", "k") if back else ("q", "k", "yq", "yk")
+        fields = ("q_stride", "k_stride", "yq_stride", "yk_stride")
+        for i, (t, name) in enumerate(zip(acts, names)):
+            if t is None and (self.shapes[i % 2][2] == 0 or i >= 4):
+                continue   # (the library needs q and k where there is a norm)
+            if t is None:
+                raise ValueError(f"{name}: need a tensor")
+            _need(t, name, self.tdtype, self.shapes[i % 2], dense=False)
+            if i < 4:
+                setattr(self.desc, fields[i], self._strides(t, name))
+            elif any(x != y for x, y, n in zip(t.stride(), acts[i - 4].stride(), t.shape) if n > 1):
+                raise ValueError(f"{name}: need the strides of its gradient "
+                                 f"{acts[i - 4].stride()}, got {t.stride()}")
+        for t, name in zip(params, ("q_norm", "q_norm", "k_norm", "k_norm", "dq_norm", "dq_norm",
+                                    "dk_norm", "dk_norm")):
+            if t is not None:
+                if self.norm is None:
+                    raise ValueError(f"{name}: this owner has no norm")
+                _need(t, name, self.ftype, self.param_shape)
         if positions is not None:
             _need(positions, "positions", self.itype, self.positions_shape)
+        self.form = (back, form)
 
     @staticmethod
     def _strides(t, name: str):
@@ -278,8 +297,7 @@ class HeadNorm(_Owner):
         """Writes yq and yk.  q_norm and k_norm: (gamma, beta or None), fp32; positions: int32
         [axes, batch, length] (None: a token's index)."""
         self._need_norms(q_norm, k_norm)
-        self._lay((("q", q), ("k", k)), (("yq", yq), ("yk", yk)),
-                  (("q_norm", q_norm), ("k_norm", k_norm)), positions)
+        self._lay(False, (q, k, yq, yk), (q_norm or _NONE) + (k_norm or _NONE), positions)
         L.petra_heads_forward(self.desc, q, k, q_norm, k_norm, positions, yq, yk, stream)
 
     def backward(self, q, k, dyq, dyk, dq, dk, q_norm=None, k_norm=None, dq_norm=None,
@@ -287,16 +305,8 @@ class HeadNorm(_Owner):
         """Writes dq, dk (strides of q and k) and the norms' parameters' gradients.  Without a
         norm q and k may be None."""
         self._need_norms(q_norm, k_norm)
-        self._lay((("dq", dq), ("dk", dk)), (("dyq", dyq), ("dyk", dyk)),
-                  (("q_norm", q_norm), ("k_norm", k_norm), ("dq_norm", dq_norm),
-                   ("dk_norm", dk_norm)), positions)
-        for t, name, like in ((q, "q", dq), (k, "k", dk)):
-            if t is None:
-                continue
-            _need(t, name, self.tdtype, like.shape, dense=False)
-            st, want = t.stride(), like.stride()
-            if st != want and any(x != y for x, y, n in zip(st, want, t.shape) if n > 1):
-                raise ValueError(f"{name}: need the strides of its gradient {want}, got {st}")
+        self._lay(True, (dq, dk, dyq, dyk, q, k), (q_norm or _NONE) + (k_norm or _NONE)
+                  + (dq_norm or _NONE) + (dk_norm or _NONE), positions)
         L.petra_heads_backward(self.desc, q, k, q_norm, k_norm, positions, dyq, dyk, dq, dk,
                                dq_norm, dk_norm, self.workspace, self.ws_bytes, self._on(stream))
 
@@ -420,6 +430,10 @@ class AdamW(_Owner):
         L.petra_adamw_layout(self.desc, tensors, self.count, table, self.table_bytes)
         self.table = table.to(device)
         self._own(ws_bytes, device)
+
+    def _owned(self):
+        return [t for t in (self.workspace, self.table, self.m, self.v, self.m_scale,
+                            self.v_scale, self.lr, self.steps) if t is not None]
 
     def step(self, rng=None, grad_scale=None, stream=None) -> None:
         """Updates params, copies and states; rng (device int64 [seed, offset], for fp8): another
