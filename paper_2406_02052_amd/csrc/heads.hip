@@ -132,38 +132,54 @@ struct Place {
   }
 };
 
-// The lane's C angles a token.
+// The angles of a wave's tokens.  Each is formed by one lane, an entry (token, pair) each, and read by all heads' teams from LDS:
+// forming them in every team takes as long as memory does (16384 tokens x 20 heads of 128 bf16: 46 us in all).
 template <int C>
 struct Angles {
-  uint64_t f[C];
-  uint32_t axes;             // 4 bits a pair
+  int count, split;          // entries of the wave; 2^16 / pairs, rounded up
+  int first;                 // position of the lane's first entry of the next tokens
   float c[C], s[C];
-  // Those of the lane's pairs.  The table is read by constant indexes, into scalar registers: a lane's own index would read the
-  // arguments' memory again (8 x 1 tokens: 4.5 us in place of 3).
-  template <int LANES>
-  __device__ __forceinline__ void pairs(const HeadsArgs& a, int lane) {
-    axes = 0;
-#pragma unroll
-    for (int j = 0; j < C; ++j) f[j] = 0;
-#pragma unroll
-    for (int t = 0; t < LANES && t * C < HEADS_PAIRS; ++t) {
-      if (t * C >= a.pairs) break;
-#pragma unroll
-      for (int j = 0; j < C; ++j) f[j] = lane == t ? a.freq[t * C + j] : f[j];   // (0 past the pairs)
-      axes = lane == t ? a.axes4[t * C / 8] >> (t * C % 8 * 4) : axes;
-    }
+
+  __device__ __forceinline__ void begin(const HeadsArgs& a, int tokens) {
+    count = tokens * a.pairs;
+    split = a.pairs > 0 ? (65535 + a.pairs) / a.pairs : 0;
+    first = 0;
   }
-  __device__ __forceinline__ void at(const HeadsArgs& a, uint32_t token, uint32_t index) {
-    int p[HEADS_AXES];
-#pragma unroll
-    for (int x = 0; x < HEADS_AXES; ++x)
-      p[x] = a.positions == nullptr ? static_cast<int>(index) : x < a.axes ? a.positions[x * a.tokens + token] : 0;
+  // Entry e's token of the wave (e < 512: exact) and pair.
+  __device__ __forceinline__ int token(int e) const { return (e * split) >> 16; }
+  __device__ __forceinline__ int position(const HeadsArgs& a, long base, int e) const {
+    const int t = token(e), pair = e - t * a.pairs;
+    const long at = base + t;
+    if (e >= count || at >= a.tokens) return 0;
+    const int axis = a.axes == 1 ? 0 : (a.axes4[pair >> 3] >> (pair % 8 * 4)) & 15;
+    return a.positions != nullptr ? a.positions[axis * a.tokens + at] : static_cast<int>(static_cast<uint32_t>(at) % a.len);
+  }
+  // Asks for the first position of the tokens from `base` on: where heads fill a wave it is all.
+  __device__ __forceinline__ void fetch(const HeadsArgs& a, long base) { first = position(a, base, threadIdx.x & 63); }
+  // Forms the angles of the tokens from `base` on, whose first positions have been asked for.
+  __device__ __forceinline__ void form(const HeadsArgs& a, long base, const uint64_t* freq, float2* table) const {
+    __builtin_amdgcn_wave_barrier();
+    int v = first;
+#pragma unroll 1
+    for (int k = 0; 64 * k < count; ++k) {
+      const int e = 64 * k + (threadIdx.x & 63);
+      if (k > 0) v = position(a, base, e);
+      const int t = token(e);
+      const uint64_t f = freq[e < count ? e - t * a.pairs : 0];
+      const uint32_t lo = static_cast<uint32_t>(f), hi = static_cast<uint32_t>(f >> 32), u = static_cast<uint32_t>(v);
+      float2 r;
+      turn(__umulhi(u, lo) + u * hi - (v < 0 ? lo : 0u), r.x, r.y);
+      table[e] = r;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  // Those of the lane's pairs, of the wave's token `token`.
+  __device__ __forceinline__ void read(const HeadsArgs& a, const float2* table, int token, int lane) {
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      const uint32_t x = (axes >> (4 * j)) & 15u;
-      const int v = x < 2 ? (x == 0 ? p[0] : p[1]) : (x == 2 ? p[2] : p[3]);
-      const uint32_t lo = static_cast<uint32_t>(f[j]), hi = static_cast<uint32_t>(f[j] >> 32), u = static_cast<uint32_t>(v);
-      turn(__umulhi(u, lo) + u * hi - (v < 0 ? lo : 0u), c[j], s[j]);
+      const float2 t = lane * C + j < a.pairs ? table[token * a.pairs + lane * C + j] : make_float2(1.f, 0.f);
+      c[j] = t.x;
+      s[j] = t.y;
     }
   }
 };
@@ -206,31 +222,38 @@ __device__ __forceinline__ float unit(float (&x)[2 * C], bool layer, bool in_a, 
 // rest of a wave's teams tokens beside each other.  A wave takes a group of tokens and `rounds` times its heads, so
 // that a token's angles are formed once for them.
 struct Lane {
-  int lane, head;
-  long token, step;          // the first token of this lane, and how far the next is
+  int lane, head, token;     // token: of the wave's
+  int tokens;                // of a wave
+  long base, step;           // the wave's first token, and how far the next group is
 };
 template <int LANES>
 __device__ __forceinline__ Lane my_lane(const HeadsPart& p, int block) {
   const int in_wave = (threadIdx.x & 63) / LANES, wave = threadIdx.x >> 6;
-  const int tokens = (64 / LANES) >> p.head_bits;
   Lane l;
+  l.tokens = (64 / LANES) >> p.head_bits;
   l.lane = threadIdx.x & (LANES - 1);
   l.head = in_wave & ((1 << p.head_bits) - 1);
   const int group = block / p.splits, split = block - group * p.splits;
   l.head += split * (p.rounds << p.head_bits);
-  l.token = (static_cast<long>(group) * (THREADS / 64) + wave) * tokens + (in_wave >> p.head_bits);
-  l.step = static_cast<long>(p.groups) * (THREADS / 64) * tokens;
+  l.token = in_wave >> p.head_bits;
+  l.base = (static_cast<long>(group) * (THREADS / 64) + __builtin_amdgcn_readfirstlane(wave)) * l.tokens;
+  l.step = static_cast<long>(p.groups) * (THREADS / 64) * l.tokens;
   return l;
 }
 
 template <typename T, int C, int LANES, bool HALVES>
 __global__ __launch_bounds__(THREADS) void heads_forward_kernel(HeadsArgs a) {
+  __shared__ uint64_t freq[HEADS_PAIRS];
+  __shared__ float2 turns[THREADS / 64][64 * C];
+  if (threadIdx.x < HEADS_PAIRS) freq[threadIdx.x] = a.freq[threadIdx.x];
+  __syncthreads();
   const bool second = static_cast<int>(blockIdx.x) >= a.part[0].blocks;
   const HeadsPart& p = a.part[second];
   const Lane l = my_lane<LANES>(p, blockIdx.x - (second ? a.part[0].blocks : 0));
   const Place<C, HALVES> at(l.lane, a.dim, a.pairs);
   Angles<C> angles;
-  angles.template pairs<LANES>(a, l.lane);
+  angles.begin(a, l.tokens);
+  float2* const mine_turns = turns[threadIdx.x >> 6];
   float gamma[2 * C];
 #pragma unroll
   for (int e = 0; e < 2 * C; ++e) gamma[e] = 1.f;
@@ -243,29 +266,35 @@ __global__ __launch_bounds__(THREADS) void heads_forward_kernel(HeadsArgs a) {
   struct Item {
     Chunk<T, C> a, b;
     uint32_t row, index;     // batch row, token of it
-    long token;
+    long base;               // the wave's first token: all its lanes take as many turns
+    bool in;
     int round;
   } next{};
-  auto fetch = [&](long token, int round) {
-    if (round == 0 && token < a.tokens) {
+  auto fetch = [&](long base, int round) {
+    const long token = base + l.token;
+    if (round == 0 && base < a.tokens) {
       next.row = static_cast<uint32_t>(token) / a.len;
       next.index = static_cast<uint32_t>(token) - next.row * a.len;
+      angles.fetch(a, base);
     }
-    next.token = token;
+    next.base = base;
     next.round = round;
     const int h = l.head + (round << p.head_bits);
     const T* const x = static_cast<const T*>(p.x) + next.row * p.x_stride[0] + next.index * p.x_stride[1] + h * p.x_stride[2];
     next.a = next.b = Chunk<T, C>{};
-    const bool in = token < a.tokens && h < p.heads;
+    const bool in = next.in = token < a.tokens && h < p.heads;
     if (in && at.in_a) next.a.load(x + at.a);
     if (in && at.in_b) next.b.load(x + at.b);
   };
-  fetch(l.token, 0);
-  while (next.token < a.tokens) {
+  fetch(l.base, 0);
+  while (next.base < a.tokens) {
     const Item now = next;
-    if (now.round == 0) angles.at(a, static_cast<uint32_t>(now.token), now.index);
+    if (now.round == 0) {
+      angles.form(a, now.base, freq, mine_turns);
+      angles.read(a, mine_turns, l.token, l.lane);
+    }
     const bool more = now.round + 1 < p.rounds;
-    fetch(more ? now.token : now.token + l.step, more ? now.round + 1 : 0);
+    fetch(more ? now.base : now.base + l.step, more ? now.round + 1 : 0);
     float x[2 * C];
     now.a.get(x);
     now.b.get(x + C);
@@ -284,7 +313,7 @@ __global__ __launch_bounds__(THREADS) void heads_forward_kernel(HeadsArgs a) {
     }
     rotate<C, HALVES, false>(x, angles, at);
     const int h = l.head + (now.round << p.head_bits);
-    if (h >= p.heads) continue;
+    if (!now.in) continue;
     T* const y = static_cast<T*>(p.y) + now.row * p.y_stride[0] + now.index * p.y_stride[1] + h * p.y_stride[2];
     if (at.in_a) Chunk<T, C>::store(y + at.a, x);
     if (at.in_b) Chunk<T, C>::store(y + at.b, x + C);
@@ -293,17 +322,23 @@ __global__ __launch_bounds__(THREADS) void heads_forward_kernel(HeadsArgs a) {
 
 // Sums of the parameters' gradients stay in registers over a workgroup's tokens; its teams' are then added
 // in a fixed order and written as a row of partial sums, which heads_join_kernel adds in a fixed order too.
-// BETA: a norm has one.
-template <typename T, int C, int LANES, bool HALVES, bool BETA>
-__global__ __launch_bounds__(THREADS) void heads_backward_kernel(HeadsArgs a) {
+// FULL: a layer norm or a beta (what only those need).
+template <typename T, int C, int LANES, bool HALVES, bool FULL>
+__global__ __launch_bounds__(THREADS, FULL ? 1 : 4) void heads_backward_kernel(HeadsArgs a) {
+  const bool layer = FULL && a.layer != 0;
   __shared__ float joined[THREADS / 64][128];
+  __shared__ uint64_t freq[HEADS_PAIRS];
+  __shared__ float2 turns[THREADS / 64][64 * C];
+  if (threadIdx.x < HEADS_PAIRS) freq[threadIdx.x] = a.freq[threadIdx.x];
+  __syncthreads();
   const bool second = static_cast<int>(blockIdx.x) >= a.part[0].blocks;
   const HeadsPart& p = a.part[second];
   const int block = blockIdx.x - (second ? a.part[0].blocks : 0);
   const Lane l = my_lane<LANES>(p, block);
   const Place<C, HALVES> at(l.lane, a.dim, a.pairs);
   Angles<C> angles;
-  angles.template pairs<LANES>(a, l.lane);
+  angles.begin(a, l.tokens);
+  float2* const mine_turns = turns[threadIdx.x >> 6];
   const bool norm = p.gamma != nullptr;
   float gamma[2 * C], dgamma[2 * C] = {}, dbeta[2 * C] = {};
 #pragma unroll
@@ -316,21 +351,24 @@ __global__ __launch_bounds__(THREADS) void heads_backward_kernel(HeadsArgs a) {
   struct Item {
     Chunk<T, C> ga, gb, xa, xb;
     uint32_t row, index;     // batch row, token of it
-    long token;
+    long base;               // the wave's first token: all its lanes take as many turns
+    bool in;
     int round;
   } next{};
-  auto fetch = [&](long token, int round) {
-    if (round == 0 && token < a.tokens) {
+  auto fetch = [&](long base, int round) {
+    const long token = base + l.token;
+    if (round == 0 && base < a.tokens) {
       next.row = static_cast<uint32_t>(token) / a.len;
       next.index = static_cast<uint32_t>(token) - next.row * a.len;
+      angles.fetch(a, base);
     }
-    next.token = token;
+    next.base = base;
     next.round = round;
     const int h = l.head + (round << p.head_bits);
     const T* const dy = static_cast<const T*>(p.dy) + next.row * p.y_stride[0] + next.index * p.y_stride[1] + h * p.y_stride[2];
     const T* const x = static_cast<const T*>(p.x) + next.row * p.x_stride[0] + next.index * p.x_stride[1] + h * p.x_stride[2];
     next.ga = next.gb = next.xa = next.xb = Chunk<T, C>{};
-    const bool in = token < a.tokens && h < p.heads;
+    const bool in = next.in = token < a.tokens && h < p.heads;
     if (in && at.in_a) {
       next.ga.load(dy + at.a);
       if (norm) next.xa.load(x + at.a);
@@ -340,12 +378,15 @@ __global__ __launch_bounds__(THREADS) void heads_backward_kernel(HeadsArgs a) {
       if (norm) next.xb.load(x + at.b);
     }
   };
-  fetch(l.token, 0);
-  while (next.token < a.tokens) {
+  fetch(l.base, 0);
+  while (next.base < a.tokens) {
     const Item now = next;
-    if (now.round == 0) angles.at(a, static_cast<uint32_t>(now.token), now.index);
+    if (now.round == 0) {
+      angles.form(a, now.base, freq, mine_turns);
+      angles.read(a, mine_turns, l.token, l.lane);
+    }
     const bool more = now.round + 1 < p.rounds;
-    fetch(more ? now.token : now.token + l.step, more ? now.round + 1 : 0);
+    fetch(more ? now.base : now.base + l.step, more ? now.round + 1 : 0);
     float g[2 * C];
     now.ga.get(g);
     now.gb.get(g + C);
@@ -354,22 +395,22 @@ __global__ __launch_bounds__(THREADS) void heads_backward_kernel(HeadsArgs a) {
       float x[2 * C], s = 0.f, m = 0.f;
       now.xa.get(x);
       now.xb.get(x + C);
-      const float r = unit<C, LANES>(x, a.layer, at.in_a, at.in_b, a.inv_dim, a.eps);
+      const float r = unit<C, LANES>(x, layer, at.in_a, at.in_b, a.inv_dim, a.eps);
 #pragma unroll
       for (int e = 0; e < 2 * C; ++e) {
         dgamma[e] = fmaf(g[e], x[e], dgamma[e]);
-        if (BETA) dbeta[e] += g[e];
+        if (FULL) dbeta[e] += g[e];
         g[e] *= gamma[e];
         s = fmaf(g[e], x[e], s);
-        m += g[e];
+        if (FULL) m += g[e];
       }
       s = team_sum<LANES>(s) * a.inv_dim;
-      m = a.layer ? team_sum<LANES>(m) * a.inv_dim : 0.f;
+      m = layer ? team_sum<LANES>(m) * a.inv_dim : 0.f;
 #pragma unroll
       for (int e = 0; e < 2 * C; ++e) g[e] = r * (g[e] - x[e] * s - m);
     }
     const int h = l.head + (now.round << p.head_bits);
-    if (h >= p.heads) continue;
+    if (!now.in) continue;
     T* const dx = static_cast<T*>(p.dx) + now.row * p.x_stride[0] + now.index * p.x_stride[1] + h * p.x_stride[2];
     if (at.in_a) Chunk<T, C>::store(dx + at.a, g);
     if (at.in_b) Chunk<T, C>::store(dx + at.b, g + C);
@@ -392,7 +433,7 @@ __global__ __launch_bounds__(THREADS) void heads_backward_kernel(HeadsArgs a) {
     }
   };
   flush(dgamma, p.part_gamma);
-  if (BETA && p.beta != nullptr) flush(dbeta, p.part_beta);
+  if (FULL && p.beta != nullptr) flush(dbeta, p.part_beta);
 }
 
 // Output blockIdx.x (dgamma and dbeta of the queries, then of the keys), channels 16 blockIdx.y ..: the sum over rows of
@@ -437,7 +478,7 @@ void launch(const HeadsArgs& a, bool backward, hipStream_t s) {
   auto by_layout = [&](auto halves) {
     constexpr bool HALVES = decltype(halves)::value;
     if (!backward) heads_forward_kernel<T, C, LANES, HALVES><<<n, THREADS, 0, s>>>(a);
-    else if (a.part[0].beta != nullptr || a.part[1].beta != nullptr) heads_backward_kernel<T, C, LANES, HALVES, true><<<n, THREADS, 0, s>>>(a);
+    else if (a.layer || a.part[0].beta != nullptr || a.part[1].beta != nullptr) heads_backward_kernel<T, C, LANES, HALVES, true><<<n, THREADS, 0, s>>>(a);
     else heads_backward_kernel<T, C, LANES, HALVES, false><<<n, THREADS, 0, s>>>(a);
   };
   if (a.halves) by_layout(std::true_type{});
@@ -468,24 +509,34 @@ void by_shape(const HeadsArgs& a, bool backward, hipStream_t s) {
 
 void heads_plan(HeadsArgs& a, bool backward) {
   const int teams = 64 / lanes(a);
-  // workgroups of both parts together: 8 a CU forward; backward, where each leaves a row of partial sums, 4
-  const long most = backward ? 1024 : 2048;
-  const long work = a.tokens * (a.part[0].heads + a.part[1].heads);
-  for (HeadsPart& p : a.part) {
-    p.blocks = 0;
+  // workgroups of both parts together: as many as the chip holds at once
+  const long most = 256 * (!backward ? 8 : chunk(a) == 8 ? 4 : 5);
+  long units = 0, want[2] = {}, all[2] = {};
+  for (int i = 0; i < 2; ++i) {
+    HeadsPart& p = a.part[i];
+    p.blocks = p.head_bits = 0;
     if (p.heads == 0 || a.tokens == 0) continue;
-    p.head_bits = 0;
     while ((1 << p.head_bits) < p.heads && (2 << p.head_bits) <= teams) ++p.head_bits;
-    const int all = (p.heads + (1 << p.head_bits) - 1) >> p.head_bits;
     const long tokens = static_cast<long>(teams >> p.head_bits) * (THREADS / 64);
-    const long want = (a.tokens + tokens - 1) / tokens;
-    long share = static_cast<long>(static_cast<double>(most) * a.tokens * p.heads / work);
-    if (share < 1) share = 1;
-    // few tokens: the rounds over heads go to workgroups of their own
-    p.splits = want * all <= share ? all : 1;
-    p.rounds = (all + p.splits - 1) / p.splits;
-    p.groups = static_cast<int>(want < share ? want : share);
-    p.blocks = p.groups * p.splits;
+    all[i] = (p.heads + (1 << p.head_bits) - 1) >> p.head_bits;
+    want[i] = (a.tokens + tokens - 1) / tokens;
+    units += want[i] * all[i];
+  }
+  // rounds a workgroup: the fewest by which no workgroup is left for a second turn (16384 tokens, 16 + 4 heads of 128: 10 give 1025
+  // workgroups and take 73 us backward, 11 give 870)
+  for (long each = (units + most - 1) / most, total = most + 1; total > most; ++each) {
+    total = 0;
+    for (int i = 0; i < 2; ++i) {
+      HeadsPart& p = a.part[i];
+      if (want[i] == 0) continue;
+      // few tokens: the rounds over heads go to workgroups of their own
+      p.splits = each == 1 ? static_cast<int>(all[i]) : 1;
+      p.rounds = static_cast<int>(all[i] / p.splits);
+      const long per = (each + p.rounds - 1) / p.rounds;
+      p.groups = static_cast<int>((want[i] + per - 1) / per);
+      p.blocks = p.groups * p.splits;
+      total += p.blocks;
+    }
   }
 }
 
