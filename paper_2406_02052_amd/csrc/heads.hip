@@ -241,6 +241,7 @@ __device__ __forceinline__ Lane my_lane(const HeadsPart& p, int block) {
   return l;
 }
 
+// 16384 tokens of 16 + 4 heads of 128 bf16 in 39 us, 4.3 TB/s (30 from the last cache).
 template <typename T, int C, int LANES, bool HALVES>
 __global__ __launch_bounds__(THREADS) void heads_forward_kernel(HeadsArgs a) {
   __shared__ uint64_t freq[HEADS_PAIRS];
@@ -323,6 +324,7 @@ __global__ __launch_bounds__(THREADS) void heads_forward_kernel(HeadsArgs a) {
 // Sums of the parameters' gradients stay in registers over a workgroup's tokens; its teams' are then added
 // in a fixed order and written as a row of partial sums, which heads_join_kernel adds in a fixed order too.
 // FULL: a layer norm or a beta (what only those need).
+// 16384 tokens of 16 + 4 heads of 128 bf16 in 64 us, 3.9 TB/s; of 16 + 16 with 60 pairs, 8 bytes a load, 93 us, 4.3 TB/s.
 template <typename T, int C, int LANES, bool HALVES, bool FULL>
 __global__ __launch_bounds__(THREADS, FULL ? 1 : 4) void heads_backward_kernel(HeadsArgs a) {
   const bool layer = FULL && a.layer != 0;

@@ -9,8 +9,8 @@
 // Z_i = sum_j e_ij = exp(loss_i), and both gradients are products of e as it lies:
 //   f_i = scale weight_i / Z_i,  e'_it = e_it - Z_i,  dx_i = f_i sum_j e'_ij w_j,  dw_j = sum_i e'_ij (f_i x_i)
 // where a maximum as the reference would have e rescaled, or the first product made twice.  bf16
-// has the exponents of fp32; a tile with scores of more than 2^86 times the target's takes its own largest as the
-// reference, and the row's e are brought to one when all are known.
+// has the exponents of fp32; a tile whose sum of a row passes 2^86 takes its own largest as the reference, and the
+// row's e are brought to one when all are known.
 //
 // Scores, sums, statistics and accumulators are fp32.  With bf16 tensors e and f x are rounded to bf16 as
 // operands of the products (the matrix unit takes bf16), 2^-9 of each term at most.
@@ -355,7 +355,10 @@ __global__ __launch_bounds__(1024) void vocab_mean_kernel(VocabArgs a) {
   }
 }
 
-// e of a tile (KEEP: kept; a bf16 tile goes through LDS, so that whole lines are written) and each row's sum of it.
+// e of a tile (KEEP: kept; a bf16 tile goes through LDS, so that whole lines are written) and each row's sum of it.  4096 x 4096 by
+// 131072 bf16 in 3.75 ms, 1.17 PFLOP/s (matrix units 67 % busy at 1.6 GHz, where power holds the clock); with 1024 inner indices the 65536
+// exponentials of a tile come after 16 steps only: 2048 by 32768 in 150 us, 0.9.  With e written by the lanes that hold it, 8 bytes in a line
+// each, 4.14 ms and 178 us.
 template <typename T, typename P, bool KEEP>
 __global__ __launch_bounds__(P::THREADS, 2) void vocab_scores_kernel(VocabArgs a) {
   constexpr int MB = P::MB, NB = P::NB, CHUNKS = P::BN / 8;   // chunks of 16 bytes of a line of e, moved by the line's number
@@ -472,7 +475,7 @@ __global__ __launch_bounds__(P::THREADS, 2) void vocab_scores_kernel(VocabArgs a
 }
 
 // A row's Z, loss and lse from its tiles' sums; with gradients also its factor, f x, the target's e' and what had another
-// reference.  A workgroup a row.
+// reference.  A workgroup a row: 4096 rows of 4096 over 512 tiles in 20 us.
 template <typename T, bool KEEP>
 __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a) {
   __shared__ float lds[8];
@@ -571,7 +574,9 @@ __device__ __forceinline__ void finish(const VocabGrad& g, long row, long col, f
   }
 }
 
-// rows x cols results, inner indices split over g.splits workgroups, whose sums then go to g.part.
+// rows x cols results, inner indices split over g.splits workgroups, whose sums then go to g.part.  dx of 4096 x 4096 over 131072 bf16
+// 3.4 ms, 1.3 PFLOP/s (79 % busy at 1.4 GHz; a library's product of that order 3.1); dw, whose operands both have to be
+// transposed on their way from LDS, 4.0 (3.6 to 3.9).
 template <typename T, typename P>
 __global__ __launch_bounds__(P::THREADS, 2) void vocab_grad_kernel(VocabGrad g) {
   __shared__ __attribute__((aligned(16))) char lds[P::LDS];
