@@ -642,7 +642,7 @@ petra_status petra_vocab_gradient(const petra_vocab_desc* desc, const void* x, c
  *
  * The tensors are laid out once: petra_adamw_layout writes a table, which the caller copies to
  * device memory (16-byte aligned) and keeps, with the tensors, as long as it steps.
- * Limits: n >= 0, count at most 2^20, all chunks of 4096 elements below 2^31. */
+ * Limits: n >= 0, count at most 2^20, all chunks of 4096 elements fewer than 2^24. */
 enum { PETRA_E4M3 = 2 };   /* state_dtype only */
 
 typedef struct {

@@ -279,6 +279,12 @@ def _stream(stream) -> int:
     return stream.cuda_stream
 
 
+def _device() -> int:
+    """The current device, -1 where none has been used."""
+    import torch
+    return torch.cuda.current_device() if torch.cuda.is_initialized() else -1
+
+
 # ---------------------------------------------------------------------------
 # One wrapper per C entry point, same names and argument order.
 # ---------------------------------------------------------------------------

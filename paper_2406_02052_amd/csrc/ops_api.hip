@@ -934,6 +934,7 @@ petra_status petra_vocab_gradient(const petra_vocab_desc* desc, const void* x, c
 namespace {
 
 constexpr size_t ADAMW_WORKSPACE = 16;
+constexpr int64_t ADAMW_CHUNKS = int64_t{1} << 24;   // a workgroup of 256 each: a grid has fewer than 2^32 lanes
 
 struct AdamwTable {
   int64_t chunks = 0;
@@ -960,7 +961,7 @@ AdamwTable adamw_table(const petra_adamw_desc* d, const petra_adamw_tensor* tens
   for (int64_t i = 0; i < count; ++i) {
     need(tensors[i].n >= 0 && tensors[i].n <= (int64_t{1} << 42), PETRA_ERR_SHAPE, "negative or too large tensor");
     t.chunks += (tensors[i].n + petra::ADAMW_CHUNK - 1) / petra::ADAMW_CHUNK;
-    need(t.chunks < (int64_t{1} << 31), PETRA_ERR_SHAPE, "too many elements");
+    need(t.chunks < ADAMW_CHUNKS, PETRA_ERR_SHAPE, "too many elements");
   }
   t.bytes = adamw_bytes(count, t.chunks);
   return t;
@@ -1039,7 +1040,7 @@ petra_status petra_adamw_step(const petra_adamw_desc* desc, const void* table, s
                               void* workspace, size_t workspace_bytes, void* stream) {
   return entry("petra_adamw_step", [&]() -> bool {
     need_adamw(desc);
-    need(count >= 0 && count <= (int64_t{1} << 20) && chunks >= 0 && chunks < (int64_t{1} << 31), PETRA_ERR_SHAPE,
+    need(count >= 0 && count <= (int64_t{1} << 20) && chunks >= 0 && chunks < ADAMW_CHUNKS, PETRA_ERR_SHAPE,
          "negative or too large count");
     need(chunks == 0 || table != nullptr, PETRA_ERR_INVALID_ARG, "null pointer: table");
     need(table_bytes >= adamw_bytes(count, chunks), PETRA_ERR_WORKSPACE, "table too small for its tensors and chunks");

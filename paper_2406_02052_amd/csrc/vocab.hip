@@ -318,13 +318,12 @@ __device__ __forceinline__ float max16f(float v) {
   return over(v, Const<0x140>{});
 }
 
-// A row's reference, its target's score in binary logarithms, a wave a row.
+// A row's reference, its target's score in binary logarithms, a wave a row of those at work.
 template <typename T>
 __global__ __launch_bounds__(256) void vocab_target_kernel(VocabArgs a) {
-  const long row = static_cast<long>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (row >= a.rows) return;
+  const long of = static_cast<long>(blockIdx.x) * 4 + (threadIdx.x >> 6), row = a.row0 + of;
   const int lane = threadIdx.x & 63;
-  if (!takes_part(a, row)) return;
+  if (of >= a.piece || !takes_part(a, row)) return;
   const int t = a.targets[row];
   const T* const x = static_cast<const T*>(a.x) + row * a.width;
   const T* const w = static_cast<const T*>(a.w) + static_cast<long>(t) * a.width;
@@ -727,7 +726,6 @@ void run(const VocabArgs& all, const VocabPlan& p, bool gradients, hipStream_t s
     if (gradients) add<T>(none, s);
     return;
   }
-  vocab_target_kernel<T><<<static_cast<unsigned>(up(a.rows, 4)), 256, 0, s>>>(a);
   if (gradients && a.weight == nullptr) vocab_mean_kernel<<<1, 1024, 0, s>>>(a);
   a.row_tile = p.row_tile;
   a.col_tile = p.col_tile;
@@ -735,6 +733,7 @@ void run(const VocabArgs& all, const VocabPlan& p, bool gradients, hipStream_t s
   for (a.row0 = 0; a.row0 < a.rows; a.row0 += p.piece) {
     a.piece = a.rows - a.row0 < p.piece ? a.rows - a.row0 : p.piece;
     a.row_tiles = static_cast<int>(up(a.piece, a.row_tile));
+    vocab_target_kernel<T><<<static_cast<unsigned>(up(a.piece, 4)), 256, 0, s>>>(a);
     scores<T>(a, gradients, s);
     const unsigned n = static_cast<unsigned>(a.piece);
     if (!gradients) {
@@ -763,6 +762,7 @@ VocabPlan vocab_plan(const VocabArgs& a, int dtype, bool gradients, long piece_r
   // 2^30 bytes of e at a time, in whole tiles; without it 2^30 of sums
   long most = gradients ? (1L << 30) / (a.vocab_padded * static_cast<long>(esz)) : (1L << 30) / (8 * up(a.vocab, 64));
   most = most < 256 ? 256 : most / 256 * 256;
+  if (most > 1L << 23) most = 1L << 23;   // (a grid has fewer than 2^32 lanes, and some have a workgroup a row)
   if (piece_rows > 0 && piece_rows < most) most = piece_rows;
   const long rows = a.rows > 0 ? a.rows : 1;
   p.piece = rows < most ? rows : most;

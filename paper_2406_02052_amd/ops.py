@@ -65,6 +65,17 @@ class _Owner:
         """The owner's memory that its calls use."""
         return (self.workspace,)
 
+    def _need_here(self, *tensors) -> None:
+        """The tensors, and the current device, whose stream runs the call, are the owner's."""
+        index = self.workspace.get_device()
+        for t in tensors:
+            if t is not None and t.get_device() != index:
+                raise ValueError(f"need all tensors on the owner's device {self.workspace.device}, "
+                                 f"got one on {t.device}")
+        if L._device() != index:
+            raise ValueError(f"the current device is {L._device()}, the owner's "
+                             f"{self.workspace.device}")
+
 
 class Attention(_Owner):
     """Attention of [batch, q_len, heads, head_dim] over [batch, kv_len, kv_heads, head_dim]
@@ -247,7 +258,7 @@ class HeadNorm(_Owner):
 
     @staticmethod
     def _form(tensors):
-        return [(t.shape, t.stride(), t.dtype, t.is_cuda) if t is not None else None
+        return [(t.shape, t.stride(), t.dtype, t.get_device()) if t is not None else None
                 for t in tensors]
 
     def _lay(self, back, acts, params, positions) -> None:
@@ -255,8 +266,8 @@ class HeadNorm(_Owner):
         their gradients too, at the end) and what is laid out like the results; params: the
         norms' and (back) their gradients'.  What was checked last (types, shapes and strides) is
         not checked again."""
-        form = self._form(acts + params + (positions,))
-        if self.form == (back, form):
+        form = (back, L._device(), self._form(acts + params + (positions,)))
+        if self.form == form:
             return
         self.form = None
         names = ("dq", "dk", "dyq", "dyk", "q", "k") if back else ("q", "k", "yq", "yk")
@@ -280,7 +291,8 @@ class HeadNorm(_Owner):
                 _need(t, name, self.ftype, self.param_shape)
         if positions is not None:
             _need(positions, "positions", self.itype, self.positions_shape)
-        self.form = (back, form)
+        self._need_here(*acts, *params, positions)
+        self.form = form
 
     @staticmethod
     def _strides(t, name: str):
@@ -339,6 +351,7 @@ class VocabLoss(_Owner):
         _need(targets, "targets", self.itype, self.row_shape)
         _need(loss, "loss", self.ftype, self.row_shape)
         _need(lse, "lse", self.ftype, self.row_shape)
+        self._need_here(x, w, targets, loss, lse)
 
     def forward(self, x, w, targets, loss, lse, stream=None) -> None:
         """Writes loss and lse, fp32 [rows]."""
@@ -354,6 +367,7 @@ class VocabLoss(_Owner):
         _need(dw, "dw", self.tdtype, self.w_shape)
         if weight is not None:
             _need(weight, "weight", self.ftype, self.row_shape)
+        self._need_here(dx, dw, weight)
         L.petra_vocab_gradient(self.desc, x, w, targets, weight, loss, lse, dx, dw,
                                self.workspace, self.ws_bytes, self._on(stream))
 
@@ -443,6 +457,7 @@ class AdamW(_Owner):
         if grad_scale is not None:
             _need(grad_scale, "grad_scale", self.ftype, (1,))
         _need(self.lr, "lr", self.ftype, (1,))
+        self._need_here(rng, grad_scale, self.lr)
         L.petra_adamw_step(self.desc, self.table, self.table_bytes, self.count, self.chunks,
                            self.steps, self.lr, grad_scale, rng, self.workspace, self.ws_bytes,
                            self._on(stream))

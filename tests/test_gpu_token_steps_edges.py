@@ -266,3 +266,25 @@ def test_vocab_over_32_bits_of_offset():
     for j in (0, 12345, vocab // 2 + 1, vocab - 1, int(t[0])):
         p = (x.double() @ w[j].double() - total.log()).exp() - (t == j).double()
         near(dw[j], (p @ x.double() / rows).cpu().numpy(), TWO["bf16"], j)
+
+
+def test_vocab_of_more_rows_than_a_grid_has_waves():
+    """2^26 rows and some, in several pieces: rows of one of four kinds, whose results are each other's."""
+    from paper_2406_02052_amd import VocabLoss
+
+    rows, width, vocab = 2 ** 26 + 5, 8, 3
+    x4, = draw(1, (4, width), dtype="bf16")
+    w, = draw(2, (vocab, width), dtype="bf16")
+    t4 = np.array([2, 0, -1, 1])
+    kind = torch.arange(rows, device="cuda") % 4
+    t = i32(t4)[kind]
+    x = torch.empty(rows, width, dtype=torch.bfloat16, device="cuda")
+    for to, k in zip(x.split(2 ** 22), kind.split(2 ** 22)):   # (indexing for all at once leaves all but the first 5 rows empty)
+        to.copy_(dev(x4, "bf16")[k])
+    op = VocabLoss(rows, width, vocab, gradients=False)
+    loss, lse = nan((rows,)), nan((rows,))
+    op.forward(x, dev(w, "bf16"), t, loss, lse)
+    want = T.vocab_loss(x4, w, t4)
+    for got, r in ((loss, want[0]), (lse, want[1])):
+        r = torch.tensor(r, device="cuda")[kind]
+        assert ((got.double() - r).abs() <= 1e-5 * r.abs() + 1e-6).all()

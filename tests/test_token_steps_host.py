@@ -187,6 +187,26 @@ def test_adamw_descriptions(wrong, name):
     assert status(lambda: L.petra_adamw_query(d, t, 2)) == "PETRA_ERR_" + name
 
 
+def test_adamw_most_elements():
+    """A workgroup a chunk: fewer chunks than a grid holds."""
+    d, t = adam(n=4096 * (2 ** 23 - 1))
+    assert L.petra_adamw_query(d, t, 2)[1] == 2 ** 24 - 2
+    d, t = adam(n=4096 * 2 ** 23)
+    assert status(lambda: L.petra_adamw_query(d, t, 2)) == "PETRA_ERR_SHAPE"
+
+
+def test_owners_refuse_another_device():
+    """By what they compare, without a second one."""
+    import torch
+
+    from paper_2406_02052_amd.ops import _Owner
+
+    owner = _Owner()
+    owner.workspace = torch.empty(4)
+    with pytest.raises(ValueError, match="owner's device"):
+        owner._need_here(None, type("Elsewhere", (), {"get_device": lambda self: 1, "device": "cuda:1"})())
+
+
 def test_adamw_layout():
     d, t = adam(n=5000)
     size, chunks, ws = L.petra_adamw_query(d, t, 2)
