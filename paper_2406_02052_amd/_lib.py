@@ -282,7 +282,12 @@ def _stream(stream) -> int:
 def _device() -> int:
     """The current device, -1 where none has been used."""
     import torch
-    return torch.cuda.current_device() if torch.cuda.is_initialized() else -1
+    if not torch.cuda.is_initialized():
+        return -1
+    try:
+        return torch._C._cuda_getDevice()   # (0.1 us; the public call 0.3)
+    except AttributeError:
+        return torch.cuda.current_device()
 
 
 # ---------------------------------------------------------------------------

@@ -609,6 +609,21 @@ namespace {
 
 static_assert(petra::HEADS_AXES == PETRA_HEAD_AXES && petra::HEADS_PAIRS == PETRA_HEAD_PAIRS, "the header's limits");
 
+// The fraction of a turn that `radians` are, in 64 bits; a whole one wraps.  (Without the library's floorl and roundl, which take
+// longer than all else that a call does on the host.)
+uint64_t turn_fraction(double radians) {
+  long double f = static_cast<long double>(radians) * 0.159154943091895335768883763372514362L;   // 1 / 2 pi
+  if (f < 4.6e18L && f > -4.6e18L) {
+    const auto whole = static_cast<int64_t>(f);
+    f -= static_cast<long double>(whole);
+  } else {
+    f = fmodl(f, 1.0L);
+  }
+  if (f < 0.0L) f += 1.0L;
+  f = f * 18446744073709551616.0L + 0.5L;
+  return f >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(f);
+}
+
 struct Heads {
   petra::HeadsArgs a{};
   int64_t n[2][3];   // positions of the queries and of the keys
@@ -646,10 +661,7 @@ struct Heads {
       need(d->axis[i] >= 0 && d->axis[i] < d->axes, PETRA_ERR_INVALID_ARG, "a pair's axis is none of the axes");
       need(std::isfinite(d->freq[i]), PETRA_ERR_INVALID_ARG, "frequencies must be finite");
       a.axes4[i / 8] |= static_cast<uint32_t>(d->axis[i]) << (i % 8 * 4);
-      // the fraction of a turn in 64 bits; a whole one wraps
-      long double f = static_cast<long double>(d->freq[i]) / 6.283185307179586476925286766559005768L;
-      f = roundl((f - floorl(f)) * 18446744073709551616.0L);
-      a.freq[i] = f >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(f);
+      a.freq[i] = turn_fraction(d->freq[i]);
     }
     for (int i = 0; i < 2; ++i) {
       petra::HeadsPart& p = a.part[i];
