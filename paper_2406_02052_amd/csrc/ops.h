@@ -106,7 +106,8 @@ void heads_backward(const HeadsArgs& a, int dtype, hipStream_t s);
 struct VocabGrad {
   const void *a, *b;
   void* out;
-  const float* factor;                       // [rows], nullable
+  const float *factor, *rest;                // [rows], nullable together: factors, and those of b's lines `targets` beside the product
+  const int32_t* targets;
   float *part, *acc;                         // the splits' sums; sums over the pieces of rows
   long rows, cols, inner, a_ld, a_free, b_inner, per_split;   // a_free: rows, or as many as a's lines have
   int splits, tile, row_tiles, col_tiles, add, last;
@@ -122,8 +123,8 @@ struct VocabArgs {
   int row_tiles, col_tiles, row_tile, col_tile;
   float scale, scale_log2;                   // scale_log2 = scale log2(e)
   // workspace: each row's reference; of a piece the tiles' sums, the references that differ and which tiles
-  // have them, e, factors and x times them
-  float *ref, *sums, *shift, *mean, *factor, *part, *acc;
+  // have them, e, factors, x times them, and what rounding the target's e left
+  float *ref, *sums, *shift, *mean, *factor, *rest, *part, *acc;
   int* slow;
   void *scaled, *e;
 };
@@ -131,7 +132,7 @@ struct VocabPlan {
   long piece;
   int row_tile, col_tile;                    // of the scores
   VocabGrad dx, dw;                          // tile, splits and per_split
-  size_t ref, sums, shift, slow, mean, factor, scaled, e, part, acc, bytes;   // offsets in the workspace
+  size_t ref, sums, shift, slow, mean, factor, rest, scaled, e, part, acc, bytes;   // offsets in the workspace
 };
 
 // piece_rows: rows at a time (0: by the rule).

@@ -487,7 +487,7 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a) {
     if (threadIdx.x == 0) {
       a.loss[all] = 0.f;
       a.lse[all] = 0.f;
-      if (KEEP) a.factor[row] = 0.f;
+      if (KEEP) a.factor[row] = a.rest[row] = 0.f;
     }
     if (KEEP) {
       const float none[8] = {};
@@ -531,9 +531,11 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a) {
       }
       __syncthreads();   // before the target's
     }
+    // the target's, of which dx mostly consists: what its rounding leaves goes to dx by itself
     if (threadIdx.x == 0) {
-      T* const p = e + a.targets[all];
-      store1(p, load1(p) - z);
+      const float t = __builtin_amdgcn_exp2f(-top) - z;
+      store1(e + a.targets[all], t);
+      a.rest[row] = f * (t - quant(t, static_cast<const T*>(nullptr)));
     }
     const T* const x = static_cast<const T*>(a.x) + all * a.width;
     for (int c = threadIdx.x * 8; c < a.width; c += 2048) {
@@ -550,7 +552,7 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a) {
 // gradients
 // ---------------------------------------------------------------------------
 
-// Where a gradient's sums go: times the row's factor, added to what earlier pieces gave, and on to the tensor or to the sums
+// Where a gradient's sums go: times the row's factor, with what is left of its target's term, added to what earlier pieces gave, and on to the tensor or to the sums
 // for the next piece.
 template <typename T>
 __device__ __forceinline__ void finish(const VocabGrad& g, long row, long col, float (&v)[4]) {
@@ -559,6 +561,16 @@ __device__ __forceinline__ void finish(const VocabGrad& g, long row, long col, f
     const float f = g.factor[row];
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] *= f;
+    if constexpr (sizeof(T) == 2) {
+      const float r = g.rest[row];
+      if (r != 0.f) {
+        const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const T*>(g.b) + static_cast<long>(g.targets[row]) * g.cols + col);
+        v[0] = fmaf(r, __uint_as_float(w.x << 16), v[0]);
+        v[1] = fmaf(r, __uint_as_float(w.x & 0xffff0000u), v[1]);
+        v[2] = fmaf(r, __uint_as_float(w.y << 16), v[2]);
+        v[3] = fmaf(r, __uint_as_float(w.y & 0xffff0000u), v[3]);
+      }
+    }
   }
   if (g.add) {
     const float4 o = *reinterpret_cast<const float4*>(g.acc + at);
@@ -743,7 +755,7 @@ void run(const VocabArgs& all, const VocabPlan& p, bool gradients, hipStream_t s
     vocab_join_kernel<T, true><<<n, 256, 0, s>>>(a);
     VocabGrad x = p.dx, w = p.dw;
     x.a = a.e, x.b = a.w, x.a_ld = a.vocab_padded, x.a_free = a.piece, x.b_inner = a.vocab, x.rows = a.piece, x.cols = a.width, x.inner = a.vocab_padded;
-    x.out = static_cast<T*>(a.dx) + a.row0 * a.width, x.factor = a.factor, x.part = a.part, x.last = 1;
+    x.out = static_cast<T*>(a.dx) + a.row0 * a.width, x.factor = a.factor, x.rest = a.rest, x.targets = a.targets + a.row0, x.part = a.part, x.last = 1;
     grad<T, true, false>(x, s);
     w.a = a.e, w.b = a.scaled, w.a_ld = w.a_free = a.vocab_padded, w.b_inner = a.piece, w.rows = a.vocab, w.cols = a.width, w.inner = a.piece;
     w.out = a.dw, w.part = a.part, w.acc = a.acc, w.add = a.row0 > 0, w.last = a.row0 + a.piece == a.rows;
@@ -789,6 +801,7 @@ VocabPlan vocab_plan(const VocabArgs& a, int dtype, bool gradients, long piece_r
   if (gradients) {
     p.mean = take(4);
     p.factor = take(static_cast<size_t>(p.piece) * 4);
+    p.rest = take(static_cast<size_t>(p.piece) * 4);
     p.scaled = take(static_cast<size_t>(p.piece) * a.width * esz);
     p.e = take(static_cast<size_t>(p.piece) * a.vocab_padded * esz);
     p.dx.rows = p.piece, p.dx.cols = a.width, p.dx.inner = a.vocab_padded;
@@ -816,6 +829,7 @@ void vocab_run(VocabArgs a, const VocabPlan& p, int dtype, bool gradients, void*
   if (gradients) {
     a.mean = reinterpret_cast<float*>(ws + p.mean);
     a.factor = reinterpret_cast<float*>(ws + p.factor);
+    a.rest = reinterpret_cast<float*>(ws + p.rest);
     a.scaled = ws + p.scaled;
     a.e = ws + p.e;
     a.part = reinterpret_cast<float*>(ws + p.part);
