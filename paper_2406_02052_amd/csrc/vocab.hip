@@ -487,7 +487,7 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a) {
     if (threadIdx.x == 0) {
       a.loss[all] = 0.f;
       a.lse[all] = 0.f;
-      if (KEEP) a.factor[row] = a.rest[row] = 0.f;
+      if (KEEP) a.factor[row] = a.rest[row] = a.term[row] = 0.f;
     }
     if (KEEP) {
       const float none[8] = {};
@@ -531,11 +531,12 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a) {
       }
       __syncthreads();   // before the target's
     }
-    // the target's, of which dx mostly consists: what its rounding leaves goes to dx by itself
+    // the target's, of which the gradients mostly consist: what its rounding leaves goes to them by itself
     if (threadIdx.x == 0) {
       const float t = __builtin_amdgcn_exp2f(-top) - z;
       store1(e + a.targets[all], t);
       a.rest[row] = f * (t - quant(t, static_cast<const T*>(nullptr)));
+      a.term[row] = t;
     }
     const T* const x = static_cast<const T*>(a.x) + all * a.width;
     for (int c = threadIdx.x * 8; c < a.width; c += 2048) {
@@ -554,9 +555,21 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a) {
 
 // Where a gradient's sums go: times the row's factor, with what is left of its target's term, added to what earlier pieces gave, and on to the tensor or to the sums
 // for the next piece.
+// dw's result row is a column of the vocabulary, whose target rows are order[first .. last).
 template <typename T>
-__device__ __forceinline__ void finish(const VocabGrad& g, long row, long col, float (&v)[4]) {
+__device__ __forceinline__ void finish(const VocabGrad& g, long row, long col, int first, int last, float (&v)[4]) {
   const long at = row * g.cols + col;
+  if constexpr (sizeof(T) == 2) {
+    for (int k = first; k < last; ++k) {
+      const long i = g.order[k];
+      const float f = g.row_factor[i], t = g.term[i], q = quant(t, static_cast<const T*>(nullptr));
+      const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const T*>(g.x) + i * g.cols + col);
+      const float x[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                          __uint_as_float(w.y & 0xffff0000u)};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += fmaf(f * t, x[e], -q * quant(f * x[e], static_cast<const T*>(nullptr)));
+    }
+  }
   if (g.factor != nullptr) {
     const float f = g.factor[row];
 #pragma unroll
@@ -591,11 +604,14 @@ __device__ __forceinline__ void finish(const VocabGrad& g, long row, long col, f
 template <typename T, typename P>
 __global__ __launch_bounds__(P::THREADS, 2) void vocab_grad_kernel(VocabGrad g) {
   __shared__ __attribute__((aligned(16))) char lds[P::LDS];
+  __shared__ int lists[P::BM + 1];
   const int id = blockIdx.x / g.splits, split = blockIdx.x - id * g.splits;
   int mt, nt;
   tile_of(id, g.row_tiles, g.col_tiles, mt, nt);
   const long m0 = static_cast<long>(mt) * P::BM, n0 = static_cast<long>(nt) * P::BN;
   const long k0 = split * g.per_split, k1 = k0 + g.per_split < g.inner ? k0 + g.per_split : g.inner;
+  if (g.start != nullptr)   // (seen by all after the product's barriers)
+    for (int r = threadIdx.x; r <= P::BM; r += P::THREADS) lists[r] = g.start[m0 + r < g.rows ? m0 + r : g.rows];
   f32x16_t acc[P::MB][P::NB];
   P::zero(acc);
   {
@@ -634,8 +650,60 @@ __global__ __launch_bounds__(P::THREADS, 2) void vocab_grad_kernel(VocabGrad g) 
       const float4 x = *reinterpret_cast<const float4*>(lds + r * (CHUNKS * 16) + ((chunk ^ (r & 31 & (CHUNKS - 1))) << 4));
       float v[4] = {x.x, x.y, x.z, x.w};
       if (g.splits > 1) *reinterpret_cast<float4*>(g.part + (split * g.rows + row) * g.cols + col) = x;
-      else finish<T>(g, row, col, v);
+      else finish<T>(g, row, col, g.start != nullptr ? lists[row - m0] : 0, g.start != nullptr ? lists[row - m0 + 1] : 0, v);
     }
+  }
+}
+
+// The rows of a piece by their targets, those of one target in their own order: start[j] .. start[j + 1] of `order` are the rows with
+// target j.  A workgroup takes 256 columns and reads all targets twice, a quarter each wave: how many are below its columns
+// and at each of them, then where each row goes, wave after wave and a wave's rows one by one.
+__global__ __launch_bounds__(256) void vocab_lists_kernel(VocabArgs a) {
+  __shared__ int count[4][256], below[4], sums[4];
+  const int base = blockIdx.x * 256, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int32_t* const targets = a.targets + a.row0;
+  const long part = (a.piece + 255) / 256 * 64, from = wave * part, to = from + part < a.piece ? from + part : a.piece;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) count[w][tid] = 0;
+  __syncthreads();
+  int less = 0;
+#pragma unroll 4
+  for (long i = from + lane; i < to; i += 64) {
+    const int t = targets[i], c = t - base;
+    if (t < 0 || t >= a.vocab) continue;
+    less += c < 0;
+    if (c >= 0 && c < 256) atomicAdd(&count[wave][c], 1);   // (whole numbers: their order changes nothing)
+  }
+  for (int d = 32; d > 0; d >>= 1) less += __shfl_xor(less, d, 64);
+  if (lane == 0) below[wave] = less;
+  __syncthreads();
+  const int n = count[0][tid] + count[1][tid] + count[2][tid] + count[3][tid];
+  int upto = n;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int v = __shfl_up(upto, d, 64);
+    if (lane >= d) upto += v;
+  }
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  int at = below[0] + below[1] + below[2] + below[3] + upto - n;
+  for (int w = 0; w < wave; ++w) at += sums[w];
+  if (base + tid < a.vocab) a.start[base + tid] = at;
+  if (base + tid == a.vocab - 1) a.start[a.vocab] = at + n;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {   // where the next row of this column goes, for each wave
+    const int v = count[w][tid];
+    count[w][tid] = at;
+    at += v;
+  }
+  __syncthreads();
+  int next = from + lane < to ? targets[from + lane] : -1;
+  for (long first = from; first < to; first += 64) {
+    const long i = first + lane;
+    const int t = next, c = t - base;
+    next = i + 64 < to ? targets[i + 64] : -1;
+    for (uint64_t left = __ballot(t >= 0 && t < a.vocab && c >= 0 && c < 256); left != 0; left &= left - 1)
+      if (lane == __ffsll(static_cast<unsigned long long>(left)) - 1)   // (one at a time)
+        a.order[atomicAdd(&count[wave][c], 1)] = static_cast<int>(i);
   }
 }
 
@@ -650,7 +718,7 @@ __global__ __launch_bounds__(256) void vocab_add_kernel(VocabGrad g) {
       v[0] += o.x, v[1] += o.y, v[2] += o.z, v[3] += o.w;
     }
     const long row = at / g.cols;
-    finish<T>(g, row, at - row * g.cols, v);
+    finish<T>(g, row, at - row * g.cols, g.start != nullptr ? g.start[row] : 0, g.start != nullptr ? g.start[row + 1] : 0, v);
   }
 }
 
@@ -759,6 +827,11 @@ void run(const VocabArgs& all, const VocabPlan& p, bool gradients, hipStream_t s
     grad<T, true, false>(x, s);
     w.a = a.e, w.b = a.scaled, w.a_ld = w.a_free = a.vocab_padded, w.b_inner = a.piece, w.rows = a.vocab, w.cols = a.width, w.inner = a.piece;
     w.out = a.dw, w.part = a.part, w.acc = a.acc, w.add = a.row0 > 0, w.last = a.row0 + a.piece == a.rows;
+    if (p.lists) {
+      vocab_lists_kernel<<<static_cast<unsigned>(up(a.vocab, 256)), 256, 0, s>>>(a);
+      w.start = a.start, w.order = a.order, w.term = a.term, w.row_factor = a.factor;
+      w.x = static_cast<const T*>(a.x) + a.row0 * a.width;
+    }
     if (w.per_split >= w.inner) w.splits = 1;   // a last, smaller piece
     else w.splits = static_cast<int>(up(w.inner, w.per_split));
     grad<T, false, false>(w, s);
@@ -802,6 +875,11 @@ VocabPlan vocab_plan(const VocabArgs& a, int dtype, bool gradients, long piece_r
     p.mean = take(4);
     p.factor = take(static_cast<size_t>(p.piece) * 4);
     p.rest = take(static_cast<size_t>(p.piece) * 4);
+    p.term = take(static_cast<size_t>(p.piece) * 4);
+    // fp32 has no rounding to take back; and lists of many rows a column would be gone through by one thread each
+    p.lists = esz == 2 && p.piece <= 65536 && p.piece <= 16L * a.vocab;
+    p.start = take(p.lists ? (static_cast<size_t>(a.vocab) + 1) * 4 : 0);
+    p.order = take(p.lists ? static_cast<size_t>(p.piece) * 4 : 0);
     p.scaled = take(static_cast<size_t>(p.piece) * a.width * esz);
     p.e = take(static_cast<size_t>(p.piece) * a.vocab_padded * esz);
     p.dx.rows = p.piece, p.dx.cols = a.width, p.dx.inner = a.vocab_padded;
@@ -830,6 +908,9 @@ void vocab_run(VocabArgs a, const VocabPlan& p, int dtype, bool gradients, void*
     a.mean = reinterpret_cast<float*>(ws + p.mean);
     a.factor = reinterpret_cast<float*>(ws + p.factor);
     a.rest = reinterpret_cast<float*>(ws + p.rest);
+    a.term = reinterpret_cast<float*>(ws + p.term);
+    a.start = reinterpret_cast<int*>(ws + p.start);
+    a.order = reinterpret_cast<int*>(ws + p.order);
     a.scaled = ws + p.scaled;
     a.e = ws + p.e;
     a.part = reinterpret_cast<float*>(ws + p.part);

@@ -288,3 +288,24 @@ def test_vocab_of_more_rows_than_a_grid_has_waves():
     for got, r in ((loss, want[0]), (lse, want[1])):
         r = torch.tensor(r, device="cuda")[kind]
         assert ((got.double() - r).abs() <= 1e-5 * r.abs() + 1e-6).all()
+
+
+@pytest.mark.parametrize("rows,vocab,piece", [(2000, 300, 0), (1500, 1000, 700), (3000, 260, 0), (700, 257, 100), (64, 5000, 0), (5000, 300, 0)])
+def test_vocab_targets_of_many_rows(rows, vocab, piece):
+    """Targets that repeat (a third of all rows at one column, as of a frequent token), at the edges of groups of 256 columns and in
+    several pieces.  Where rows are listed by target (16 a column at most) what rounding leaves of their terms is taken
+    back and dw, whose larger part they are, is off by its own rounding and two of the smaller part: 2^-8, as dx."""
+    width = 72
+    x, w, t, weight = vocab_case(rows, width, vocab, "bf16", seed=3)
+    r = np.random.RandomState(1)
+    t[r.rand(rows) < 0.33] = 255
+    t[r.rand(rows) < 0.1] = vocab - 1
+    t[r.rand(rows) < 0.1] = -1
+    t[:3] = 0, 256 % vocab, vocab - 1
+    for wt in (None, weight):
+        out, _ = run_vocab(x, w, t, "bf16", wt, piece=piece)
+        want = T.vocab_loss(x, w, t, 1.0, wt)
+        near(out[2], want[2], ONE["bf16"], "dx")
+        near(out[3], want[3], ONE["bf16"] if (piece or rows) <= 16 * vocab else TWO["bf16"], "dw")
+        again, _ = run_vocab(x, w, t, "bf16", wt, piece=piece)
+        assert torch.equal(out[3], again[3])
