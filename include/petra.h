@@ -599,8 +599,9 @@ petra_status petra_heads_backward(const petra_heads_desc* desc, const void* q, c
  *
  * Rows are worked on in pieces (piece_rows at a time; 0: as many as keep a piece's scores within 1 GiB), whose
  * gradients of w are summed in fp32.  Scores, statistics and sums are fp32.  With bf16 tensors the softmax
- * and the weighted rows are rounded to bf16 as operands of the gradients' products: dx is off by about 1.4
- * times, dw by 1.75 times what rounding them alone to bf16 would give.
+ * and the weighted rows are rounded to bf16 as operands of the gradients' products, but for the targets' terms, which
+ * make most of them: dx and dw are off by 1.0 to 1.1 times what rounding them alone to bf16 would give (dw, in pieces of more
+ * than 16 rows a column or 65536 rows, by up to 1.75 times).
  * x, dx [rows][width] and w, dw [vocab][width] are contiguous, targets int32 [rows].
  * Limits: width a multiple of 8, at most 65536; 1 <= vocab <= 2^20; rows at most 2^30; scale > 0. */
 typedef struct {
