@@ -5,12 +5,14 @@
 //
 // Three products of 2 rows width vocabulary operations each; bound by them for all but a few rows.
 // The rows go in pieces, of which one at a time is held as e_ij = exp(s_ij - s_it) in the storage type: the
-// target's score is known before the product and a softmax may take any reference, so that
-// Z_i = sum_j e_ij = exp(loss_i), and both gradients are products of e as it lies:
-//   f_i = scale weight_i / Z_i,  e'_it = e_it - Z_i,  dx_i = f_i sum_j e'_ij w_j,  dw_j = sum_i e'_ij (f_i x_i)
-// where a maximum as the reference would have e rescaled, or the first product made twice.  bf16
-// has the exponents of fp32; a tile whose sum of a row passes 2^86 takes its own largest as the reference, and the
-// row's e are brought to one when all are known.
+// target's score is known before the product and a softmax may take any reference, so that with R_i = sum_{j != t} e_ij
+// loss_i = log(1 + R_i), and both gradients are products of e as it lies:
+//   f_i = scale weight_i / (1 + R_i),  e_it = -R_i,  dx_i = f_i sum_j e_ij w_j,  dw_j = sum_i e_ij (f_i x_i)
+// where a maximum as the reference would have e rescaled, or the first product made twice.  The product's own e_it is left
+// out of the sums: its score is the reference's sum in another order, and what they differ by (1e-5 at scores of 30) would be
+// the loss and gradient of a row whose target has all but 1e-5 of the softmax.  bf16 has the exponents of fp32; a tile
+// whose sum of a row passes 2^86 takes its own largest as the reference, and the row's e are brought to one when all are
+// known.
 //
 // Scores, sums, statistics and accumulators are fp32.  With bf16 tensors e and f x are rounded to bf16 as
 // operands of the products (the matrix unit takes bf16), 2^-9 of each term at most.  The targets' terms are most of both
@@ -395,6 +397,15 @@ __global__ __launch_bounds__(P::THREADS, 2) void vocab_scores_kernel(VocabArgs a
     const bool in = row < a.piece && takes_part(a, a.row0 + row);
     live[i] = in ? ~0u : 0u;
     c[i] = in ? -a.ref[a.row0 + row] : 0.f;
+    // the target's, which few waves have
+    const int own = in ? a.targets[a.row0 + row] - static_cast<int>(n0) - wn : -1;
+    if (__any(own >= 0 && own < 32 * NB)) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (own == 32 * j + 8 * (e >> 2) + 4 * h + (e & 3)) acc[i][j][e] = -INF;
+    }
   }
   // e and its sums; whether a row's passed MOST
   auto exponentials = [&]() {
@@ -474,7 +485,7 @@ __global__ __launch_bounds__(P::THREADS, 2) void vocab_scores_kernel(VocabArgs a
   }
 }
 
-// A row's Z, loss and lse from its tiles' sums; with gradients also its factor, f x, the target's e' and what had another
+// A row's R, loss and lse from its tiles' sums; with gradients also its factor, f x, the target's e and what had another
 // reference.  A workgroup a row: 4096 rows of 4096 over 512 tiles in 20 us.
 template <typename T, bool KEEP>
 __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a) {
@@ -510,8 +521,9 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a) {
   s = wave_sum(s);
   if (lane == 0) lds[4 + wave] = s;
   __syncthreads();
-  const float z = lds[4] + lds[5] + lds[6] + lds[7];
-  const float loss = LN2 * (top + log2f(z));
+  // of the others and the target, with 2^top as the unit (own: NaN where the target's score is no finite number)
+  const float rest = lds[4] + lds[5] + lds[6] + lds[7], own = __builtin_amdgcn_exp2f(ref - ref - top), z = own + rest;
+  const float loss = top > 0.f ? LN2 * (top + log2f(z)) : log1pf(rest / own);
   if (threadIdx.x == 0) {
     a.loss[all] = loss;
     a.lse[all] = fmaf(LN2, ref, loss);
@@ -534,7 +546,7 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a) {
     }
     // the target's, of which the gradients mostly consist: what its rounding leaves goes to them by itself
     if (threadIdx.x == 0) {
-      const float t = __builtin_amdgcn_exp2f(-top) - z;
+      const float t = -rest;
       store1(e + a.targets[all], t);
       a.rest[row] = f * (t - quant(t, static_cast<const T*>(nullptr)));
       a.term[row] = t;
