@@ -587,6 +587,8 @@ __device__ __forceinline__ void finish(const VocabGrad& g, long row, long col, i
     const float f = g.factor[row];
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] *= f;
+    // a row that takes no part: w may hold infinities or NaN, which zeros of e do not take out of a product
+    if (f == 0.f && (g.targets[row] < 0 || g.targets[row] >= g.b_inner)) v[0] = v[1] = v[2] = v[3] = 0.f;
     if constexpr (sizeof(T) == 2) {
       const float r = g.rest[row];
       if (r != 0.f) {
