@@ -108,10 +108,12 @@ struct VocabGrad {
   void* out;
   const float *factor, *rest;                // [rows], nullable together: factors, and those of b's lines `targets` beside the product
   const int32_t* targets;
-  // dw: where each column's target rows begin in `order` (nullable), the rows' terms of it, factors and x
+  // dw: where each column's target rows begin in `order` (nullable), the rows' terms of it, factors and x; and for columns of many
+  // what rounding left of these, a sum for each run of 2^run_bits rows
   const int *start, *order;
-  const float *term, *row_factor;
+  const float *term, *row_factor, *left;
   const void* x;
+  int run_bits;
   float *part, *acc;                         // the splits' sums; sums over the pieces of rows
   long rows, cols, inner, a_ld, a_free, b_inner, per_split;   // a_free: rows, or as many as a's lines have
   int splits, tile, row_tiles, col_tiles, add, last;
@@ -127,17 +129,18 @@ struct VocabArgs {
   int row_tiles, col_tiles, row_tile, col_tile;
   float scale, scale_log2;                   // scale_log2 = scale log2(e)
   // workspace: each row's reference; of a piece the tiles' sums, the references that differ and which tiles
-  // have them, e, factors, x times them, and what rounding the target's e left
-  float *ref, *sums, *shift, *mean, *factor, *rest, *term, *part, *acc;
+  // have them, e, factors, x times them, and what rounding the targets' terms left
+  float *ref, *sums, *shift, *mean, *factor, *rest, *term, *left, *part, *acc;
   int *slow, *start, *order;
   void *scaled, *e;
 };
 struct VocabPlan {
   long piece;
   bool lists;                                // rows by their targets, for dw
+  int run_bits;
   int row_tile, col_tile;                    // of the scores
   VocabGrad dx, dw;                          // tile, splits and per_split
-  size_t ref, sums, shift, slow, mean, factor, rest, term, start, order, scaled, e, part, acc, bytes;   // offsets in the workspace
+  size_t ref, sums, shift, slow, mean, factor, rest, term, start, order, left, scaled, e, part, acc, bytes;   // offsets in the workspace
 };
 
 // piece_rows: rows at a time (0: by the rule).

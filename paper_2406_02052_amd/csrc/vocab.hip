@@ -321,10 +321,79 @@ __device__ __forceinline__ float max16f(float v) {
   return over(v, Const<0x140>{});
 }
 
-// A row's reference, its target's score in binary logarithms, a wave a row of those at work.
+// The rows of a piece by their targets, those of one target in their own order: start[j] .. start[j + 1] of `order` are the rows with
+// target j.  A workgroup takes 256 columns and reads all targets twice, a quarter each wave: how many are below its columns
+// and at each of them, then where each row goes, wave after wave and a wave's rows in turn.
+__device__ __forceinline__ void list_rows(const VocabArgs& a, int base) {
+  __shared__ int count[4][256], below[4], sums[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int32_t* const targets = a.targets + a.row0;
+  const long part = (a.piece + 255) / 256 * 64, from = wave * part, to = from + part < a.piece ? from + part : a.piece;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) count[w][tid] = 0;
+  __syncthreads();
+  int less = 0;
+#pragma unroll 4
+  for (long i = from + lane; i < to; i += 64) {
+    const int t = targets[i], c = t - base;
+    if (t < 0 || t >= a.vocab) continue;
+    less += c < 0;
+    if (c >= 0 && c < 256) atomicAdd(&count[wave][c], 1);   // (whole numbers: their order changes nothing)
+  }
+  for (int d = 32; d > 0; d >>= 1) less += __shfl_xor(less, d, 64);
+  if (lane == 0) below[wave] = less;
+  __syncthreads();
+  const int n = count[0][tid] + count[1][tid] + count[2][tid] + count[3][tid];
+  int upto = n;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int v = __shfl_up(upto, d, 64);
+    if (lane >= d) upto += v;
+  }
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  int at = below[0] + below[1] + below[2] + below[3] + upto - n;
+  for (int w = 0; w < wave; ++w) at += sums[w];
+  if (base + tid < a.vocab) a.start[base + tid] = at;
+  if (base + tid == a.vocab - 1) a.start[a.vocab] = at + n;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {   // where the next row of this column goes, for each wave
+    const int v = count[w][tid];
+    count[w][tid] = at;
+    at += v;
+  }
+  __syncthreads();
+  int next = from + lane < to ? targets[from + lane] : -1;
+  for (long first = from; first < to; first += 64) {
+    const long i = first + lane;
+    const int t = next, c = t - base;
+    next = i + 64 < to ? targets[i + 64] : -1;
+    const bool in = t >= 0 && t < a.vocab && c >= 0 && c < 256;
+    // the lanes with the same column, by its bits: the first of them takes places for all, in the lanes' order
+    uint64_t same = __ballot(in);
+    if (same == 0) continue;
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+      const bool set = (c >> b & 1) != 0;
+      const uint64_t with = __ballot(set);
+      same &= set ? with : ~with;
+    }
+    const int leader = in ? __ffsll(static_cast<unsigned long long>(same)) - 1 : 0;
+    int place = 0;
+    if (in && lane == leader) place = atomicAdd(&count[wave][c], __popcll(same));
+    place = __shfl(place, leader, 64);
+    if (in) a.order[place + __popcll(same & ((uint64_t{1} << lane) - 1))] = static_cast<int>(i);
+  }
+}
+
+// A row's reference, its target's score in binary logarithms, a wave a row of those at work.  The first `lists` workgroups list the
+// rows by their targets: beside the others that takes no time of its own (7 us as a launch, at 2048 rows over 32768).
 template <typename T>
-__global__ __launch_bounds__(256) void vocab_target_kernel(VocabArgs a) {
-  const long of = static_cast<long>(blockIdx.x) * 4 + (threadIdx.x >> 6), row = a.row0 + of;
+__global__ __launch_bounds__(256) void vocab_target_kernel(VocabArgs a, int lists) {
+  if (static_cast<int>(blockIdx.x) < lists) {
+    list_rows(a, static_cast<int>(blockIdx.x) * 256);
+    return;
+  }
+  const long of = static_cast<long>(blockIdx.x - lists) * 4 + (threadIdx.x >> 6), row = a.row0 + of;
   const int lane = threadIdx.x & 63;
   if (of >= a.piece || !takes_part(a, row)) return;
   const int t = a.targets[row];
@@ -566,6 +635,21 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a) {
 // gradients
 // ---------------------------------------------------------------------------
 
+// Columns with up to FEW target rows are gone through where dw's sums leave, all rows on their way at once; of the others
+// there are sums of runs of rows, in lines of their own: a column whose rows are first .. last - 1 of the order has at least one place
+// there that is a multiple of FEW for each of its runs, and its runs' lines are those places' / FEW.
+constexpr int FEW = 4;
+__device__ __forceinline__ int line_of(int first) { return (first + FEW - 1) / FEW; }
+
+// What rounding left of 4 channels w of a row's term t x f: the product took round(t) round(f x).
+__device__ __forceinline__ void add_left(float t, float f, uint2 w, float (&v)[4]) {
+  const float q = quant(t, static_cast<const bf16_t*>(nullptr));
+  const float x[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                      __uint_as_float(w.y & 0xffff0000u)};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] += fmaf(f * t, x[e], -q * quant(f * x[e], static_cast<const bf16_t*>(nullptr)));
+}
+
 // Where a gradient's sums go: times the row's factor, with what is left of its target's term, added to what earlier pieces gave, and on to the tensor or to the sums
 // for the next piece.
 // dw's result row is a column of the vocabulary, whose target rows are order[first .. last).
@@ -573,14 +657,32 @@ template <typename T>
 __device__ __forceinline__ void finish(const VocabGrad& g, long row, long col, int first, int last, float (&v)[4]) {
   const long at = row * g.cols + col;
   if constexpr (sizeof(T) == 2) {
-    for (int k = first; k < last; ++k) {
-      const long i = g.order[k];
-      const float f = g.row_factor[i], t = g.term[i], q = quant(t, static_cast<const T*>(nullptr));
-      const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const T*>(g.x) + i * g.cols + col);
-      const float x[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
-                          __uint_as_float(w.y & 0xffff0000u)};
+    if (last - first > FEW) {
+      const float* const left = g.left + static_cast<long>(line_of(first)) * g.cols + col;
+      const int runs = (last - first + (1 << g.run_bits) - 1) >> g.run_bits;
+      for (int k = 0; k < runs; k += 4) {
+        float4 q[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += fmaf(f * t, x[e], -q * quant(f * x[e], static_cast<const T*>(nullptr)));
+        for (int u = 0; u < 4; ++u) q[u] = *reinterpret_cast<const float4*>(left + static_cast<long>(k + u < runs ? k + u : k) * g.cols);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (k + u < runs) v[0] += q[u].x, v[1] += q[u].y, v[2] += q[u].z, v[3] += q[u].w;
+      }
+    } else if (first < last) {
+      int row_of[FEW];
+      float f[FEW], t[FEW];
+      uint2 x[FEW];
+#pragma unroll
+      for (int u = 0; u < FEW; ++u) row_of[u] = g.order[first + u < last ? first + u : first];
+#pragma unroll
+      for (int u = 0; u < FEW; ++u) {
+        f[u] = g.row_factor[row_of[u]];
+        t[u] = g.term[row_of[u]];
+        x[u] = *reinterpret_cast<const uint2*>(static_cast<const T*>(g.x) + row_of[u] * g.cols + col);
+      }
+#pragma unroll
+      for (int u = 0; u < FEW; ++u)
+        if (first + u < last) add_left(t[u], f[u], x[u], v);
     }
   }
   if (g.factor != nullptr) {
@@ -670,56 +772,36 @@ __global__ __launch_bounds__(P::THREADS, 2) void vocab_grad_kernel(VocabGrad g) 
   }
 }
 
-// The rows of a piece by their targets, those of one target in their own order: start[j] .. start[j + 1] of `order` are the rows with
-// target j.  A workgroup takes 256 columns and reads all targets twice, a quarter each wave: how many are below its columns
-// and at each of them, then where each row goes, wave after wave and a wave's rows one by one: 2048 rows over 32768 in 7 us.
-__global__ __launch_bounds__(256) void vocab_lists_kernel(VocabArgs a) {
-  __shared__ int count[4][256], below[4], sums[4];
-  const int base = blockIdx.x * 256, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int32_t* const targets = a.targets + a.row0;
-  const long part = (a.piece + 255) / 256 * 64, from = wave * part, to = from + part < a.piece ? from + part : a.piece;
+// What rounding left of the targets' terms of dw for columns of more than FEW target rows: a wave a run of 2^run_bits of a
+// column's rows and 256 channels, its rows on their way four at a time.  So the time goes by all rows and not by how many
+// have one target: 2048 x 1024 over 32768 with one for all took 1.53 ms when dw's epilogue went through whole lists.
+__global__ __launch_bounds__(256) void vocab_left_kernel(VocabArgs a, int run_bits) {
+  const int lane = threadIdx.x & 63, parts = (a.width + 255) / 256;
+  const long id = static_cast<long>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int line = static_cast<int>(id / parts), col = static_cast<int>(id % parts) * 256 + lane * 4;
+  if (line * FEW >= a.start[a.vocab]) return;
+  // whose line it is, and of which run
+  const int target = a.targets[a.row0 + a.order[line * FEW]], first = a.start[target], last = a.start[target + 1];
+  const int from = first + ((line - line_of(first)) << run_bits), to = from + (1 << run_bits) < last ? from + (1 << run_bits) : last;
+  if (last - first <= FEW || from >= last || col >= a.width) return;
+  float v[4] = {};
+  for (int k = from; k < to; k += 4) {
+    int row[4];
+    float f[4], t[4];
+    uint2 x[4];
 #pragma unroll
-  for (int w = 0; w < 4; ++w) count[w][tid] = 0;
-  __syncthreads();
-  int less = 0;
-#pragma unroll 4
-  for (long i = from + lane; i < to; i += 64) {
-    const int t = targets[i], c = t - base;
-    if (t < 0 || t >= a.vocab) continue;
-    less += c < 0;
-    if (c >= 0 && c < 256) atomicAdd(&count[wave][c], 1);   // (whole numbers: their order changes nothing)
-  }
-  for (int d = 32; d > 0; d >>= 1) less += __shfl_xor(less, d, 64);
-  if (lane == 0) below[wave] = less;
-  __syncthreads();
-  const int n = count[0][tid] + count[1][tid] + count[2][tid] + count[3][tid];
-  int upto = n;
-  for (int d = 1; d < 64; d <<= 1) {
-    const int v = __shfl_up(upto, d, 64);
-    if (lane >= d) upto += v;
-  }
-  if (lane == 63) sums[wave] = upto;
-  __syncthreads();
-  int at = below[0] + below[1] + below[2] + below[3] + upto - n;
-  for (int w = 0; w < wave; ++w) at += sums[w];
-  if (base + tid < a.vocab) a.start[base + tid] = at;
-  if (base + tid == a.vocab - 1) a.start[a.vocab] = at + n;
+    for (int u = 0; u < 4; ++u) row[u] = a.order[k + u < to ? k + u : k];
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {   // where the next row of this column goes, for each wave
-    const int v = count[w][tid];
-    count[w][tid] = at;
-    at += v;
+    for (int u = 0; u < 4; ++u) {
+      f[u] = a.factor[row[u]];
+      t[u] = a.term[row[u]];
+      x[u] = *reinterpret_cast<const uint2*>(static_cast<const bf16_t*>(a.x) + (a.row0 + row[u]) * a.width + col);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (k + u < to) add_left(t[u], f[u], x[u], v);
   }
-  __syncthreads();
-  int next = from + lane < to ? targets[from + lane] : -1;
-  for (long first = from; first < to; first += 64) {
-    const long i = first + lane;
-    const int t = next, c = t - base;
-    next = i + 64 < to ? targets[i + 64] : -1;
-    for (uint64_t left = __ballot(t >= 0 && t < a.vocab && c >= 0 && c < 256); left != 0; left &= left - 1)
-      if (lane == __ffsll(static_cast<unsigned long long>(left)) - 1)   // (one at a time)
-        a.order[atomicAdd(&count[wave][c], 1)] = static_cast<int>(i);
-  }
+  *reinterpret_cast<float4*>(a.left + static_cast<long>(line) * a.width + col) = make_float4(v[0], v[1], v[2], v[3]);
 }
 
 // Adds the splits' sums, 4 columns a thread.
@@ -828,7 +910,8 @@ void run(const VocabArgs& all, const VocabPlan& p, bool gradients, hipStream_t s
   for (a.row0 = 0; a.row0 < a.rows; a.row0 += p.piece) {
     a.piece = a.rows - a.row0 < p.piece ? a.rows - a.row0 : p.piece;
     a.row_tiles = static_cast<int>(up(a.piece, a.row_tile));
-    vocab_target_kernel<T><<<static_cast<unsigned>(up(a.piece, 4)), 256, 0, s>>>(a);
+    const int lists = p.lists ? static_cast<int>(up(a.vocab, 256)) : 0;
+    vocab_target_kernel<T><<<static_cast<unsigned>(lists + up(a.piece, 4)), 256, 0, s>>>(a, lists);
     scores<T>(a, gradients, s);
     const unsigned n = static_cast<unsigned>(a.piece);
     if (!gradients) {
@@ -843,8 +926,9 @@ void run(const VocabArgs& all, const VocabPlan& p, bool gradients, hipStream_t s
     w.a = a.e, w.b = a.scaled, w.a_ld = w.a_free = a.vocab_padded, w.b_inner = a.piece, w.rows = a.vocab, w.cols = a.width, w.inner = a.piece;
     w.out = a.dw, w.part = a.part, w.acc = a.acc, w.add = a.row0 > 0, w.last = a.row0 + a.piece == a.rows;
     if (p.lists) {
-      vocab_lists_kernel<<<static_cast<unsigned>(up(a.vocab, 256)), 256, 0, s>>>(a);
-      w.start = a.start, w.order = a.order, w.term = a.term, w.row_factor = a.factor;
+      const long waves = up(a.piece, FEW) * up(a.width, 256);
+      vocab_left_kernel<<<static_cast<unsigned>(up(waves, 4)), 256, 0, s>>>(a, p.run_bits);
+      w.start = a.start, w.order = a.order, w.term = a.term, w.row_factor = a.factor, w.left = a.left, w.run_bits = p.run_bits;
       w.x = static_cast<const T*>(a.x) + a.row0 * a.width;
     }
     if (w.per_split >= w.inner) w.splits = 1;   // a last, smaller piece
@@ -891,8 +975,13 @@ VocabPlan vocab_plan(const VocabArgs& a, int dtype, bool gradients, long piece_r
     p.factor = take(static_cast<size_t>(p.piece) * 4);
     p.rest = take(static_cast<size_t>(p.piece) * 4);
     p.term = take(static_cast<size_t>(p.piece) * 4);
-    // fp32 has no rounding to take back; and lists of many rows a column would be gone through by one thread each
+    // fp32 has no rounding to take back; and where many rows share few columns, and few workgroups list them, that would take as
+    // long as the products
     p.lists = esz == 2 && p.piece <= 65536 && p.piece <= 16L * a.vocab;
+    // runs of 16 rows, and of more where a column of all rows would have over 256; their sums where the tiles' have been, if they fit
+    for (p.run_bits = 4; p.piece > 256L << p.run_bits; ++p.run_bits) {}
+    const size_t left = p.lists ? static_cast<size_t>(up(p.piece, FEW)) * a.width * 4 : 0;
+    p.left = left <= p.mean - p.sums ? p.sums : take(left);
     p.start = take(p.lists ? (static_cast<size_t>(a.vocab) + 1) * 4 : 0);
     p.order = take(p.lists ? static_cast<size_t>(p.piece) * 4 : 0);
     p.scaled = take(static_cast<size_t>(p.piece) * a.width * esz);
@@ -926,6 +1015,7 @@ void vocab_run(VocabArgs a, const VocabPlan& p, int dtype, bool gradients, void*
     a.term = reinterpret_cast<float*>(ws + p.term);
     a.start = reinterpret_cast<int*>(ws + p.start);
     a.order = reinterpret_cast<int*>(ws + p.order);
+    a.left = reinterpret_cast<float*>(ws + p.left);
     a.scaled = ws + p.scaled;
     a.e = ws + p.e;
     a.part = reinterpret_cast<float*>(ws + p.part);
