@@ -544,7 +544,8 @@ petra_status petra_dropout(int64_t n, int32_t dtype, float p, float alpha, const
  * no pair are not rotated.  n is over the head's channels, as in petra_coupling_desc, with one
  * gamma (and beta, nullable) [head_dim] for all query heads and one for all key heads; without
  * (NULL) n(x) = x.  With several axes (time, height and width of images, say) a pair
- * turns by the position on its own.  Angles are exact to 2^-32 of a turn for every position.
+ * turns by the position on its own.  Angles are within 2^-31 of a turn for every position and finite
+ * frequency.
  *
  * Layout: q [batch][len][heads][head_dim], k [batch][len][kv_heads][head_dim] with the given
  * strides as in petra_attn_desc, the results likewise (all three zero: contiguous).  kv_heads = 0:

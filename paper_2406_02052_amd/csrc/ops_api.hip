@@ -3,6 +3,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <cstring>
+#include <iterator>
 #include <string>
 #include <vector>
 
@@ -609,19 +611,34 @@ namespace {
 
 static_assert(petra::HEADS_AXES == PETRA_HEAD_AXES && petra::HEADS_PAIRS == PETRA_HEAD_PAIRS, "the header's limits");
 
-// The fraction of a turn that `radians` are, in 64 bits; a whole one wraps.  (Without the library's floorl and roundl, which take
-// longer than all else that a call does on the host.)
+// The binary digits of 1 / 2 pi, from the one of 2^-1 on: by 2 pi = 8 (4 arctan 1/5 - arctan 1/239) in whole numbers.
+constexpr uint64_t TURN[19] = {
+    0x28be60db9391054a, 0x7f09d5f47d4d3770, 0x36d8a5664f10e410, 0x7f9458eaf7aef158,
+    0x6dc91b8e909374b8, 0x01924bba82746487, 0x3f877ac72c4a69cf, 0xba208d7d4baed121,
+    0x3a671c09ad17df90, 0x4e64758e60d4ce7d, 0x272117e2ef7e4a0e, 0xc7fe25fff7816603,
+    0xfbcbc462d6829b47, 0xdb4d9fb3c9f2c26d, 0xd3d18fd9a797fa8b, 0x5d49eeb1faf97c5e,
+    0xcf41ce7de294a4ba, 0x9afed7ec47e35742, 0x1580cc11bf1edaea};
+
+// 128 digits of 1 / 2 pi that begin with the one of 2^-(at + 1); before the first they are zeros.
+unsigned __int128 turn_digits(int at) {
+  auto word = [](int i) { return i < 0 || i >= static_cast<int>(std::size(TURN)) ? uint64_t{0} : TURN[i]; };
+  const int first = at >> 6, by = at & 63;   // (rounded down)
+  const uint64_t a = word(first), b = word(first + 1), c = word(first + 2);
+  const uint64_t hi = by == 0 ? a : a << by | b >> (64 - by), lo = by == 0 ? b : b << by | c >> (64 - by);
+  return static_cast<unsigned __int128>(hi) << 64 | lo;
+}
+
+// The fraction of a turn that finite `radians` are, in 64 bits, to the nearest; a whole one wraps.  radians = m 2^e with a whole m
+// below 2^53: digits of 1 / 2 pi before the e-th give whole turns, and those past the next 128 less than 2^-75 of one.  (The bits
+// are taken apart here: library calls for it take longer than all else that a call does on the host.)
 uint64_t turn_fraction(double radians) {
-  long double f = static_cast<long double>(radians) * 0.159154943091895335768883763372514362L;   // 1 / 2 pi
-  if (f < 4.6e18L && f > -4.6e18L) {
-    const auto whole = static_cast<int64_t>(f);
-    f -= static_cast<long double>(whole);
-  } else {
-    f = fmodl(f, 1.0L);
-  }
-  if (f < 0.0L) f += 1.0L;
-  f = f * 18446744073709551616.0L + 0.5L;
-  return f >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(f);
+  uint64_t bits;
+  std::memcpy(&bits, &radians, 8);
+  const int e = static_cast<int>(bits >> 52 & 0x7ff);
+  const uint64_t m = (bits & 0xfffffffffffffULL) | (e > 0 ? uint64_t{1} << 52 : 0);
+  const unsigned __int128 f = turn_digits((e > 0 ? e : 1) - 1075) * m + (uint64_t{1} << 63);
+  const auto u = static_cast<uint64_t>(f >> 64);
+  return radians < 0. ? 0 - u : u;
 }
 
 struct Heads {
