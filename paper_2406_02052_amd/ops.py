@@ -53,6 +53,7 @@ class _Owner:
 
     def _on(self, stream) -> int:
         """The stream's handle; tells the allocator of a stream that is new to the workspace."""
+        self._need_stream(stream)
         handle = L._stream(stream)
         if handle not in self.streams and not isinstance(stream, int):
             import torch
@@ -60,6 +61,14 @@ class _Owner:
                 t.record_stream(torch.cuda.current_stream() if stream is None else stream)
             self.streams.add(handle)
         return handle
+
+    def _need_stream(self, stream) -> None:
+        """A stream that is given is one of the owner's device.  (Its handle does not tell: that of
+        the default stream is the same for every device.)"""
+        index = self.workspace.get_device()
+        if getattr(stream, "device_index", index) != index:
+            raise ValueError(f"need a stream of the owner's device {self.workspace.device}, "
+                             f"got {stream}")
 
     def _owned(self):
         """The owner's memory that its calls use."""
@@ -186,6 +195,7 @@ class Coupling(_Owner):
         """Writes y and, with pre, u.  Without f only u = n(x; pre)."""
         self._check((("x", x), ("f", f), ("y", y), ("u", u)), (("gate", gate),),
                     (("post", post), ("pre", pre)), rng)
+        self._need_stream(stream)
         L.petra_coupling_forward(self.desc, x, f, gate, post, pre, rng, y, u, stream)
 
     def backward(self, y, f, dy, gate, post, x, dx, df, dgate, dpost, du=None, pre=None,
@@ -308,6 +318,7 @@ class HeadNorm(_Owner):
     def forward(self, q, k, yq, yk, q_norm=None, k_norm=None, positions=None, stream=None) -> None:
         """Writes yq and yk.  q_norm and k_norm: (gamma, beta or None), fp32; positions: int32
         [axes, batch, length] (None: a token's index)."""
+        self._need_stream(stream)
         self._need_norms(q_norm, k_norm)
         self._lay(False, (q, k, yq, yk), (q_norm or _NONE) + (k_norm or _NONE), positions)
         L.petra_heads_forward(self.desc, q, k, q_norm, k_norm, positions, yq, yk, stream)
