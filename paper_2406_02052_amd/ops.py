@@ -385,12 +385,18 @@ class VocabLoss(_Owner):
 
 class AdamW(_Owner):
     """An AdamW step over many tensors: params (fp32) and their grads (fp32 or bf16, all of one
-    type), which the owner keeps and whose memory stays theirs.
+    type), which the owner keeps.
+
+    A step works on the memory that the tensors had when the owner was made, and the owner keeps
+    that.  It does not follow a tensor that is given other memory (`p.data = ...`): each step
+    looks at 8 of the tensors in turn and refuses one that has moved, now and from then on.  m,
+    v and their scales are copied into, not replaced.  Storage that is resized away under the
+    owner is not seen in time.
 
     states: 'fp32', or 'fp8' for 8 bits an element.  m and v (fp8: r = sqrt(v), as
     float8_e4m3fn, with m_scale and v_scale for each 64 elements) are one tensor each for all, each
     parameter's from a multiple of 64 on: m[starts[i]:starts[i] + n].  lr (fp32) and steps
-    (int64) are device tensors of one element, for the caller to set.  weight_decay: one for all, or
+    (int64) are device tensors of one element, for the caller to set or replace.  weight_decay: one for all, or
     one for each.  copies: bf16 tensors that follow their parameters (None: none).  zero_grads: each
     step sets the gradients to 0."""
 
@@ -433,7 +439,7 @@ class AdamW(_Owner):
                                       if fp8 else (None, None))
         self.lr = torch.full((1,), lr, device=device)
         self.steps = torch.zeros(1, dtype=torch.int64, device=device)
-        self.fp8, self.ftype = fp8, torch.float32
+        self.fp8, self.ftype, self.itype = fp8, torch.float32, torch.int64
         self.desc = L.AdamwDesc(betas[0], betas[1], eps,
                                 L.PETRA_BF16 if gtype is torch.bfloat16 else L.PETRA_FP32,
                                 L.PETRA_E4M3 if fp8 else L.PETRA_FP32, int(zero_grads))
@@ -454,11 +460,37 @@ class AdamW(_Owner):
         table = torch.empty(max(self.table_bytes, 1), dtype=torch.uint8)
         L.petra_adamw_layout(self.desc, tensors, self.count, table, self.table_bytes)
         self.table = table.to(device)
+        self._keep()
         self._own(ws_bytes, device)
 
+    def _keep(self) -> None:
+        """What the table points to, whatever becomes of the caller's tensors: (name, the tensor,
+        one of the same memory, its address) of each, and the states."""
+        self._laid = [(f"{name}[{i}]", t, t.detach(), t.data_ptr())
+                      for name, of in (("params", self.params), ("grads", self.grads),
+                                       ("copies", self.copies))
+                      for i, t in enumerate(of) if t is not None]
+        self._states = self.m, self.v, self.m_scale, self.v_scale
+        self._state_memory = [t.detach() for t in self._states if t is not None]
+        self._turn, self._set = 0, (self.lr, self.steps)
+
+    def _need_laid(self) -> None:
+        """The table's memory is still the tensors': of the states, and of the next of the others (an
+        address takes 0.1 us to ask for, all of 300 tensors would take longer than their step)."""
+        m, v, m_scale, v_scale = self._states
+        if not (self.m is m and self.v is v and self.m_scale is m_scale and self.v_scale is v_scale):
+            name = next(n for n, t in zip(("m", "v", "m_scale", "v_scale"), self._states)
+                        if getattr(self, n) is not t)
+            raise ValueError(f"{name}: has been replaced, copy into it instead")
+        turn = self._turn
+        for name, t, _, at in self._laid[turn:turn + 8]:
+            if t.data_ptr() != at:
+                raise ValueError(f"{name}: its memory is not what was laid out, make a new owner")
+        self._turn = turn + 8 if turn + 8 < len(self._laid) else 0
+
     def _owned(self):
-        return [t for t in (self.workspace, self.table, self.m, self.v, self.m_scale,
-                            self.v_scale, self.lr, self.steps) if t is not None]
+        return [self.workspace, self.table, self.lr, self.steps, *self._state_memory,
+                *(laid[2] for laid in self._laid)]
 
     def step(self, rng=None, grad_scale=None, stream=None) -> None:
         """Updates params, copies and states; rng (device int64 [seed, offset], for fp8): another
@@ -468,7 +500,12 @@ class AdamW(_Owner):
         if grad_scale is not None:
             _need(grad_scale, "grad_scale", self.ftype, (1,))
         _need(self.lr, "lr", self.ftype, (1,))
-        self._need_here(rng, grad_scale, self.lr)
+        _need(self.steps, "steps", self.itype, (1,))
+        self._need_here(rng, grad_scale, self.lr, self.steps)
+        self._need_laid()
+        if self.lr is not self._set[0] or self.steps is not self._set[1]:
+            self.streams.clear()   # (tells the allocator of them)
+            self._set = (self.lr, self.steps)
         L.petra_adamw_step(self.desc, self.table, self.table_bytes, self.count, self.chunks,
                            self.steps, self.lr, grad_scale, rng, self.workspace, self.ws_bytes,
                            self._on(stream))

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_2406_02052_amd import Attention, Coupling, HeadNorm, VocabLoss
+from paper_2406_02052_amd import AdamW, Attention, Coupling, HeadNorm, VocabLoss
 from paper_2406_02052_amd.ops import _Owner
 
 
@@ -35,3 +35,57 @@ def test_owners_have_streams_of_their_own():
         assert op.streams == set()   # (on no device there are none)
         with pytest.raises(ValueError, match="stream of the owner's device"):
             op._on(Stream(0))
+
+
+def adamw(count, copies=False):
+    """An owner of tensors on the host, as it is once they are laid out."""
+    op = AdamW.__new__(AdamW)
+    op.params, op.grads = ([torch.zeros(5 + i) for i in range(count)] for _ in range(2))
+    op.copies = [torch.zeros(5 + i, dtype=torch.bfloat16) if copies else None for i in range(count)]
+    op.m, op.v, op.m_scale, op.v_scale = torch.zeros(64), torch.zeros(64), None, None
+    op.lr, op.steps = torch.zeros(1), torch.zeros(1, dtype=torch.int64)
+    op.workspace, op.table = torch.empty(4), torch.empty(4)
+    op._keep()
+    return op
+
+
+@pytest.mark.parametrize("what", ["params", "grads", "copies"])
+@pytest.mark.parametrize("count,at", [(1, 0), (5, 4), (40, 33)])
+def test_adamw_refuses_tensors_of_other_memory(count, at, what):
+    """In the turn of the one that moved, and from then on; what was laid out stays as long as the owner."""
+    op = adamw(count, copies=True)
+    turns = -(-3 * count // 8)
+    for _ in range(2 * turns):
+        op._need_laid()
+    t = getattr(op, what)[at]
+    t.fill_(3.0)
+    old = t.data_ptr()
+    t.data = torch.zeros_like(t)
+    kept = [x for x in op._owned() if x.data_ptr() == old]
+    assert len(kept) == 1 and (kept[0] == 3).all()
+    passed = 0
+    with pytest.raises(ValueError, match=rf"{what}\[{at}\]: its memory"):
+        for passed in range(turns + 1):
+            op._need_laid()
+    assert passed <= turns
+    for _ in range(3):
+        with pytest.raises(ValueError, match="its memory"):
+            op._need_laid()
+
+
+def test_adamw_refuses_replaced_states():
+    for name in ("m", "v", "m_scale"):
+        op = adamw(2)
+        op._need_laid()
+        setattr(op, name, torch.zeros(64))
+        with pytest.raises(ValueError, match=f"{name}: has been replaced"):
+            op._need_laid()
+        assert sum(t.numel() == 64 for t in op._owned()) == 2   # the memory of those laid out stays
+
+
+def test_adamw_without_elements():
+    op = adamw(1)
+    op.params, op.grads = [torch.empty(0)], [torch.empty(0)]
+    op._keep()
+    for _ in range(3):
+        op._need_laid()
