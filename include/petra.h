@@ -659,7 +659,7 @@ typedef struct {
 
 typedef struct {
   double beta1, beta2;        /* in [0, 1) */
-  float eps;                  /* > 0 */
+  float eps;                  /* at least 2^-126 */
   int32_t grad_dtype;         /* PETRA_FP32 or PETRA_BF16 */
   int32_t state_dtype;        /* PETRA_FP32 or PETRA_E4M3 */
   int32_t zero_grads;         /* gradients are set to 0 as they are read */

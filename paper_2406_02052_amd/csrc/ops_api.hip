@@ -5,6 +5,7 @@
 #include <cstdint>
 #include <cstring>
 #include <iterator>
+#include <limits>
 #include <string>
 #include <vector>
 
@@ -977,7 +978,8 @@ size_t adamw_bytes(int64_t count, int64_t chunks) {
 void need_adamw(const petra_adamw_desc* d) {
   need(d != nullptr, PETRA_ERR_INVALID_ARG, "null description");
   need(d->beta1 >= 0. && d->beta1 < 1. && d->beta2 >= 0. && d->beta2 < 1., PETRA_ERR_INVALID_ARG, "betas outside [0, 1)");
-  need(d->eps > 0.f && std::isfinite(d->eps), PETRA_ERR_INVALID_ARG, "eps must be positive and finite");
+  // (of less the reciprocal is infinite, and a state of 0 times it NaN)
+  need(d->eps >= std::numeric_limits<float>::min() && std::isfinite(d->eps), PETRA_ERR_INVALID_ARG, "eps must be at least 2^-126 and finite");
   need_dtype(d->grad_dtype);
   need(d->state_dtype == PETRA_FP32 || d->state_dtype == PETRA_E4M3, PETRA_ERR_DTYPE, "states must be fp32 or e4m3");
 }

@@ -63,3 +63,11 @@ def test_adamw_with_replaced_lr_and_steps_on_another_stream():
         want = 0.5 - 0.25 * 0.19 / (1 - 0.9 ** 10) / math.sqrt(0.001999 / (1 - 0.999 ** 10))
         assert steps == 10 and ((theta - want).abs() < 1e-6).all()
         del junk
+
+
+@pytest.mark.parametrize("states", ["fp32", "fp8"])
+def test_adamw_least_eps_leaves_parameters_without_gradients(states):
+    op, theta, grad = owner(states=states, eps=2.0 ** -126)
+    grad[:100] = 0.0
+    op.step(rng=torch.tensor([1, 2], device="cuda"))
+    assert (theta[:100] == 1).all() and ((theta[100:] - 0.5).abs() < 1e-6).all()
