@@ -604,7 +604,7 @@ petra_status petra_heads_backward(const petra_heads_desc* desc, const void* q, c
  * make most of them: dx and dw are off by 1.0 to 1.1 times what rounding them alone to bf16 would give (dw, in pieces of more
  * than 16 rows a column or 65536 rows, by up to 1.75 times).
  * x, dx [rows][width] and w, dw [vocab][width] are contiguous, targets int32 [rows].
- * Limits: width a multiple of 8, at most 65536; 1 <= vocab <= 2^20; rows at most 2^30; scale > 0. */
+ * Limits: width a multiple of 8, at most 65536; 1 <= vocab <= 2^20; rows at most 2^30; 0 < scale < 2^127. */
 typedef struct {
   int64_t rows;
   int64_t piece_rows;

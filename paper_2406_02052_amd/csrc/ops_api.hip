@@ -873,7 +873,8 @@ struct Vocab {
     need(d->width >= 8 && d->width <= 65536 && d->width % 8 == 0, PETRA_ERR_SHAPE,
          "width must be a multiple of 8, at most 65536");
     need(d->vocab >= 1 && d->vocab <= (1 << 20), PETRA_ERR_SHAPE, "vocab must be 1 .. 2^20");
-    need(d->scale > 0.f && std::isfinite(d->scale), PETRA_ERR_INVALID_ARG, "scale must be positive and finite");
+    // (2^127 and more pass fp32 with log2(e), and times a score of 0 are NaN)
+    need(d->scale > 0.f && d->scale < 0x1p127f, PETRA_ERR_INVALID_ARG, "scale must be positive and below 2^127");
     a.rows = d->rows;
     a.width = d->width;
     a.vocab = d->vocab;

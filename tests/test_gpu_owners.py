@@ -71,3 +71,12 @@ def test_adamw_least_eps_leaves_parameters_without_gradients(states):
     grad[:100] = 0.0
     op.step(rng=torch.tensor([1, 2], device="cuda"))
     assert (theta[:100] == 1).all() and ((theta[100:] - 0.5).abs() < 1e-6).all()
+
+
+def test_vocab_largest_scale():
+    from paper_2406_02052_amd import VocabLoss
+
+    x, w, t = torch.zeros(4, 8, device="cuda"), torch.ones(5, 8, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    loss, lse, dx, dw = torch.empty(4, device="cuda"), torch.empty(4, device="cuda"), torch.empty_like(x), torch.empty_like(w)
+    VocabLoss(4, 8, 5, "fp32", scale=2.0 ** 126).gradient(x, w, t, loss, lse, dx, dw)
+    assert ((loss - math.log(5)).abs() < 1e-6).all() and torch.isfinite(dx).all()

@@ -101,3 +101,14 @@ def test_adamw_eps_has_a_finite_reciprocal():
         else:
             with pytest.raises(L.PetraError, match="eps"):
                 L.petra_adamw_query(desc, None, 0)
+
+
+def test_vocab_scale_is_finite_with_its_logarithm():
+    from paper_2406_02052_amd import _lib as L
+
+    for scale, ok in ((2.0 ** 126, True), (2.0 ** 127, False), (3e38, False), (1e-44, True)):
+        if ok:
+            VocabLoss(4, 8, 8, scale=scale, device="cpu")
+        else:
+            with pytest.raises(L.PetraError, match="scale"):
+                VocabLoss(4, 8, 8, scale=scale, device="cpu")
