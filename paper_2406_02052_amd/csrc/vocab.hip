@@ -592,7 +592,9 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a) {
   __syncthreads();
   // of the others and the target, with 2^top as the unit (own: NaN where the target's score is no finite number)
   const float rest = lds[4] + lds[5] + lds[6] + lds[7], own = __builtin_amdgcn_exp2f(ref - ref - top), z = own + rest;
-  const float loss = top > 0.f ? LN2 * (top + log2f(z)) : log1pf(rest / own);
+  // log(1 + rest) = log(z) rest / (z - 1) with the rounded z in all places: what rounding 1 + rest lost goes out again
+  const float by = z - own, log_z = LN2 * (top + log2f(z));
+  const float loss = top > 0.f ? log_z : by == 0.f ? rest : log_z * (rest * __builtin_amdgcn_rcpf(by));
   if (threadIdx.x == 0) {
     a.loss[all] = loss;
     a.lse[all] = fmaf(LN2, ref, loss);

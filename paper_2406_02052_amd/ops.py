@@ -396,7 +396,7 @@ class AdamW(_Owner):
     states: 'fp32', or 'fp8' for 8 bits an element.  m and v (fp8: r = sqrt(v), as
     float8_e4m3fn, with m_scale and v_scale for each 64 elements) are one tensor each for all, each
     parameter's from a multiple of 64 on: m[starts[i]:starts[i] + n].  lr (fp32) and steps
-    (int64) are device tensors of one element, for the caller to set or replace.  weight_decay: one for all, or
+    (int64) are device tensors of one element, for the caller to set.  weight_decay: one for all, or
     one for each.  copies: bf16 tensors that follow their parameters (None: none).  zero_grads: each
     step sets the gradients to 0."""
 

@@ -104,3 +104,15 @@ def test_vocab_target_scores_that_are_no_numbers(where, dtype):
             v[t[11], 5] = bad
         _, alone = run_vocab(y, v, t, dtype)
         assert not torch.isfinite(alone[0][11]) and not torch.isfinite(alone[1][11])
+
+
+def test_vocab_loss_of_known_scores():
+    """Two columns with scores of 0 and -c: log(1 + e^-c), from c = 0 to where it leaves fp32's normal numbers.  The scale by log2(e) is off
+    by 2^-24 of c in its factor and its product each, and power, logarithm, quotient and their products by 2^-23 each."""
+    c = host(torch.linspace(0.0, 86.0, 777))
+    x, w = np.zeros((777, 8)), np.zeros((2, 8))
+    x[:, 0], w[1, 0] = -c, 1.0
+    _, alone = run_vocab(x, w, np.zeros(777, int), "fp32")
+    want = np.log1p(np.exp(-c))
+    off = np.abs(host(alone[0]) - want) / want
+    assert (off <= 2.0 ** -23 * (c + 8)).all(), (off / (c + 8)).max() * 2 ** 23
