@@ -599,10 +599,13 @@ petra_status petra_heads_backward(const petra_heads_desc* desc, const void* q, c
  * dx are 0.  weight: device fp32 [rows]; NULL: the mean, 1 / (the rows that take part).
  *
  * Rows are worked on in pieces (piece_rows at a time; 0: as many as keep a piece's scores within 1 GiB), whose
- * gradients of w are summed in fp32.  Scores, statistics and sums are fp32.  With bf16 tensors the softmax
- * and the weighted rows are rounded to bf16 as operands of the gradients' products, but for the targets' terms, which
- * make most of them: dx and dw are off by 1.0 to 1.1 times what rounding them alone to bf16 would give (dw, in pieces of more
- * than 16 rows a column or 65536 rows, by up to 1.75 times).
+ * gradients of w are summed in fp32.  Scores, statistics and sums are fp32, and a loss is log(1 + R) of the others'
+ * sum R, so that rows whose target has nearly all of the softmax keep theirs.  With bf16 tensors each term of dx is rounded to
+ * bf16 once before the sums (2^-8 of it at most) and each of dw twice; once more in rows with a loss of 59 or more.  The
+ * targets' terms are not (in dw: unless a piece has more than 16 rows a column, or 65536 rows).  Measured against what
+ * rounding the results to bf16 alone gives: dx and the rows of dw whose columns are targets are off by 1.0 to 1.1 times that (over
+ * a vocabulary of 2, where the other terms are as large, by 1.2 and 1.5), the other rows of dw, which have only rounded terms,
+ * by 1.6 times in the median and 3 at most.
  * x, dx [rows][width] and w, dw [vocab][width] are contiguous, targets int32 [rows].
  * Limits: width a multiple of 8, at most 65536; 1 <= vocab <= 2^20; rows at most 2^30; 0 < scale < 2^127. */
 typedef struct {

@@ -21,7 +21,7 @@
 //
 // Scores, sums, statistics and accumulators are fp32.  p and ds are rounded to the
 // storage type as operands of the products (the matrix unit takes bf16): an error of
-// each term of 2^-9 at most, as of the result's own rounding.
+// each term of 2^-8 at most, as of the result's own rounding.
 #include "common.h"
 #include "ops.h"
 #include "philox.h"

@@ -511,7 +511,9 @@ void by_shape(const HeadsArgs& a, bool backward, hipStream_t s) {
 
 void heads_plan(HeadsArgs& a, bool backward) {
   const int teams = 64 / lanes(a);
-  // workgroups of both parts together: as many as the chip holds at once
+  // workgroups of both parts together: as many as CUs would hold with 8 each forward and 4 or 5 backward.  By their registers they hold
+  // 4 to 6 of the forwards of 8 channels a chunk (8 of those of 4), which so take up to two turns, 4 to 7 of the rms
+  // backwards, and 3 to 6 of those with a layer norm or a beta (fp32 of 8 channels 2 or 3, up to two turns)
   const long most = 256 * (!backward ? 8 : chunk(a) == 8 ? 4 : 5);
   long units = 0, want[2] = {}, all[2] = {};
   for (int i = 0; i < 2; ++i) {
@@ -524,7 +526,7 @@ void heads_plan(HeadsArgs& a, bool backward) {
     want[i] = (a.tokens + tokens - 1) / tokens;
     units += want[i] * all[i];
   }
-  // rounds a workgroup: the fewest by which no workgroup is left for a second turn (16384 tokens, 16 + 4 heads of 128: 10 give 1025
+  // rounds a workgroup: the fewest by which there are no more workgroups than that (16384 tokens, 16 + 4 heads of 128: 10 give 1025
   // workgroups and take 73 us backward, 11 give 870)
   for (long each = (units + most - 1) / most, total = most + 1; total > most; ++each) {
     total = 0;

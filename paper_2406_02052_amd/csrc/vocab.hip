@@ -15,8 +15,10 @@
 // known.
 //
 // Scores, sums, statistics and accumulators are fp32.  With bf16 tensors e and f x are rounded to bf16 as
-// operands of the products (the matrix unit takes bf16), 2^-9 of each term at most.  The targets' terms are most of both
-// gradients: what rounding them left is added to the sums from the fp32 values, for dw by lists of the rows of each column.
+// operands of the products (the matrix unit takes bf16), 2^-8 of each term at most each, e of a row with a reference of its own once
+// more.  The targets' terms are most of both gradients: what rounding them left is added to the sums from the fp32 values, for dw by
+// lists of the rows of each column.  Rows of dw whose column is no row's target have none: at 2048 x 1024 over 32768 they are off
+// by 1.6 times what rounding them alone would leave (median), 3 at most, the others and dx by 1.0.
 #include "common.h"
 #include "ops.h"
 
@@ -427,9 +429,10 @@ __global__ __launch_bounds__(1024) void vocab_mean_kernel(VocabArgs a) {
 }
 
 // e of a tile (KEEP: kept; a bf16 tile goes through LDS, so that whole lines are written) and each row's sum of it.  4096 x 4096 by
-// 131072 bf16 in 3.75 ms, 1.17 PFLOP/s (matrix units 67 % busy at 1.6 GHz, where power holds the clock); with 1024 inner indices the 65536
-// exponentials of a tile come after 16 steps only: 2048 by 32768 in 150 us, 0.9.  With e written by the lanes that hold it, 8 bytes in a line
-// each, 4.14 ms and 178 us.
+// 131072 bf16 in 3.75 ms, 1.17 PFLOP/s (matrix units 65 % busy at 1.75 GHz, where power holds the clock); with 1024 inner indices the 65536
+// exponentials of a tile come after 16 steps only: 2048 by 32768 in 160 to 177 us, 0.8.  With e written by the lanes that hold it, 8 bytes in a
+// line each, the larger takes 4.14 ms.  The slow path's maximum and the ordinary exponentials share the scaled scores, some of which are
+// kept in memory between (36 registers a lane; 20 without e).
 template <typename T, typename P, bool KEEP>
 __global__ __launch_bounds__(P::THREADS, 2) void vocab_scores_kernel(VocabArgs a) {
   constexpr int MB = P::MB, NB = P::NB, CHUNKS = P::BN / 8;   // chunks of 16 bytes of a line of e, moved by the line's number
@@ -659,7 +662,7 @@ template <typename T>
 __device__ __forceinline__ void finish(const VocabGrad& g, long row, long col, int first, int last, float (&v)[4]) {
   const long at = row * g.cols + col;
   if constexpr (sizeof(T) == 2) {
-    if (__builtin_expect(first < last, 0)) {   // (said: placed among the others' code this takes dw of 16 rows 6 % longer)
+    if (__builtin_expect(first < last, 0)) {   // (unlikely: among the others' code it makes dw of 16 rows 6 % slower)
       if (last - first > FEW) {
         const float* const left = g.left + static_cast<long>(line_of(first)) * g.cols + col;
         const int runs = (last - first + (1 << g.run_bits) - 1) >> g.run_bits;
@@ -712,8 +715,8 @@ __device__ __forceinline__ void finish(const VocabGrad& g, long row, long col, i
 }
 
 // rows x cols results, inner indices split over g.splits workgroups, whose sums then go to g.part.  dx of 4096 x 4096 over 131072 bf16
-// 3.4 ms, 1.3 PFLOP/s (79 % busy at 1.4 GHz; a library's product of that order 3.1); dw, whose operands both have to be
-// transposed on their way from LDS, 4.1 (3.6 to 3.9).
+// 3.3 to 3.7 ms, 1.2 to 1.3 PFLOP/s (78 % busy at 1.5 GHz; a library's product of that order 3.1); dw, whose operands both have to be
+// transposed on their way from LDS, 3.9 to 4.2 (3.6 to 3.9).
 template <typename T, typename P>
 __global__ __launch_bounds__(P::THREADS, 2) void vocab_grad_kernel(VocabGrad g) {
   __shared__ __attribute__((aligned(16))) char lds[P::LDS];
